@@ -377,9 +377,132 @@ int skipconv_frame_macs(skipconv_t h, void* stream, uint64_t* dense, uint64_t* a
 /* Static text for a status code. Host only. */
 const char* skipconv_status_string(int status);
 
-/* Last error message recorded on this handle (or the last failed create on
- * this thread when h is NULL); never NULL. Host only. */
+/* Last error message recorded on this handle (or, when h is NULL, of the last
+ * failed create or call without a handle on this thread); never NULL. Host only. */
 const char* skipconv_last_error(skipconv_t h);
+
+/* ---- attention over a stream's earlier tokens ----
+ *
+ * A 1 x 1 layer's activation output, N x H x W x (heads * head_dim), is a tensor
+ * of tokens x heads x head_dim. The calls below turn such queries and keys by
+ * their positions, keep the keys and values of earlier frames in a paged
+ * cache, and attend from each frame's new tokens to it. They keep no
+ * handle: every call describes its tensors, allocates nothing, copies nothing
+ * to the host and enqueues its kernels on `stream`, so it may be captured in a
+ * graph. Strides are in elements; the last dimension is packed. Errors are
+ * recorded for skipconv_last_error(NULL) (of the calling thread). */
+
+/* Pairs of a head's elements that turn together: HALVES (j, j + pairs),
+ * ADJACENT (2 j, 2 j + 1), j < pairs. */
+enum { SKIPCONV_PAIR_HALVES = 0, SKIPCONV_PAIR_ADJACENT = 1 };
+
+/* Rotary positions with several axes. Token t has integer positions
+ * pos[t][a] (frame, row, column, ...); pair j of every head turns by
+ *   angle(t, j) = sum over a of pos[t][a] * freq[a][j],
+ *   (u, w) -> (u cos - w sin, w cos + u sin).
+ * A table with one nonzero per column deals the pairs to the axes; one with
+ * several mixes them. Elements past 2 * pairs stay. Angles are formed in 64
+ * bits, the elements in 32, rounded once to the dtype. `inverse` turns by
+ * -angle, which is also the gradient: the rotation is orthogonal, dx = R^T dy. */
+typedef struct skipconv_rotary {
+  const int32_t* pos;   /* device, tokens x axes */
+  const float* freq;    /* device, axes x pairs */
+  int32_t axes;         /* 1..8 */
+  int32_t pairs;        /* 1..head_dim / 2 */
+  int32_t pairing;      /* SKIPCONV_PAIR_* */
+  int32_t inverse;      /* 0 or 1 */
+} skipconv_rotary;
+
+/* Turn x (tokens x heads x head_dim) into y, which may be x itself with the
+ * same strides but must not overlap it otherwise. Any strides and alignment:
+ * 16-byte accesses are used where pointers, strides and head_dim are multiples
+ * of 16 bytes. tokens, heads >= 0 (0: nothing to do), head_dim 2..1024. */
+int skipconv_rotate(const skipconv_rotary* r, int64_t tokens, int32_t heads, int32_t head_dim, int32_t dtype,
+                    const void* x, int64_t x_token, int64_t x_head, void* y, int64_t y_token, int64_t y_head,
+                    void* stream);
+
+/* A paged cache and a batch of sequences in it. Pages hold page_size
+ * consecutive tokens of one sequence; page p, key head h, slot s of the keys
+ * begins at k_pages + p * k_page + h * k_head + s * k_slot, of the values
+ * likewise. Token l of sequence b lies in page
+ * page_table[b * table_width + l / page_size], slot l % page_size.
+ * Sequence b has the rows row_start[b] .. row_start[b + 1] of the new tokens'
+ * tensors, and kv_len[b] tokens in the cache with them: row i of n is token
+ * kv_len[b] - n + i. A sequence may have no new tokens, or none at all; rows
+ * past row_start[batch] belong to no sequence and nothing is written for them.
+ * The three arrays are read on the device: their values cannot be
+ * refused by the call. No value of theirs makes a kernel read or write
+ * outside the tensors described here; entries of the page table that hold no
+ * token that a row sees may hold anything. */
+typedef struct skipconv_cache {
+  void* k_pages;              /* device, 16-byte aligned */
+  void* v_pages;
+  int64_t k_page, k_head, k_slot;  /* multiples of 16 bytes */
+  int64_t v_page, v_head, v_slot;
+  const int32_t* page_table;  /* device, batch x table_width */
+  const int32_t* row_start;   /* device, batch + 1, ascending */
+  const int32_t* kv_len;      /* device, batch */
+  int64_t tokens;             /* rows of the new tokens' tensors */
+  int32_t batch, table_width; /* >= 0; >= 1; table_width * page_size <= 2^30 */
+  int32_t pages, page_size;   /* >= 1 */
+  int32_t kv_heads, head_dim; /* >= 1; a multiple of 8, 8..256 */
+  int32_t dtype;              /* SKIPCONV_F32 or SKIPCONV_BF16: cache and new tokens */
+} skipconv_cache;
+
+/* Append the new tokens' keys and values (tokens x kv_heads x head_dim) to the
+ * cache; with a rotation, the keys turn on the way. With queries (tokens x
+ * q_heads x head_dim; NULL: none), these turn in the same launch into q_out,
+ * which may be q. Tokens whose page number is outside the cache are
+ * left out. q, k, v and q_out take any strides and alignment, like
+ * skipconv_rotate's tensors. Two rows that share a slot of the cache race. */
+typedef struct skipconv_append {
+  const void* k;
+  const void* v;
+  const void* q;
+  void* q_out;
+  int64_t k_token, k_head, v_token, v_head, q_token, q_head, q_out_token, q_out_head;
+  int32_t q_heads;
+  const skipconv_rotary* rotary;  /* NULL: nothing turns (q must be NULL) */
+} skipconv_append;
+int skipconv_cache_append(const skipconv_cache* c, const skipconv_append* a, void* stream);
+
+/* Attention of the new tokens over the cache (the new tokens appended before).
+ * Query head h reads key head h / (q_heads / kv_heads). For the row at token
+ * position p = kv_len - n + i of its sequence:
+ *   causal 1: it sees the tokens l <= p, and of those l >= p - window;
+ *   causal 0: it sees the whole sequence (the chunk's tokens see each other),
+ *             of that l >= (kv_len - n) - window;
+ *   window < 0: no lower bound.
+ *   out = sum over the seen l of softmax(scale q . k_l) v_l,
+ *   lse = log of the sum over the seen l of exp(scale q . k_l) (NULL: not kept).
+ * A row that sees nothing has out = 0 and lse = -inf. Keys and values that a row
+ * does not see do not reach it, whatever they hold (NaN and infinities too).
+ * Scores, sums and outputs are formed in 32 bits; for bf16 the exponentials are
+ * rounded to bf16 for the product with v. max_new: the most new tokens that a
+ * sequence has, or more (0: not known); it selects the kernel, and the results
+ * are right whatever it is. */
+typedef struct skipconv_attend {
+  const void* q;         /* tokens x q_heads x head_dim, 16-byte aligned with strides of whole 16 bytes */
+  void* out;             /* likewise; must not overlap any input */
+  float* lse;            /* tokens x q_heads, or NULL */
+  int64_t q_token, q_head, out_token, out_head;
+  int32_t q_heads;       /* a multiple of kv_heads */
+  int32_t causal;        /* 0 or 1 */
+  int32_t window;
+  float scale;           /* > 0, finite */
+  int32_t max_new;
+} skipconv_attend;
+
+/* Device bytes that skipconv_cache_attend needs for these descriptions (0
+ * where it needs none); pointers are not looked at. Host only. */
+int skipconv_attend_workspace(const skipconv_cache* c, const skipconv_attend* a, size_t* bytes);
+
+/* workspace: device pointer, 16-byte aligned, of at least that many bytes; its contents
+ * need not be kept. Calls that may overlap need workspaces of their own.
+ * Keys are split over workgroups where the rows alone would not fill the GPU; the
+ * partial results are joined in a fixed order, so equal calls give equal bits. */
+int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /* ---- kernel timing (benchmarks) ----
  * Time kernel by kernel, with HIP events recorded on the step's stream, every

@@ -1,0 +1,84 @@
+// Parameter blocks and launchers of the streaming attention operators (host + device):
+// rotary positions, appending to a paged cache, attention over it.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sc {
+
+// The paged cache and what says where a batch's tokens lie in it. Strides in elements.
+struct CacheView {
+  char* k;
+  char* v;
+  int64_t k_page, k_head, k_slot, v_page, v_head, v_slot;
+  const int32_t* table;      // batch x width page numbers
+  const int32_t* row_start;  // batch + 1
+  const int32_t* kv_len;     // batch
+  int batch, width, page_size, pages;
+  uint32_t magic;            // position / page_size = umulhi(2 * position, magic) >> shift
+  int shift;
+  int tokens;                // rows of the new tokens' tensors
+};
+
+// position / page_size for 0 <= position < 2^31. magic = ceil(2^(31 + shift) / d) with
+// 2^shift the least power of two >= d: the product's excess is below 2^31 * 2^shift / 2^(31 + shift)
+// parts of 1 / d, so truncation gives the quotient.
+__host__ __device__ __forceinline__ int page_of(const CacheView& c, int position) {
+  return (int)((((uint64_t)(2u * (uint32_t)position) * c.magic) >> 32) >> c.shift);
+}
+
+// Heads of up to three tensors turned (or copied) in one launch: queries into a tensor, keys and values into the cache.
+struct RotateParams {
+  const char* src[3];
+  int64_t src_token[3], src_head[3];
+  char* dst;                  // of the queries
+  int64_t dst_token, dst_head;
+  int heads[3];
+  CacheView cache;            // used where `paged`
+  const int32_t* pos;         // tokens x axes
+  const float* freq;          // axes x pairs; NULL = nothing turns
+  int tokens, dim, axes, pairs;
+  int adjacent;
+  float sign;                 // -1 turns back
+  int paged;                  // 1: keys and values go to the cache, and rows of no sequence are left alone
+  int tok_per_wg, heads_per_wg, head_groups;  // set by the launcher
+};
+
+// dtype: SKIPCONV_*; mode: what a thread turns at a time (see sc_rotary.hip).
+hipError_t launch_rotate(const RotateParams& p, int dtype, int mode, hipStream_t stream);
+
+struct AttendParams {
+  CacheView c;
+  const char* q;
+  char* out;
+  float* lse;        // tokens x q_heads or NULL
+  float* part_o;     // per unit: rows x dim
+  float* part_ml;    // per unit: rows x {reference, sum}
+  int64_t q_token, q_head, o_token, o_head;
+  int q_heads, kv_heads, group, dim;
+  int causal, window;
+  float scale_log2;  // scale * log2(e)
+  int log_rows;      // a unit's rows (new tokens x query heads of one key head): 2^log_rows
+  int keys;          // rows of a key tile: chunks are whole tiles
+  int target;        // units wanted per key head; 0: a tile's keys are never split
+  int min_chunk;     // fewest keys of a unit where they are split
+  int units;         // workgroups of the launch, and parts in the workspace
+};
+
+constexpr int kMostKeys = 1 << 30;  // positions of a sequence stay below it
+constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel
+constexpr int kLogFewRows = 4;      // rows of a block of the few-rows kernel, which takes one or two
+
+// Rows of a key tile. The wide kernel's: two buffers of keys and values take 64 KB where the head allows 32 rows or more.
+inline int wide_keys_of(int elem_bytes, int dim) { return dim * elem_bytes > 256 ? 32 : 64; }
+inline int few_keys_of(int elem_bytes) { return elem_bytes == 2 ? 32 : 16; }
+int few_waves_of(int elem_bytes, int dim);  // waves of a workgroup of the few-rows kernel
+
+hipError_t launch_attend_wide_bf16(const AttendParams& p, int uniform_pages, hipStream_t stream);
+hipError_t launch_attend_wide_f32(const AttendParams& p, int uniform_pages, hipStream_t stream);
+hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream);
+hipError_t launch_attend_few_f32(const AttendParams& p, hipStream_t stream);
+hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream);
+
+}  // namespace sc

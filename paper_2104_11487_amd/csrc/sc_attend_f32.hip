@@ -1,0 +1,10 @@
+// Attention over the paged cache, many rows at once, fp32 (sc_attend_wide.h).
+#include "sc_attend_wide.h"
+
+namespace sc {
+
+hipError_t launch_attend_wide_f32(const AttendParams& p, int uniform_pages, hipStream_t stream) {
+  return launch_wide_dim<float>(p, uniform_pages, stream);
+}
+
+}  // namespace sc

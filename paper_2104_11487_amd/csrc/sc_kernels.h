@@ -8,6 +8,8 @@
 
 namespace sc {
 
+char* thread_error();  // the message skipconv_last_error(NULL) returns on this thread (256 bytes)
+
 // counters[] slots in the workspace
 constexpr int kCtrCount = 0;  // active blocks of the last gate pass
 constexpr int kCtrSpare = 1;

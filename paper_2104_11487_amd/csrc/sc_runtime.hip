@@ -1034,6 +1034,9 @@ void destroy_events(skipconv_layer* h) {
 
 }  // namespace
 
+// The message that skipconv_last_error(NULL) returns on this thread (256 bytes).
+char* sc::thread_error() { return g_create_error; }
+
 extern "C" {
 
 int skipconv_desc_init(skipconv_desc* d) {

@@ -44,6 +44,31 @@ class skipconv_desc(ctypes.Structure):
                 ("eps", ctypes.c_float), ("gate", ctypes.c_int32)]
 
 
+class skipconv_rotary(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("freq", ctypes.c_void_p), ("axes", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("inverse", ctypes.c_int32)]
+
+
+class skipconv_cache(ctypes.Structure):
+    _fields_ = ([("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p)]
+                + [(f"{t}_{d}", ctypes.c_int64) for t in "kv" for d in ("page", "head", "slot")]
+                + [(n, ctypes.c_void_p) for n in ("page_table", "row_start", "kv_len")] + [("tokens", ctypes.c_int64)]
+                + [(n, ctypes.c_int32) for n in ("batch", "table_width", "pages", "page_size", "kv_heads", "head_dim", "dtype")])
+
+
+class skipconv_append(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "q", "q_out")]
+                + [(f"{t}_{d}", ctypes.c_int64) for t in ("k", "v", "q", "q_out") for d in ("token", "head")]
+                + [("q_heads", ctypes.c_int32), ("rotary", ctypes.POINTER(skipconv_rotary))])
+
+
+class skipconv_attend(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "out", "lse")]
+                + [(f"{t}_{d}", ctypes.c_int64) for t in ("q", "out") for d in ("token", "head")]
+                + [("q_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float),
+                   ("max_new", ctypes.c_int32)])
+
+
 class SkipConvError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"skipconv error {code}: {msg}")
@@ -85,6 +110,13 @@ _SIGS = {
                                            ctypes.POINTER(ctypes.c_uint64)]),
     "skipconv_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "skipconv_last_error": (ctypes.c_char_p, [_P]),
+    "skipconv_rotate": (ctypes.c_int, [ctypes.POINTER(skipconv_rotary), ctypes.c_int64] + [ctypes.c_int32] * 3
+                        + [_P, ctypes.c_int64, ctypes.c_int64] * 2 + [_P]),
+    "skipconv_cache_append": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_append), _P]),
+    "skipconv_attend_workspace": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_attend),
+                                                 ctypes.POINTER(ctypes.c_size_t)]),
+    "skipconv_cache_attend": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_attend), _P,
+                                             ctypes.c_size_t, _P]),
     "skipconv_timing_begin": (ctypes.c_int, [_P, ctypes.c_int, ctypes.c_int]),
     "skipconv_timing_read": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_double),
                                             ctypes.POINTER(ctypes.c_int), _P, ctypes.c_int]),
