@@ -248,7 +248,8 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
     while (chunks * 16 < ((c->head_dim + 31) / 32 * 32) * elem) chunks *= 2;
     const int rows = 64 / chunks;
     const int64_t reach = (int64_t)rows * std::max(c->k_slot, c->v_slot) * elem;
-    const int uniform = c->page_size % rows == 0 && reach < (1ll << 31);
+    const int64_t page_bytes = std::max(c->k_page, c->v_page) * elem;
+    const int uniform = c->page_size % rows == 0 && reach < (1ll << 31) && page_bytes < (1ll << 32);
     e = elem == 2 ? sc::launch_attend_wide_bf16(p, uniform, s) : sc::launch_attend_wide_f32(p, uniform, s);
   }
   if (e == hipSuccess && plan.target) e = sc::launch_attend_join(p, elem, s);

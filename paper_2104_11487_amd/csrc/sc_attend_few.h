@@ -45,27 +45,20 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     __syncthreads();
   }
 
-  const char* kb = p.c.k + (int64_t)u.head * p.c.k_head * (int64_t)sizeof(T);
-  const char* vb = p.c.v + (int64_t)u.head * p.c.v_head * (int64_t)sizeof(T);
   constexpr int kStep = KEYS * NW;
   const int begin = u.lo + wave * KEYS;
   const int count = begin < u.hi ? (u.hi - begin + kStep - 1) / kStep : 0;  // tiles of this wave
 
   // Page numbers are looked up three tiles ahead and copies run two tiles ahead, so that no wait for
   // a page number waits for the copies behind it.
-  using Src = Source<TL, false>;
-  Src ahead, next;
+  Stager<T, TL, 1, false> ahead(p, u, 0, lane, chunks), next(p, u, 0, lane, chunks);
   if (count > 0) {
-    Src s0, s1;
-    find_pages<TL, 1>(p.c, u.b, begin, 0, lane, &s0);
-    find_pages<TL, 1>(p.c, u.b, min(begin + kStep, kMostKeys), 0, lane, &s1);
-    find_pages<TL, 1>(p.c, u.b, min(begin + 2 * kStep, kMostKeys), 0, lane, &next);
-    stage<T, TL, 1>(kb, p.c.k_page, p.c.k_slot, s0, chunks, 0, lane, mine);
-    stage<T, TL, 1>(vb, p.c.v_page, p.c.v_slot, s0, chunks, 0, lane, mine + TL::kBytes);
-    if (count > 1) {
-      stage<T, TL, 1>(kb, p.c.k_page, p.c.k_slot, s1, chunks, 0, lane, mine + 2 * TL::kBytes);
-      stage<T, TL, 1>(vb, p.c.v_page, p.c.v_slot, s1, chunks, 0, lane, mine + 3 * TL::kBytes);
-    }
+    Stager<T, TL, 1, false> zero(p, u, 0, lane, chunks);
+    zero.find(begin);
+    ahead.find(begin + kStep);
+    next.find(begin + 2 * kStep);
+    zero.copy(mine, mine + TL::kBytes);
+    if (count > 1) ahead.copy(mine + 2 * TL::kBytes, mine + 3 * TL::kBytes);
   }
 
   // the rows' queries, in the operand's layout
@@ -239,10 +232,9 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     // this tile's buffers are free: the fragments read from them have reached their products
     if (it + 2 < count) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      ahead = next;
-      find_pages<TL, 1>(p.c, u.b, min(key0 + 3 * kStep, kMostKeys), 0, lane, &next);
-      stage<T, TL, 1>(kb, p.c.k_page, p.c.k_slot, ahead, chunks, 0, lane, kt);
-      stage<T, TL, 1>(vb, p.c.v_page, p.c.v_slot, ahead, chunks, 0, lane, vt);
+      ahead.take(next);
+      next.find(key0 + 3 * kStep);
+      ahead.copy(kt, vt);
     }
   }
 

@@ -47,41 +47,69 @@ struct Tile {
   }
 };
 
-// Where a wave's loads of one tile come from. UNI: the rows of a load lie in one page (page sizes that are a multiple of
-// kGroup), so the page is looked up once a load, by the scalar unit; otherwise each lane looks up its row.
-template <typename TL, bool UNI>
-struct Source {
-  int page[TL::kLoads], slot[TL::kLoads];
-};
-
-template <typename TL, int NW, bool UNI>
-__device__ __forceinline__ void find_pages(const CacheView& c, int b, int key0, int wave, int lane, Source<TL, UNI>* s) {
-#pragma unroll
-  for (int t = 0; t < TL::kLoads; ++t) {
-    const int row = (t * NW + wave) * TL::kGroup + (UNI ? 0 : lane / TL::kChunks);
-    s->page[t] = page_at(c, b, key0 + row, UNI ? TL::kGroup : 1, &s->slot[t]);
-  }
-}
-
-// Copies the tile's rows of one head (keys or values) into LDS at `to`.
+// A wave's share of the copies of one tile of keys and one of values, in two steps, so that page numbers are looked up a
+// tile before the copies that need them.
+//
+// UNI: the rows of each load lie in one page (page sizes that are a multiple of kGroup). Then lane i finds the address of
+// load i's first row (keys, then values), all loads in one go, and the copies take it as their scalar base: their
+// lanes' offsets to it never change. Otherwise each lane finds its own row's.
 template <typename T, typename TL, int NW, bool UNI>
-__device__ __forceinline__ void stage(const char* base, int64_t page_stride, int64_t slot_stride, const Source<TL, UNI>& s, int chunks,
-                                      int wave, int lane, char* to) {
-  const int in = lane / TL::kChunks, at = lane % TL::kChunks;
-#pragma unroll
-  for (int t = 0; t < TL::kLoads; ++t) {
-    const int g = t * NW + wave;
-    const int chunk = at ^ (TL::swizzle(g * TL::kGroup + in) & (TL::kChunks - 1));
-    const char* from;
+struct Stager {
+  const AttendParams& p;
+  const int b, lane, wave, chunks;
+  const char* kb;
+  const char* vb;
+  int page[UNI ? 1 : TL::kLoads], slot[UNI ? 1 : TL::kLoads];
+
+  __device__ __forceinline__ Stager(const AttendParams& q, const Unit& u, int w, int l, int c)
+      : p(q), b(u.b), lane(l), wave(w), chunks(c), kb(q.c.k + (int64_t)u.head * q.c.k_head * (int64_t)sizeof(T)),
+        vb(q.c.v + (int64_t)u.head * q.c.v_head * (int64_t)sizeof(T)) {}
+
+  __device__ __forceinline__ void find(int key0) {
     if constexpr (UNI) {
-      const char* row0 = base + ((int64_t)s.page[t] * page_stride + (int64_t)s.slot[t] * slot_stride) * (int64_t)sizeof(T);
-      from = row0 + (uint32_t)(in * (int)slot_stride * (int)sizeof(T) + chunk * 16);
+      page[0] = page_at(p.c, b, key0 + ((lane % TL::kLoads) * NW + wave) * TL::kGroup, TL::kGroup, &slot[0]);
     } else {
-      from = base + ((int64_t)s.page[t] * page_stride + (int64_t)s.slot[t] * slot_stride) * (int64_t)sizeof(T) + chunk * 16;
+#pragma unroll
+      for (int t = 0; t < TL::kLoads; ++t) page[t] = page_at(p.c, b, key0 + (t * NW + wave) * TL::kGroup + lane / TL::kChunks, 1, &slot[t]);
     }
-    if (chunk < chunks) __builtin_amdgcn_global_load_lds(from, SC_LDS(to + g * 1024, void), 16, 0, 0);
   }
-}
+
+  __device__ __forceinline__ void take(const Stager& other) {
+#pragma unroll
+    for (int t = 0; t < (UNI ? 1 : TL::kLoads); ++t) page[t] = other.page[t], slot[t] = other.slot[t];
+  }
+
+  __device__ __forceinline__ int chunk_of(int t) const {  // that this lane's 16 bytes of load t come from
+    return (lane % TL::kChunks) ^ (TL::swizzle((t * NW + wave) * TL::kGroup + lane / TL::kChunks) & (TL::kChunks - 1));
+  }
+
+  __device__ __forceinline__ void copy(char* keys, char* values) const {
+    if constexpr (UNI) {
+      const bool val = (lane / TL::kLoads) & 1;
+      const uint64_t row0 = (uint64_t)(val ? vb : kb) + (uint64_t)(uint32_t)page[0] * (uint32_t)((val ? p.c.v_page : p.c.k_page) * sizeof(T)) +
+                            (uint64_t)(uint32_t)slot[0] * (uint32_t)((val ? p.c.v_slot : p.c.k_slot) * sizeof(T));
+      const int lo = (int)(uint32_t)row0, hi = (int)(uint32_t)(row0 >> 32);
+#pragma unroll
+      for (int i = 0; i < 2 * TL::kLoads; ++i) {
+        const int t = i % TL::kLoads;
+        const char* from = reinterpret_cast<const char*>(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32) | (uint32_t)__builtin_amdgcn_readlane(lo, i));
+        const int stride = (int)((i < TL::kLoads ? p.c.k_slot : p.c.v_slot) * (int)sizeof(T));
+        const uint32_t off = (uint32_t)((lane / TL::kChunks) * stride + chunk_of(t) * 16);
+        char* to = (i < TL::kLoads ? keys : values) + (t * NW + wave) * 1024;
+        if (chunk_of(t) < chunks) __builtin_amdgcn_global_load_lds(from + off, SC_LDS(to, void), 16, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2 * TL::kLoads; ++i) {
+        const int t = i % TL::kLoads;
+        const bool val = i >= TL::kLoads;
+        const char* from = (val ? vb : kb) + ((int64_t)page[t] * (val ? p.c.v_page : p.c.k_page) + (int64_t)slot[t] * (val ? p.c.v_slot : p.c.k_slot)) * (int64_t)sizeof(T) + chunk_of(t) * 16;
+        char* to = (val ? values : keys) + (t * NW + wave) * 1024;
+        if (chunk_of(t) < chunks) __builtin_amdgcn_global_load_lds(from, SC_LDS(to, void), 16, 0, 0);
+      }
+    }
+  }
+};
 
 // Four bf16 of one column, from four consecutive rows: lane l of each 16 lanes gives the address of row l / 4,
 // columns 4 (l % 4).., and receives column l.

@@ -13,13 +13,13 @@
 // more, which after the first tiles is seldom.
 #pragma once
 
+#include <type_traits>
+
 #include "sc_attend_tile.h"
 
 #pragma clang fp contract(off)
 
 namespace sc {
-
-template <typename T> struct Wide;
 
 // Keys of a tile: two buffers of keys and values take 64 KB where the head allows 32 rows or more of it.
 template <typename T, int DP>
@@ -46,7 +46,6 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
   const int rows = u.n * p.group;
   const int row0 = u.row0 + 32 * wave, row = row0 + col;
   const int chunks = p.dim / TL::kElems;
-  const bool live = row0 < rows;  // the wave has rows at all
 
   // the row's queries: lane `half` holds the dimensions that its k indexes of the products stand for
   uint4 qf[QF];
@@ -66,51 +65,30 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
   }
 
   const Seen seen = seen_by(p, u, row);
-  // of the wave's rows: keys that all see are [all_lo, all_hi], that any sees [any_lo, any_hi]
-  const Seen first = seen_by(p, u, row0), last = seen_by(p, u, row0 + 31);
-  const int all_lo = last.lo, all_hi = first.hi, any_lo = first.lo, any_hi = last.hi;
-
-  const char* kb = p.c.k + (int64_t)u.head * p.c.k_head * (int64_t)sizeof(T);
-  const char* vb = p.c.v + (int64_t)u.head * p.c.v_head * (int64_t)sizeof(T);
+  // keys that every row of the unit sees are [all_lo, all_hi]; that a row of the wave sees, [any_lo, any_hi]
+  const int all_lo = seen_by(p, u, u.row0 + ROWS - 1).lo, all_hi = seen_by(p, u, u.row0).hi;
+  const int any_lo = seen_by(p, u, row0).lo, any_hi = row0 < rows ? seen_by(p, u, row0 + 31).hi : -1;
 
   floatx16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = floatx16{};
   float ref = kNegInf, sum = 0.0f;
 
-  Source<TL, UNI> src;
-  if (u.lo < u.hi) {
-    find_pages<TL, NW>(p.c, u.b, u.lo, wave, lane, &src);
-    stage<T, TL, NW>(kb, p.c.k_page, p.c.k_slot, src, chunks, wave, lane, lds);
-    stage<T, TL, NW>(vb, p.c.v_page, p.c.v_slot, src, chunks, wave, lane, lds + 2 * TL::kBytes);
-    find_pages<TL, NW>(p.c, u.b, min(u.lo + KEYS, u.hi - 1), wave, lane, &src);
-  }
   // scores: row (key) col of a 32-key block, 16-byte piece 2 i + half; values: see read_column4
   const int krow = TL::swizzle(col) & (TL::kChunks - 1);
-  const char* kbase = lds + col * TL::kRowBytes;
   const int vr = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const char* kbase = lds + col * TL::kRowBytes;
+  const char* vbase = lds + 2 * TL::kBytes + vr * TL::kRowBytes + (lane & 1) * 8;
 
-  int buf = 0;
-  for (int key0 = u.lo; key0 < u.hi; key0 += KEYS, buf ^= 1) {
-    wait_loads<0>();
-    __syncthreads();
-    if (key0 + KEYS < u.hi) {
-      stage<T, TL, NW>(kb, p.c.k_page, p.c.k_slot, src, chunks, wave, lane, lds + (buf ^ 1) * TL::kBytes);
-      stage<T, TL, NW>(vb, p.c.v_page, p.c.v_slot, src, chunks, wave, lane, lds + (2 + (buf ^ 1)) * TL::kBytes);
-      find_pages<TL, NW>(p.c, u.b, min(key0 + 2 * KEYS, u.hi - 1), wave, lane, &src);
-    }
-    if (!live || key0 > any_hi || key0 + KEYS <= any_lo) continue;
-    const bool edge = key0 < all_lo || key0 + KEYS - 1 > all_hi;
-
-    floatx16 s[NS];
+  // Scores of the tile in buffer `buf`, the running reference, and the exponentials in s.
+  auto scores = [&](auto masked, int key0, int buf, floatx16(&s)[NS]) {
 #pragma unroll
     for (int j = 0; j < NS; ++j) s[j] = floatx16{};
-    const char* kt = kbase + buf * TL::kBytes;
 #pragma unroll
     for (int i = 0; i < QF; ++i) {
 #pragma unroll
       for (int j = 0; j < NS; ++j) {
-        const uint4 kf = *reinterpret_cast<const uint4*>(kt + j * 32 * TL::kRowBytes + (((2 * i + half) ^ krow) << 4));
+        const uint4 kf = *reinterpret_cast<const uint4*>(kbase + (((2 * i + half) ^ krow) << 4) + buf * TL::kBytes + j * 32 * TL::kRowBytes);
         if constexpr (kHalf) {
           s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), s[j], 0, 0, 0);
         } else {
@@ -120,7 +98,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
         }
       }
     }
-    if (edge) {
+    if constexpr (masked) {
 #pragma unroll
       for (int j = 0; j < NS; ++j)
 #pragma unroll
@@ -145,7 +123,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= keep;
     }
-    const float base = ref == kNegInf ? 0.0f : ref;
+    const float base = masked && ref == kNegInf ? 0.0f : ref;
 #pragma unroll
     for (int j = 0; j < NS; ++j)
 #pragma unroll
@@ -153,113 +131,136 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
         s[j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], p.scale_log2, -base));
         sum += s[j][r];
       }
+  };
+  auto exponentials = [](const floatx16& x, int r) {  // eight of them as the product's operand
+    const uint4 w{pack2(x[r], x[r + 1]), pack2(x[r + 2], x[r + 3]), pack2(x[r + 4], x[r + 5]), pack2(x[r + 6], x[r + 7])};
+    return __builtin_bit_cast(bf16x8, w);
+  };
+  auto column4 = [&](int buf, int k, int e, int d) {
+    const int c = (4 * d + vc) ^ (TL::swizzle(8 * e + vr + 16 * k) & (TL::kChunks - 1));
+    return read_column4(vbase + c * 16 + buf * TL::kBytes + (16 * k + 8 * e) * TL::kRowBytes);
+  };
+  auto value1 = [&](int buf, int key, int d) {
+    const int e = 32 * d + col, c = (e >> 2) ^ (TL::swizzle(key) & (TL::kChunks - 1));
+    return *reinterpret_cast<const float*>(lds + (2 + buf) * TL::kBytes + key * TL::kRowBytes + c * 16 + (e & 3) * 4);
+  };
 
-    const char* vt = lds + (2 + buf) * TL::kBytes;
-    if (!edge) {
-      if constexpr (kHalf) {
+  // A tile whose keys every row sees.
+  auto whole_tile = [&](int key0, int buf) {
+    floatx16 s[NS];
+    scores(std::false_type{}, key0, buf, s);
+    if constexpr (kHalf) {
 #pragma unroll
-        for (int k = 0; k < KEYS / 16; ++k) {
-          bf16x8 pf;
-          {
-            const floatx16& x = s[k >> 1];
-            const int r = 8 * (k & 1);
-            uint4 w{pack2(x[r], x[r + 1]), pack2(x[r + 2], x[r + 3]), pack2(x[r + 4], x[r + 5]), pack2(x[r + 6], x[r + 7])};
-            pf = __builtin_bit_cast(bf16x8, w);
-          }
+      for (int k = 0; k < KEYS / 16; ++k) {
+        const bf16x8 pf = exponentials(s[k >> 1], 8 * (k & 1));
 #pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            u32x2 q[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int r = 16 * k + 8 * e + vr, c = (4 * d + vc) ^ (TL::swizzle(8 * e + vr + 16 * k) & (TL::kChunks - 1));
-              q[e] = read_column4(vt + r * TL::kRowBytes + c * 16 + (lane & 1) * 8);
-            }
-            const uint4 a{q[0][0], q[0][1], q[1][0], q[1][1]};
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, o[d], 0, 0, 0);
-          }
+        for (int d = 0; d < ND; ++d) {
+          const u32x2 a = column4(buf, k, 0, d), b = column4(buf, k, 1, d);
+          const uint4 w{a[0], a[1], b[0], b[1]};
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < NS; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              const int e = 32 * d + col, c = (e >> 2) ^ (TL::swizzle(key) & (TL::kChunks - 1));
-              const float a = *reinterpret_cast<const float*>(vt + key * TL::kRowBytes + c * 16 + (e & 3) * 4);
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, s[j][r], o[d], 0, 0, 0);
-            }
-          }
       }
     } else {
-      // Some row does not see some key here. A masked key's exponential is zero, but zero times an infinity or a NaN is
-      // not: values of keys that no row sees are cleared, and those that are not finite leave the product and
-      // are added to the rows that see their key.
-      int odd = 0;
-      if constexpr (kHalf) {
 #pragma unroll
-        for (int k = 0; k < KEYS / 16; ++k) {
-          const floatx16& x = s[k >> 1];
-          const int x0 = 8 * (k & 1);
-          const uint4 w{pack2(x[x0], x[x0 + 1]), pack2(x[x0 + 2], x[x0 + 3]), pack2(x[x0 + 4], x[x0 + 5]), pack2(x[x0 + 6], x[x0 + 7])};
-          const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
-          uint32_t mask[2][2];
+      for (int j = 0; j < NS; ++j)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
+        for (int r = 0; r < 16; ++r) {
+          const int key = 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int key = key0 + 16 * k + 8 * e + 4 * half + 2 * i;
-              mask[e][i] = (key >= any_lo && key <= any_hi ? 0xffffu : 0u) | (key + 1 >= any_lo && key + 1 <= any_hi ? 0xffff0000u : 0u);
-            }
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            u32x2 q[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int r = 16 * k + 8 * e + vr, c = (4 * d + vc) ^ (TL::swizzle(8 * e + vr + 16 * k) & (TL::kChunks - 1));
-              q[e] = read_column4(vt + r * TL::kRowBytes + c * 16 + (lane & 1) * 8);
-              q[e][0] = finite2(q[e][0], mask[e][0], &odd);
-              q[e][1] = finite2(q[e][1], mask[e][1], &odd);
-            }
-            const uint4 a{q[0][0], q[0][1], q[1][0], q[1][1]};
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), pf, o[d], 0, 0, 0);
-          }
+          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value1(buf, key, d), s[j][r], o[d], 0, 0, 0);
         }
-      } else {
+    }
+  };
+
+  // A tile of which some row does not see some key. A masked key's exponential is zero, but zero times an infinity or a
+  // NaN is not: values of keys that no row of the wave sees are cleared, and those that are not finite leave the product
+  // and are added to the rows that see their key.
+  auto edge_tile = [&](int key0, int buf) {
+    floatx16 s[NS];
+    scores(std::true_type{}, key0, buf, s);
+    int odd = 0;
+    if constexpr (kHalf) {
 #pragma unroll
-        for (int j = 0; j < NS; ++j)
+      for (int k = 0; k < KEYS / 16; ++k) {
+        const bf16x8 pf = exponentials(s[k >> 1], 8 * (k & 1));
+        uint32_t mask[2][2];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int key = 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
-            const bool keep = key0 + key >= any_lo && key0 + key <= any_hi;
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              const int e = 32 * d + col, c = (e >> 2) ^ (TL::swizzle(key) & (TL::kChunks - 1));
-              const float a = *reinterpret_cast<const float*>(vt + key * TL::kRowBytes + c * 16 + (e & 3) * 4);
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(finite1(a, keep, &odd), s[j][r], o[d], 0, 0, 0);
-            }
+          for (int i = 0; i < 2; ++i) {
+            const int key = key0 + 16 * k + 8 * e + 4 * half + 2 * i;
+            mask[e][i] = (key >= any_lo && key <= any_hi ? 0xffffu : 0u) | (key + 1 >= any_lo && key + 1 <= any_hi ? 0xffff0000u : 0u);
           }
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          u32x2 a = column4(buf, k, 0, d), b = column4(buf, k, 1, d);
+          const uint4 w{finite2(a[0], mask[0][0], &odd), finite2(a[1], mask[0][1], &odd), finite2(b[0], mask[1][0], &odd),
+                        finite2(b[1], mask[1][1], &odd)};
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
+        }
       }
-      if (__any(odd)) {
-        const int from = max(key0, any_lo), to = min(key0 + KEYS - 1, any_hi);
-        for (int key = from; key <= to; ++key) {
-          const bool sees = key >= seen.lo && key <= seen.hi;
-          const int r = key - key0, sw = TL::swizzle(r) & (TL::kChunks - 1);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
+          const bool keep = key0 + key >= any_lo && key0 + key <= any_hi;
 #pragma unroll
           for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int e = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
-              const char* at = vt + r * TL::kRowBytes + (((e / TL::kElems) ^ sw) << 4) + (e % TL::kElems) * (int)sizeof(T);
-              float v;
-              if constexpr (kHalf) v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
-              else v = *reinterpret_cast<const float*>(at);
-              if (sees && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[d][i] += v;
-            }
+            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(finite1(value1(buf, key, d), keep, &odd), s[j][r], o[d], 0, 0, 0);
         }
+    }
+    if (__any(odd)) {
+      const int from = max(key0, any_lo), to = min(key0 + KEYS - 1, any_hi);
+      for (int key = from; key <= to; ++key) {
+        const bool sees = key >= seen.lo && key <= seen.hi;
+        const int r = key - key0, sw = TL::swizzle(r) & (TL::kChunks - 1);
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
+            const char* at = lds + (2 + buf) * TL::kBytes + r * TL::kRowBytes + (((e / TL::kElems) ^ sw) << 4) + (e % TL::kElems) * (int)sizeof(T);
+            float v;
+            if constexpr (kHalf) v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
+            else v = *reinterpret_cast<const float*>(at);
+            if (sees && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[d][i] += v;
+          }
       }
     }
+  };
+
+  Stager<T, TL, NW, UNI> stager(p, u, wave, lane, chunks);
+  if (u.lo < u.hi) {
+    stager.find(u.lo);
+    stager.copy(lds, lds + 2 * TL::kBytes);
+    stager.find(u.lo + KEYS);
+  }
+  auto arrive = [&](int key0, int buf) {  // the tile in `buf` has landed; the next one's copies leave
+    wait_loads<0>();
+    __syncthreads();
+    if (key0 + KEYS < u.hi) {
+      stager.copy(lds + (buf ^ 1) * TL::kBytes, lds + (2 + (buf ^ 1)) * TL::kBytes);
+      stager.find(key0 + 2 * KEYS);
+    }
+  };
+  auto whole = [&](int key0) { return key0 >= all_lo && key0 + KEYS - 1 <= all_hi && key0 + KEYS <= u.hi; };
+  int key0 = u.lo, buf = 0;
+  while (key0 < u.hi) {
+    // the tiles that all rows see, two a round so that a buffer's address is a constant
+    while (buf == 0 && whole(key0) && whole(key0 + KEYS)) {
+      arrive(key0, 0);
+      whole_tile(key0, 0);
+      arrive(key0 + KEYS, 1);
+      whole_tile(key0 + KEYS, 1);
+      key0 += 2 * KEYS;
+    }
+    if (key0 >= u.hi) break;
+    arrive(key0, buf);
+    if (key0 <= any_hi && key0 + KEYS > any_lo) edge_tile(key0, buf);
+    key0 += KEYS;
+    buf ^= 1;
   }
 
   sum = sum_across32(sum);
