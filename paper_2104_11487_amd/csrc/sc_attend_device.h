@@ -207,12 +207,14 @@ __device__ __forceinline__ Seen seen_by(const AttendParams& p, const Unit& u, in
   return s;
 }
 
-// Page of key position `at` and its slot there, which `rows` slots of that page begin at. Positions past the table and entries
-// outside the cache are led to slots that exist (no row sees their keys).
-__device__ __forceinline__ int page_at(const CacheView& c, int b, int at, int rows, int* slot) {
+// Where key position `at` lies: the slot, which `rows` slots of its page begin at, and the page table's entry. Positions past the
+// table and entries outside the cache are led to slots that exist (no row sees their keys). The entry is loaded by a
+// relaxed atomic so that the load stays where it is written: ahead of copies that it would otherwise wait for.
+__device__ __forceinline__ int entry_at(const CacheView& c, int b, int at, int rows, int* slot) {
   const int i = min(page_of(c, at), c.width - 1);
   *slot = min(at - i * c.page_size, c.page_size - rows);
-  return min(max(c.table[(int64_t)b * c.width + i], 0), c.pages - 1);
+  return __hip_atomic_load(c.table + (int64_t)b * c.width + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
 }
+__device__ __forceinline__ int page_of_entry(const CacheView& c, int entry) { return min(max(entry, 0), c.pages - 1); }
 
 }  // namespace sc

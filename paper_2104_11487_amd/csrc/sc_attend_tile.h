@@ -47,67 +47,95 @@ struct Tile {
   }
 };
 
-// A wave's share of the copies of one tile of keys and one of values, in two steps, so that page numbers are looked up a
-// tile before the copies that need them.
+// Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane, without a
+// wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
+// takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register is written, and
+// the addresses are read when the instruction issues; M0, the destination's base, is set in the same statement.
+__device__ __forceinline__ void copy16(const char* base, uint32_t off, char* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void copy16(const char* from, char* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(from) : "memory");
+}
+
+// A wave's share of the copies of one tile of keys and one of values (of the keys `lag` before), in two steps, so that page
+// numbers are looked up a tile before the copies that need them.
 //
 // UNI: the rows of each load lie in one page (page sizes that are a multiple of kGroup). Then lane i finds the address of
 // load i's first row (keys, then values), all loads in one go, and the copies take it as their scalar base: their
 // lanes' offsets to it never change. Otherwise each lane finds its own row's.
-template <typename T, typename TL, int NW, bool UNI>
+template <typename T, typename TL, int NW, bool UNI, int LAG = 0>
 struct Stager {
-  const AttendParams& p;
+  const CacheView& c;
   const int b, lane, wave, chunks;
-  const char* kb;
+  const char* kb;                     // the head's first page
   const char* vb;
-  int page[UNI ? 1 : TL::kLoads], slot[UNI ? 1 : TL::kLoads];
+  const char* base;                   // UNI: those of this lane's load
+  uint32_t page_bytes, slot_bytes;
+  static constexpr int kFound = UNI ? 1 : LAG ? 2 * TL::kLoads : TL::kLoads;  // rows that a lane looks up
+  int entry[kFound], slot[kFound];
 
-  __device__ __forceinline__ Stager(const AttendParams& q, const Unit& u, int w, int l, int c)
-      : p(q), b(u.b), lane(l), wave(w), chunks(c), kb(q.c.k + (int64_t)u.head * q.c.k_head * (int64_t)sizeof(T)),
-        vb(q.c.v + (int64_t)u.head * q.c.v_head * (int64_t)sizeof(T)) {}
+  __device__ __forceinline__ Stager(const AttendParams& p, const Unit& u, int w, int l, int n)
+      : c(p.c), b(u.b), lane(l), wave(w), chunks(n), kb(c.k + (int64_t)u.head * c.k_head * (int64_t)sizeof(T)),
+        vb(c.v + (int64_t)u.head * c.v_head * (int64_t)sizeof(T)) {
+    if constexpr (UNI) {
+      const bool val = ((lane / TL::kLoads) & 1) != 0;
+      const int64_t kp = c.k_page, vp = c.v_page, ks = c.k_slot, vs = c.v_slot;
+      base = val ? vb : kb;
+      page_bytes = (uint32_t)((val ? vp : kp) * (int64_t)sizeof(T));
+      slot_bytes = (uint32_t)((val ? vs : ks) * (int64_t)sizeof(T));
+    }
+  }
 
   __device__ __forceinline__ void find(int key0) {
     if constexpr (UNI) {
-      page[0] = page_at(p.c, b, key0 + ((lane % TL::kLoads) * NW + wave) * TL::kGroup, TL::kGroup, &slot[0]);
+      const int lag = ((lane / TL::kLoads) & 1) ? LAG : 0;
+      entry[0] = entry_at(c, b, max(key0 - lag, 0) + ((lane % TL::kLoads) * NW + wave) * TL::kGroup, TL::kGroup, &slot[0]);
     } else {
 #pragma unroll
-      for (int t = 0; t < TL::kLoads; ++t) page[t] = page_at(p.c, b, key0 + (t * NW + wave) * TL::kGroup + lane / TL::kChunks, 1, &slot[t]);
+      for (int i = 0; i < kFound; ++i)
+        entry[i] = entry_at(c, b, max(key0 - (i < TL::kLoads ? 0 : LAG), 0) + (i % TL::kLoads * NW + wave) * TL::kGroup + lane / TL::kChunks, 1, &slot[i]);
     }
   }
 
   __device__ __forceinline__ void take(const Stager& other) {
 #pragma unroll
-    for (int t = 0; t < (UNI ? 1 : TL::kLoads); ++t) page[t] = other.page[t], slot[t] = other.slot[t];
+    for (int t = 0; t < kFound; ++t) entry[t] = other.entry[t], slot[t] = other.slot[t];
   }
 
   __device__ __forceinline__ int chunk_of(int t) const {  // that this lane's 16 bytes of load t come from
     return (lane % TL::kChunks) ^ (TL::swizzle((t * NW + wave) * TL::kGroup + lane / TL::kChunks) & (TL::kChunks - 1));
   }
 
-  __device__ __forceinline__ void copy(char* keys, char* values) const {
-    if constexpr (UNI) {
-      const bool val = (lane / TL::kLoads) & 1;
-      const uint64_t row0 = (uint64_t)(val ? vb : kb) + (uint64_t)(uint32_t)page[0] * (uint32_t)((val ? p.c.v_page : p.c.k_page) * sizeof(T)) +
-                            (uint64_t)(uint32_t)slot[0] * (uint32_t)((val ? p.c.v_slot : p.c.k_slot) * sizeof(T));
-      const int lo = (int)(uint32_t)row0, hi = (int)(uint32_t)(row0 >> 32);
+  // FULL: the head fills its chunks, so every lane copies. PARTS: 1 keys, 2 values, 3 both.
+  template <bool FULL, int PARTS>
+  __device__ __forceinline__ void copy_rows(char* keys, char* values) const {
+    uint64_t row0 = 0;
+    if constexpr (UNI) row0 = (uint64_t)base + (uint64_t)(uint32_t)page_of_entry(c, entry[0]) * page_bytes + (uint64_t)(uint32_t)slot[0] * slot_bytes;
+    const int lo = (int)(uint32_t)row0, hi = (int)(uint32_t)(row0 >> 32);
 #pragma unroll
-      for (int i = 0; i < 2 * TL::kLoads; ++i) {
-        const int t = i % TL::kLoads;
-        const char* from = reinterpret_cast<const char*>(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32) | (uint32_t)__builtin_amdgcn_readlane(lo, i));
-        const int stride = (int)((i < TL::kLoads ? p.c.k_slot : p.c.v_slot) * (int)sizeof(T));
-        const uint32_t off = (uint32_t)((lane / TL::kChunks) * stride + chunk_of(t) * 16);
-        char* to = (i < TL::kLoads ? keys : values) + (t * NW + wave) * 1024;
-        if (chunk_of(t) < chunks) __builtin_amdgcn_global_load_lds(from + off, SC_LDS(to, void), 16, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 2 * TL::kLoads; ++i) {
-        const int t = i % TL::kLoads;
-        const bool val = i >= TL::kLoads;
-        const char* from = (val ? vb : kb) + ((int64_t)page[t] * (val ? p.c.v_page : p.c.k_page) + (int64_t)slot[t] * (val ? p.c.v_slot : p.c.k_slot)) * (int64_t)sizeof(T) + chunk_of(t) * 16;
-        char* to = (val ? values : keys) + (t * NW + wave) * 1024;
-        if (chunk_of(t) < chunks) __builtin_amdgcn_global_load_lds(from, SC_LDS(to, void), 16, 0, 0);
+    for (int i = 0; i < 2 * TL::kLoads; ++i) {
+      const int t = i % TL::kLoads;
+      const bool val = i >= TL::kLoads;
+      if (!(PARTS & (val ? 2 : 1))) continue;
+      const int64_t slot_stride = val ? c.v_slot : c.k_slot, page_stride = val ? c.v_page : c.k_page;
+      char* to = (val ? values : keys) + (t * NW + wave) * 1024;
+      if constexpr (UNI) {
+        const uint64_t first = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32) | (uint32_t)__builtin_amdgcn_readlane(lo, i);
+        const uint32_t off = (uint32_t)((lane / TL::kChunks) * (int)slot_stride * (int)sizeof(T) + chunk_of(t) * 16);
+        if (FULL || chunk_of(t) < chunks) copy16(reinterpret_cast<const char*>(first), off, to);
+      } else {
+        const char* from = (val ? vb : kb) + ((int64_t)page_of_entry(c, entry[i % kFound]) * page_stride + (int64_t)slot[i % kFound] * slot_stride) * (int64_t)sizeof(T) + chunk_of(t) * 16;
+        if (FULL || chunk_of(t) < chunks) copy16(from, to);
       }
     }
+  }
+  template <int PARTS = 3>
+  __device__ __forceinline__ void copy(char* keys, char* values) const {
+    if (chunks == TL::kChunks) copy_rows<true, PARTS>(keys, values);
+    else copy_rows<false, PARTS>(keys, values);
   }
 };
 

@@ -14,6 +14,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "sc_attend_tile.h"
 
@@ -29,6 +30,60 @@ constexpr int wide_keys() {
 
 constexpr int kWideWaves = 4;
 constexpr float kSlack = 8.0f;  // powers of two that an exponential may exceed one by
+
+// f(0), f(1), ... f(N - 1), each with its index as a constant.
+template <int... I, typename F>
+__device__ __forceinline__ void unrolled_(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(F f) {
+  unrolled_(std::make_integer_sequence<int, N>{}, f);
+}
+
+// Order of a tile's products: NQ of the next tile's scores (0 ..), and for each 16 of its NK * 16 keys ND of its values
+// (NQ + k * ND ..). A value product needs its keys' exponentials, the largest score needs all score products: half of the scores
+// (three quarters where there are but two key groups) come first, the rest between the value products.
+template <int NQ, int ND, int NK>
+struct SlotPlan {
+  static constexpr int kSlots = NQ + NK * ND;
+  struct Order {
+    int at[kSlots];
+    int last_score;
+  };
+  static constexpr Order order() {
+    Order o = {};
+    int n = 0, q = 0, upto = NK > 2 ? NQ / 2 : NQ * 3 / 4;
+    for (int k = 0; k <= NK; ++k) {
+      if (k == NK - 1) upto = NQ;
+      while (q < upto) o.last_score = n, o.at[n++] = q++;
+      if (k < NK)
+        for (int d = 0; d < ND; ++d) o.at[n++] = NQ + k * ND + d;
+      upto += (NQ - NQ / 2) / (NK > 2 ? NK - 2 : 1);
+      if (upto > NQ) upto = NQ;
+    }
+    return o;
+  }
+  static constexpr Order kOrder = order();
+  // Exponentials formed by the end of slot n (even; -1: before the first): evenly until the last score product, but in time
+  // for the first value product of each key group.
+  static constexpr int exps_by(int n, int all) {
+    const int until = kOrder.last_score + 1;
+    int e = (n + 2) * all / (until + 1);
+    e = (e + 1) / 2 * 2;
+    if (e > all) e = all;
+    for (int m = 0; m <= n + 1 && m < kSlots; ++m)
+      if (kOrder.at[m] >= NQ && e < ((kOrder.at[m] - NQ) / ND + 1) * (all / NK)) e = ((kOrder.at[m] - NQ) / ND + 1) * (all / NK);
+    return e;
+  }
+  // Scores of the next tile whose largest is known by the end of slot n: those after the last score product, in the slots behind it.
+  static constexpr int tops_by(int n, int all) {
+    const int from = kOrder.last_score + 2;
+    if (n >= kSlots - 1) return all;
+    if (n < from) return 0;
+    return (n - from + 1) * all / (kSlots - from) / 2 * 2;
+  }
+};
 
 template <typename T, int DP, bool UNI>
 __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ? 2 : 1)) attend_wide_kernel(AttendParams p) {
@@ -80,57 +135,61 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
   const char* kbase = lds + col * TL::kRowBytes;
   const char* vbase = lds + 2 * TL::kBytes + vr * TL::kRowBytes + (lane & 1) * 8;
 
-  // Scores of the tile in buffer `buf`, the running reference, and the exponentials in s.
-  auto scores = [&](auto masked, int key0, int buf, floatx16(&s)[NS]) {
+  auto score_step = [&](int i, int buf, floatx16(&s)[NS]) {  // 16 (fp32: 8) dimensions of the scores of the keys in `buf`
 #pragma unroll
-    for (int j = 0; j < NS; ++j) s[j] = floatx16{};
+    for (int j = 0; j < NS; ++j) {
+      const uint4 kf = *reinterpret_cast<const uint4*>(kbase + (((2 * i + half) ^ krow) << 4) + buf * TL::kBytes + j * 32 * TL::kRowBytes);
+      if constexpr (kHalf) {
+        s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), s[j], 0, 0, 0);
+      } else {
+        const floatx4 a = __builtin_bit_cast(floatx4, kf), b = __builtin_bit_cast(floatx4, qf[i]);
 #pragma unroll
-    for (int i = 0; i < QF; ++i) {
-#pragma unroll
-      for (int j = 0; j < NS; ++j) {
-        const uint4 kf = *reinterpret_cast<const uint4*>(kbase + (((2 * i + half) ^ krow) << 4) + buf * TL::kBytes + j * 32 * TL::kRowBytes);
-        if constexpr (kHalf) {
-          s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), s[j], 0, 0, 0);
-        } else {
-          const floatx4 a = __builtin_bit_cast(floatx4, kf), b = __builtin_bit_cast(floatx4, qf[i]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], s[j], 0, 0, 0);
-        }
+        for (int e = 0; e < 4; ++e) s[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], s[j], 0, 0, 0);
       }
     }
-    if constexpr (masked) {
+  };
+  auto clear = [](floatx16(&s)[NS]) {
 #pragma unroll
-      for (int j = 0; j < NS; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = key0 + 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
-          s[j][r] = key >= seen.lo && key <= seen.hi ? s[j][r] : kNegInf;
-        }
-    }
+    for (int j = 0; j < NS; ++j) s[j] = floatx16{};
+  };
+  auto largest = [](const floatx16(&s)[NS]) {
     float top = s[0][0];
 #pragma unroll
     for (int j = 0; j < NS; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[j][r]);
+    return top;
+  };
+  auto hide = [&](floatx16(&s)[NS], int key0) {
+#pragma unroll
+    for (int j = 0; j < NS; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int key = key0 + 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
+        s[j][r] = key >= seen.lo && key <= seen.hi ? s[j][r] : kNegInf;
+      }
+  };
+  float base = 0.0f;  // what exponents are taken relative to: the reference, or 0 before there is one
+  auto refer = [&](float top) {  // takes the largest score of the next tile into the reference
     top = max_across32(top) * p.scale_log2;
     if (__any(top > ref + kSlack)) {
       const float next = fmaxf(ref, top);
       const float keep = next == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
       ref = next;
+      base = ref == kNegInf ? 0.0f : ref;
       sum *= keep;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= keep;
     }
-    const float base = masked && ref == kNegInf ? 0.0f : ref;
+  };
+  auto exponent = [&](floatx16& x, int from, int n) {  // scores to exponentials
 #pragma unroll
-    for (int j = 0; j < NS; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[j][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], p.scale_log2, -base));
-        sum += s[j][r];
-      }
+    for (int r = from; r < from + n; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], p.scale_log2, -base));
+      sum += x[r];
+    }
   };
   auto exponentials = [](const floatx16& x, int r) {  // eight of them as the product's operand
     const uint4 w{pack2(x[r], x[r + 1]), pack2(x[r + 2], x[r + 3]), pack2(x[r + 4], x[r + 5]), pack2(x[r + 6], x[r + 7])};
@@ -145,39 +204,108 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
     return *reinterpret_cast<const float*>(lds + (2 + buf) * TL::kBytes + key * TL::kRowBytes + c * 16 + (e & 3) * 4);
   };
 
-  // A tile whose keys every row sees.
-  auto whole_tile = [&](int key0, int buf) {
-    floatx16 s[NS];
-    scores(std::false_type{}, key0, buf, s);
+  auto value_step = [&](int k, int buf, const floatx16(&s)[NS]) {  // the values of 16 keys
     if constexpr (kHalf) {
+      const bf16x8 pf = exponentials(s[k >> 1], 8 * (k & 1));
 #pragma unroll
-      for (int k = 0; k < KEYS / 16; ++k) {
-        const bf16x8 pf = exponentials(s[k >> 1], 8 * (k & 1));
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const u32x2 a = column4(buf, k, 0, d), b = column4(buf, k, 1, d);
-          const uint4 w{a[0], a[1], b[0], b[1]};
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
-        }
+      for (int d = 0; d < ND; ++d) {
+        const u32x2 a = column4(buf, k, 0, d), b = column4(buf, k, 1, d);
+        const uint4 w{a[0], a[1], b[0], b[1]};
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), pf, o[d], 0, 0, 0);
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < NS; ++j)
+      for (int i = 0; i < 8; ++i) {
+        const int r = 8 * (k & 1) + i, key = 32 * (k >> 1) + 8 * (r >> 2) + 4 * half + (r & 3);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 32 * j + 8 * (r >> 2) + 4 * half + (r & 3);
-#pragma unroll
-          for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value1(buf, key, d), s[j][r], o[d], 0, 0, 0);
-        }
+        for (int d = 0; d < ND; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value1(buf, key, d), s[k >> 1][r], o[d], 0, 0, 0);
+      }
     }
+  };
+
+  // A tile whose keys every row sees, and the scores of the next one, laid out by hand: each slot is one product, with the LDS
+  // reads of the one PRE slots later and a share of the vector unit's work (this tile's exponentials, then the next
+  // tile's largest score) to run beside it.
+  auto whole_tile_half = [&](int buf, floatx16(&s)[NS], floatx16(&next)[NS]) {
+    using PL = SlotPlan<QF * NS, ND, KEYS / 16>;
+    constexpr int PRE = 3, kExps = 16 * NS;
+    uint4 frag[PL::kSlots];
+    uint32_t packed[kExps / 2];
+    auto read = [&](auto slot) {
+      constexpr int n = slot;
+      if constexpr (n < PL::kSlots) {
+        constexpr int x = PL::kOrder.at[n];
+        if constexpr (x < QF * NS) {
+          constexpr int i = x / NS, j = x % NS;
+          frag[n] = *reinterpret_cast<const uint4*>(kbase + (((2 * i + half) ^ krow) << 4) + (buf ^ 1) * TL::kBytes + j * 32 * TL::kRowBytes);
+        } else {
+          constexpr int k = (x - QF * NS) / ND, d = (x - QF * NS) % ND;
+          const u32x2 a = column4(buf, k, 0, d), b = column4(buf, k, 1, d);
+          frag[n] = uint4{a[0], a[1], b[0], b[1]};
+        }
+      }
+    };
+    auto form = [&](auto from, auto to) {  // exponentials [from, to) of the lane, in pairs
+      constexpr int f = from, t = to;
+#pragma unroll
+      for (int e = f; e < t; e += 2) {
+        floatx16& x = s[e / 16];
+        const float u0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e % 16], p.scale_log2, -base));
+        const float u1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e % 16 + 1], p.scale_log2, -base));
+        sum += u0;
+        sum += u1;
+        packed[e / 2] = pack2(u0, u1);
+      }
+    };
+    float top = kNegInf;
+    clear(next);
+    unrolled<PRE>([&](auto n) { read(n); });
+    form(std::integral_constant<int, 0>{}, std::integral_constant<int, PL::exps_by(-1, kExps)>{});
+    __builtin_amdgcn_sched_barrier(0);
+    unrolled<PL::kSlots>([&](auto slot) {
+      constexpr int n = slot, x = PL::kOrder.at[n];
+      read(std::integral_constant<int, n + PRE>{});
+      if constexpr (x < QF * NS) {
+        constexpr int i = x / NS, j = x % NS;
+        next[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, frag[n]), __builtin_bit_cast(bf16x8, qf[i]), next[j], 0, 0, 0);
+      } else {
+        constexpr int k = (x - QF * NS) / ND, d = (x - QF * NS) % ND;
+        const uint4 w{packed[4 * k], packed[4 * k + 1], packed[4 * k + 2], packed[4 * k + 3]};
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, frag[n]), __builtin_bit_cast(bf16x8, w), o[d], 0, 0, 0);
+      }
+      form(std::integral_constant<int, PL::exps_by(n - 1, kExps)>{}, std::integral_constant<int, PL::exps_by(n, kExps)>{});
+      constexpr int f = PL::tops_by(n - 1, kExps), t = PL::tops_by(n, kExps);
+#pragma unroll
+      for (int e = f; e < t; e += 2) top = fmaxf(fmaxf(next[e / 16][e % 16], next[e / 16][e % 16 + 1]), top);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    return top;
+  };
+
+  auto whole_tile_single = [&](int buf, floatx16(&s)[NS], floatx16(&next)[NS]) {
+    clear(next);
+#pragma unroll
+    for (int k = 0; k < KEYS / 16; ++k) {
+      exponent(s[k >> 1], 8 * (k & 1), 8);
+#pragma unroll
+      for (int i = 0; i < QF; ++i)
+        if (i * (KEYS / 16) / QF == k) score_step(i, buf ^ 1, next);
+      if (k > 0) value_step(k - 1, buf, s);
+    }
+    value_step(KEYS / 16 - 1, buf, s);
+    return largest(next);
+  };
+  auto whole_tile = [&](int buf, floatx16(&s)[NS], floatx16(&next)[NS]) {
+    if constexpr (kHalf) return whole_tile_half(buf, s, next);
+    else return whole_tile_single(buf, s, next);
   };
 
   // A tile of which some row does not see some key. A masked key's exponential is zero, but zero times an infinity or a
   // NaN is not: values of keys that no row of the wave sees are cleared, and those that are not finite leave the product
   // and are added to the rows that see their key.
-  auto edge_tile = [&](int key0, int buf) {
-    floatx16 s[NS];
-    scores(std::true_type{}, key0, buf, s);
+  auto edge_tile = [&](int key0, int buf, floatx16(&s)[NS]) {
+#pragma unroll
+    for (int j = 0; j < NS; ++j) exponent(s[j], 0, 16);
     int odd = 0;
     if constexpr (kHalf) {
 #pragma unroll
@@ -231,36 +359,65 @@ __global__ void __launch_bounds__(64 * kWideWaves, (DP * (int)sizeof(T) <= 256 ?
     }
   };
 
-  Stager<T, TL, NW, UNI> stager(p, u, wave, lane, chunks);
-  if (u.lo < u.hi) {
-    stager.find(u.lo);
-    stager.copy(lds, lds + 2 * TL::kBytes);
-    stager.find(u.lo + KEYS);
-  }
-  auto arrive = [&](int key0, int buf) {  // the tile in `buf` has landed; the next one's copies leave
+  // Copies: the keys of tile i are in buffer i & 1 while tile i - 1 is worked on, its values while it is worked on itself.
+  char* const keys = lds;
+  char* const values = lds + 2 * TL::kBytes;
+  Stager<T, TL, NW, UNI, KEYS> stager(p, u, wave, lane, chunks);
+  floatx16 s0[NS], s1[NS];
+  auto whole = [&](int key0) { return key0 >= all_lo && key0 + KEYS - 1 <= all_hi && key0 + KEYS <= u.hi; };
+  auto arrive = [&](int key0, int buf) {  // the values of this tile and the keys of the next have landed; the copies after them leave
     wait_loads<0>();
     __syncthreads();
     if (key0 + KEYS < u.hi) {
-      stager.copy(lds + (buf ^ 1) * TL::kBytes, lds + (2 + (buf ^ 1)) * TL::kBytes);
-      stager.find(key0 + 2 * KEYS);
+      stager.copy(keys + buf * TL::kBytes, values + (buf ^ 1) * TL::kBytes);
+      stager.find(key0 + 3 * KEYS);
     }
   };
-  auto whole = [&](int key0) { return key0 >= all_lo && key0 + KEYS - 1 <= all_hi && key0 + KEYS <= u.hi; };
+  if (u.lo < u.hi) {
+    stager.find(u.lo);
+    stager.template copy<1>(keys, values);
+    stager.find(u.lo + KEYS);
+    stager.copy(keys + TL::kBytes, values);
+    stager.find(u.lo + 2 * KEYS);
+    wait_loads<2 * TL::kLoads>();  // the copies of the second tile's keys may be outstanding
+    __syncthreads();
+    clear(s0);
+#pragma unroll
+    for (int i = 0; i < QF; ++i) score_step(i, 0, s0);
+    if (!whole(u.lo)) hide(s0, u.lo);
+    refer(largest(s0));
+  }
   int key0 = u.lo, buf = 0;
   while (key0 < u.hi) {
-    // the tiles that all rows see, two a round so that a buffer's address is a constant
-    while (buf == 0 && whole(key0) && whole(key0 + KEYS)) {
+    // two a round, so that a buffer's address is a constant
+    while (buf == 0 && whole(key0) && whole(key0 + KEYS) && key0 + 2 * KEYS < u.hi) {
       arrive(key0, 0);
-      whole_tile(key0, 0);
+      refer(whole_tile(0, s0, s1));
       arrive(key0 + KEYS, 1);
-      whole_tile(key0 + KEYS, 1);
+      float top = whole_tile(1, s1, s0);
       key0 += 2 * KEYS;
+      if (!whole(key0)) {
+        hide(s0, key0);
+        top = largest(s0);
+      }
+      refer(top);
     }
-    if (key0 >= u.hi) break;
     arrive(key0, buf);
-    if (key0 <= any_hi && key0 + KEYS > any_lo) edge_tile(key0, buf);
+    const bool more = key0 + KEYS < u.hi;
+    clear(s1);
+    if (more) {
+#pragma unroll
+      for (int i = 0; i < QF; ++i) score_step(i, buf ^ 1, s1);
+    }
+    if (key0 <= any_hi && key0 + KEYS > any_lo) edge_tile(key0, buf, s0);
     key0 += KEYS;
     buf ^= 1;
+    if (more) {
+      if (!whole(key0)) hide(s1, key0);
+      refer(largest(s1));
+#pragma unroll
+      for (int j = 0; j < NS; ++j) s0[j] = s1[j];
+    }
   }
 
   sum = sum_across32(sum);
