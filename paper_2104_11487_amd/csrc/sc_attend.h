@@ -67,7 +67,8 @@ struct AttendParams {
 };
 
 constexpr int kMostKeys = 1 << 30;  // positions of a sequence stay below it
-constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel
+constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel; bf16 heads of up to kWideDoubleDim also take twice as many
+constexpr int kWideDoubleDim = 64;
 constexpr int kLogFewRows = 4;      // rows of a block of the few-rows kernel, which takes one or two
 
 // Rows of a key tile. The wide kernel's: two buffers of keys and values take 64 KB where the head allows 32 rows or more.

@@ -115,7 +115,8 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   const int64_t rows = c->tokens * group;  // of one key head
   const int64_t most = a->max_new > 0 ? std::min<int64_t>(a->max_new, c->tokens) : c->tokens;
   p->few = most * group <= 32;
-  p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1) : sc::kLogWideRows;
+  p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1)
+                       : sc::kLogWideRows + (elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128);
   p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim);
   // sum over the sequences of ceil(rows / 2^log_rows), at most
   const int64_t tiles = (rows >> p->log_rows) + std::min<int64_t>(c->batch, c->tokens);

@@ -141,9 +141,10 @@ struct Stager {
 
 // Four bf16 of one column, from four consecutive rows: lane l of each 16 lanes gives the address of row l / 4,
 // columns 4 (l % 4).., and receives column l.
-__device__ __forceinline__ u32x2 read_column4(const char* at) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(SC_LDS(const_cast<char*>(at), shortx4)));
+__device__ __forceinline__ u32x2 read_column4(uint32_t lds_at) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)(lds_at)));
 }
+__device__ __forceinline__ u32x2 read_column4(const char* at) { return read_column4((uint32_t)(uintptr_t)SC_LDS(at, const char)); }
 
 // Of two packed bf16 values: those outside the mask become zero, and those that are infinite or NaN too, which sets *odd.
 __device__ __forceinline__ uint32_t finite2(uint32_t v, uint32_t mask, int* odd) {
