@@ -135,7 +135,7 @@ struct Unit {
   int splits;            // chunks of the tile
 };
 
-// Finds the sequence of units that holds index `at` (`by` 0), or the sequence `at` itself (`by` 1): its number, extents, cut and
+// Finds the sequence whose units hold index `at` (`by` 0), or whose rows hold row `at` (`by` 1): its number, extents, cut and
 // the index of its first unit. False where there is none. Called by whole waves.
 __device__ __forceinline__ bool find_units(const AttendParams& p, int at, int by, int* b, Sequence* seq, Shape* cut, int* first) {
   const int lane = threadIdx.x & 63;
@@ -155,7 +155,7 @@ __device__ __forceinline__ bool find_units(const AttendParams& p, int at, int by
       const int64_t t = __shfl_up(upto, d);
       if (lane >= d) upto += t;
     }
-    const uint64_t past = __ballot(by ? b0 + lane == at : base + upto > at);
+    const uint64_t past = __ballot(by ? at >= s.start && at < s.start + s.n : base + upto > at);
     if (past) {
       const int src = (int)__ffsll((unsigned long long)past) - 1;
       *b = b0 + src;
@@ -206,6 +206,10 @@ __device__ __forceinline__ Seen seen_by(const AttendParams& p, const Unit& u, in
   s.lo = p.window < 0 ? 0 : max(0, p0 + (p.causal ? t : 0) - p.window);
   return s;
 }
+
+// What a share with reference `ref` counts in a join whose largest reference is `top`. Shares without a key (reference -inf) hold
+// zeros, or NaN where all their scores are: they count by 0, or by 1 where no share has a key, so that a NaN stays one.
+__device__ __forceinline__ float join_weight(float ref, float top) { return ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top); }
 
 // Where key position `at` lies: the slot, which `rows` slots of its page begin at, and the page table's entry. Positions past the
 // table and entries outside the cache are led to slots that exist (no row sees their keys). The entry is loaded by a

@@ -30,7 +30,8 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
   using TL = Tile<T, DP, KEYS, 1, false>;
   constexpr int QF = TL::kElems * 4 > DP ? 1 : DP / (4 * TL::kElems);  // 16-byte pieces of a row that a lane holds
   constexpr int JP = DP + 4;                                           // joining: a row's stride in LDS, in floats
-  constexpr int kBuffers = NW * 4 * TL::kBytes, kJoin = NW * ROWS * (JP + 2) * 4;
+  constexpr int kWaveBytes = 4 * TL::kBytes + 512;                     // two buffers of keys and values, of page numbers
+  constexpr int kBuffers = NW * kWaveBytes, kJoin = NW * ROWS * (JP + 2) * 4;
   __shared__ alignas(16) char lds[kBuffers > kJoin ? kBuffers : kJoin];
 
   Unit u;
@@ -38,7 +39,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4;
   const int rows = u.n * p.group, chunks = p.dim / TL::kElems;
-  char* mine = lds + wave * 4 * TL::kBytes;
+  char* mine = lds + wave * kWaveBytes;
 
   if (chunks < TL::kChunks) {  // chunks that no copy fills: those past the head's dimension
     for (int i = lane; i < 4 * TL::kBytes / 16; i += 64) reinterpret_cast<uint4*>(mine)[i] = uint4{0u, 0u, 0u, 0u};
@@ -49,16 +50,17 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
   const int begin = u.lo + wave * KEYS;
   const int count = begin < u.hi ? (u.hi - begin + kStep - 1) / kStep : 0;  // tiles of this wave
 
-  // Page numbers are looked up three tiles ahead and copies run two tiles ahead, so that no wait for
-  // a page number waits for the copies behind it.
-  Stager<T, TL, 1, false> ahead(p, u, 0, lane, chunks), next(p, u, 0, lane, chunks);
+  // Page numbers are looked up three tiles ahead, copies run two tiles ahead.
+  const LoneStager<T, TL, KEYS> stager(p, u, lane, chunks);
+  char* const entries = mine + 4 * TL::kBytes;
   if (count > 0) {
-    Stager<T, TL, 1, false> zero(p, u, 0, lane, chunks);
-    zero.find(begin);
-    ahead.find(begin + kStep);
-    next.find(begin + 2 * kStep);
-    zero.copy(mine, mine + TL::kBytes);
-    if (count > 1) ahead.copy(mine + 2 * TL::kBytes, mine + 3 * TL::kBytes);
+    stager.find(begin, entries);
+    if (count > 1) stager.find(begin + kStep, entries + 256);
+    wait_loads<0>();
+    stager.copy(begin, entries, mine, mine + TL::kBytes);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (count > 2) stager.find(begin + 2 * kStep, entries);
+    if (count > 1) stager.copy(begin + kStep, entries + 256, mine + 2 * TL::kBytes, mine + 3 * TL::kBytes);
   }
 
   // the rows' queries, in the operand's layout
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     const int key0 = begin + it * kStep;
     char* kt = mine + (it & 1) * 2 * TL::kBytes;
     char* vt = kt + TL::kBytes;
-    if (it + 1 < count) wait_loads<2 * TL::kLoads>();  // the younger tile's copies stay in flight
+    if (it + 1 < count) wait_loads<LoneStager<T, TL, KEYS>::kOps>();  // the younger tile's copies stay in flight
     else wait_loads<0>();
     const bool edge = key0 < all_lo || key0 + KEYS - 1 > all_hi;
 
@@ -232,9 +234,8 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     // this tile's buffers are free: the fragments read from them have reached their products
     if (it + 2 < count) {
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      ahead.take(next);
-      next.find(key0 + 3 * kStep);
-      ahead.copy(kt, vt);
+      if (it + 3 < count) stager.find(key0 + 3 * kStep, entries + ((it + 1) & 1) * 256);
+      stager.copy(key0 + 2 * kStep, entries + (it & 1) * 256, kt, vt);
     }
   }
 
@@ -262,14 +263,11 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     float total = 0.0f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float m = stats[(w * ROWS + r) * 2];
-      const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+      const float f = join_weight(stats[(w * ROWS + r) * 2], top);
       const floatx4 x = *reinterpret_cast<const floatx4*>(joined + (w * ROWS + r) * JP + e);
-      if (m != kNegInf) {
-        total += stats[(w * ROWS + r) * 2 + 1] * f;
+      total += stats[(w * ROWS + r) * 2 + 1] * f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += x[k] * f;
-      }
+      for (int k = 0; k < 4; ++k) v[k] += x[k] * f;
     }
     if (u.splits > 1) {
       const int64_t at = (int64_t)blockIdx.x * ROWS + r;

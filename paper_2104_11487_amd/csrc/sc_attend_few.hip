@@ -9,59 +9,71 @@ namespace {
 
 constexpr int kJoinWaves = 4;
 
-// One workgroup a row (token, query head): its chunks' references, sums and outputs, joined in chunk order. The chunks are
-// dealt to lane groups of dim / 4 lanes (a power of two), whose shares are then added in order.
+// One workgroup a row (token, query head): its chunks' references, sums and outputs, joined in chunk order. The chunks' weights go to
+// LDS, 256 at a time; the chunks are dealt to groups of dim / 4 lanes (a power of two), whose shares are then added in order.
 template <typename T>
 __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendParams p) {
-  constexpr int kMost = 64 * kJoinWaves / 8;  // lane groups at the least head dimension
-  __shared__ floatx4 shares[64 * kJoinWaves];
-  __shared__ float sums[kMost];
+  constexpr int kThreads = 64 * kJoinWaves;
+  __shared__ floatx4 shares[kThreads];
+  __shared__ float weights[kThreads], tops[kJoinWaves], sums[kJoinWaves];
   const int token = (int)blockIdx.x / p.q_heads, h = (int)blockIdx.x - token * p.q_heads;
-  const int b = owner_of(p.c.row_start, p.c.batch, token);
-  if (b >= p.c.batch) return;
-  int at, first;
+  int b, first;
   Sequence s;
   Shape o;
-  if (!find_units(p, b, 1, &at, &s, &o, &first) || o.splits <= 1) return;
-  const int row = (token - s.start) * p.group + h % p.group;
-  if (token < s.start || row >= s.n * p.group) return;
-  const int tile = row >> p.log_rows;
-  const int64_t unit = (int64_t)first + (int64_t)(h / p.group) * o.tiles * o.splits + (int64_t)(o.tiles - 1 - tile) * o.splits;
+  if (!find_units(p, token, 1, &b, &s, &o, &first) || o.splits <= 1) return;
+  const int head = h / p.group, row = (token - s.start) * p.group + (h - head * p.group);
+  const int tile = row >> p.log_rows, rows = 1 << p.log_rows;
+  const int64_t unit = (int64_t)first + (int64_t)head * o.tiles * o.splits + (int64_t)(o.tiles - 1 - tile) * o.splits;
   if (unit + o.splits > p.units) return;
-  const int rows = 1 << p.log_rows;
   const int64_t part0 = unit * rows + (row - (tile << p.log_rows));
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   int width = 8;
   while (width * 4 < p.dim) width *= 2;  // lanes of a group: 8..64
-  const int group = (int)threadIdx.x / width, groups = 64 * kJoinWaves / width, e = ((int)threadIdx.x & (width - 1)) * 4;
+  const int group = tid / width, groups = kThreads / width, e = (tid & (width - 1)) * 4;
 
   float top = kNegInf;
-  for (int i = threadIdx.x & 63; i < o.splits; i += 64) top = fmaxf(top, p.part_ml[(part0 + (int64_t)i * rows) * 2]);
+  for (int i = tid; i < o.splits; i += kThreads) top = fmaxf(top, p.part_ml[(part0 + (int64_t)i * rows) * 2]);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) tops[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
 
   floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
   float total = 0.0f;
-  for (int i = group; i < o.splits; i += groups) {
-    const int64_t part = part0 + (int64_t)i * rows;
-    const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + part * 2);
-    if (ml.x != kNegInf) {
-      const float f = __builtin_amdgcn_exp2f(ml.x - top);
-      total += ml.y * f;
-      if (e < p.dim) {
-        const floatx4 x = *reinterpret_cast<const floatx4*>(p.part_o + part * p.dim + e);
+  for (int i0 = 0; i0 < o.splits; i0 += kThreads) {
+    const int n = min(o.splits - i0, kThreads);
+    if (i0 > 0) __syncthreads();
+    if (tid < n) {
+      const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + (part0 + (int64_t)(i0 + tid) * rows) * 2);
+      weights[tid] = join_weight(ml.x, top);
+      total += ml.y * weights[tid];
+    }
+    __syncthreads();
+    if (e < p.dim) {
+      const float* x = p.part_o + (part0 + (int64_t)i0 * rows) * p.dim + e;
+#pragma unroll 4
+      for (int i = group; i < n; i += groups) {
+        const floatx4 y = *reinterpret_cast<const floatx4*>(x + (int64_t)i * rows * p.dim);
+        const float f = weights[i];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += x[k] * f;
+        for (int k = 0; k < 4; ++k) v[k] += y[k] * f;
       }
     }
   }
-  shares[threadIdx.x] = v;
-  if (e == 0) sums[group] = total;
+  shares[tid] = v;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  if (lane == 0) sums[wave] = total;
   __syncthreads();
   if (group > 0 || e >= p.dim) return;
+  total = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kJoinWaves; ++w) total += sums[w];
   for (int g = 1; g < min(groups, o.splits); ++g) {
-    const floatx4 x = shares[g * width + (int)threadIdx.x];
-    total += sums[g];
+    const floatx4 x = shares[g * width + tid];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] += x[k];
   }

@@ -60,6 +60,11 @@ __device__ __forceinline__ void copy16(const char* from, char* to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(from) : "memory");
 }
 
+// The same, 4 bytes a lane from each lane's own address.
+__device__ __forceinline__ void copy4(const void* from, char* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(from) : "memory");
+}
+
 // A wave's share of the copies of one tile of keys and one of values (of the keys `lag` before), in two steps, so that page
 // numbers are looked up a tile before the copies that need them.
 //
@@ -100,11 +105,6 @@ struct Stager {
     }
   }
 
-  __device__ __forceinline__ void take(const Stager& other) {
-#pragma unroll
-    for (int t = 0; t < kFound; ++t) entry[t] = other.entry[t], slot[t] = other.slot[t];
-  }
-
   __device__ __forceinline__ int chunk_of(int t) const {  // that this lane's 16 bytes of load t come from
     return (lane % TL::kChunks) ^ (TL::swizzle((t * NW + wave) * TL::kGroup + lane / TL::kChunks) & (TL::kChunks - 1));
   }
@@ -136,6 +136,43 @@ struct Stager {
   __device__ __forceinline__ void copy(char* keys, char* values) const {
     if (chunks == TL::kChunks) copy_rows<true, PARTS>(keys, values);
     else copy_rows<false, PARTS>(keys, values);
+  }
+};
+
+// The copies of one wave that has tiles of its own. Page numbers too arrive by copies into LDS, `entries` (64 of them a tile), so that
+// no wait of the compiler's for a loaded register lets the copies in flight run dry.
+template <typename T, typename TL, int KEYS>
+struct LoneStager {
+  const CacheView& c;
+  const int b, lane, chunks;
+  const char* kb;
+  const char* vb;
+  static constexpr int kOps = 2 * TL::kLoads;  // loads of copy()
+
+  __device__ __forceinline__ LoneStager(const AttendParams& p, const Unit& u, int l, int n)
+      : c(p.c), b(u.b), lane(l), chunks(n), kb(c.k + (int64_t)u.head * c.k_head * (int64_t)sizeof(T)),
+        vb(c.v + (int64_t)u.head * c.v_head * (int64_t)sizeof(T)) {}
+
+  __device__ __forceinline__ void find(int key0, char* entries) const {
+    copy4(c.table + (int64_t)b * c.width + min(page_of(c, key0 + (lane & (KEYS - 1))), c.width - 1), entries);
+  }
+  __device__ __forceinline__ void copy(int key0, const char* entries, char* keys, char* values) const {
+    const char* from[2 * TL::kLoads];
+#pragma unroll
+    for (int t = 0; t < TL::kLoads; ++t) {
+      const int row = t * TL::kGroup + lane / TL::kChunks, at = key0 + row;
+      const int page = page_of_entry(c, *reinterpret_cast<const int*>(entries + row * 4));
+      const int slot = min(at - min(page_of(c, at), c.width - 1) * c.page_size, c.page_size - 1);
+      const int chunk = (lane % TL::kChunks) ^ (TL::swizzle(row) & (TL::kChunks - 1));
+      from[t] = kb + ((int64_t)page * c.k_page + (int64_t)slot * c.k_slot) * (int64_t)sizeof(T) + chunk * 16;
+      from[TL::kLoads + t] = vb + ((int64_t)page * c.v_page + (int64_t)slot * c.v_slot) * (int64_t)sizeof(T) + chunk * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * TL::kLoads; ++i) {
+      const int t = i % TL::kLoads;
+      const int chunk = (lane % TL::kChunks) ^ (TL::swizzle(t * TL::kGroup + lane / TL::kChunks) & (TL::kChunks - 1));
+      if (chunk < chunks) copy16(from[i], (i < TL::kLoads ? keys : values) + t * 1024);
+    }
   }
 };
 

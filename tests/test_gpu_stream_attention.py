@@ -348,6 +348,26 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, lens, heads, value):
             assert not np.isfinite(got[seen][..., 3:9]).any() and np.isfinite(got[seen][..., 9:]).all()
 
 
+@pytest.mark.parametrize("dtype,new,kv", [("bf16", 1, 40), ("bf16", 1, 6000), ("bf16", 9, 6000), ("bf16", 50, 300), ("bf16", 200, 900),
+                                          ("f32", 1, 6000), ("f32", 40, 3000)])
+def test_scores_that_are_nan_stay_nan(dtype, new, kv):
+    """A query that is NaN, or a key that a row sees, makes the whole row NaN (its sum of exponentials is), and no other row."""
+    rng = _rng(48)
+
+    def spoil(kp, vp, table):
+        kp[table[1, 0], 1, 2, 7] = np.nan  # token 2 of the second sequence, key head 1
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, kv), (new, kv)], 4, 2, 64, 16, dtype, spoil=spoil)
+    q[new - 1, 3] = float("nan")  # the first sequence's last row, one head
+    q64[new - 1, 3] = np.nan
+    with np.errstate(all="ignore"):
+        o, l, b = O.attend(q64, k64, v64, table, starts, length)  # noqa: E741
+    bad = np.isnan(l)
+    assert bad[new - 1, 3] and bad[new:, 2:].all() and bad.sum() == 1 + 2 * new
+    for _, out, lse in _attend_both(cache, q, table, starts, length):
+        got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.repeat(bad[..., None], 64, 2)) and np.array_equal(np.isnan(gl), bad)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("new", [1, 40])
 def test_scores_of_great_range(dtype, new):
