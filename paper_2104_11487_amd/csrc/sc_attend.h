@@ -61,9 +61,11 @@ struct AttendParams {
   float scale_log2;  // scale * log2(e)
   int log_rows;      // a unit's rows (new tokens x query heads of one key head): 2^log_rows
   int keys;          // rows of a key tile: chunks are whole tiles
-  int target;        // units wanted per key head; 0: a tile's keys are never split
-  int min_chunk;     // fewest keys of a unit where they are split
-  int units;         // workgroups of the launch, and parts in the workspace
+  // wide kernel: units wanted per key head (0: an item's keys are never split) and fewest keys of a unit where they are;
+  // few-rows kernel: workgroups, and fewest key tiles of one
+  int target, min_chunk;
+  int units;         // workgroups of the launch
+  int slots;         // parts in the workspace, of 2^log_rows rows
 };
 
 constexpr int kMostKeys = 1 << 30;  // positions of a sequence stay below it

@@ -22,9 +22,9 @@ int hip_result(hipError_t e, const char* what) {
 }
 
 constexpr int64_t kMostRows = 0x7fffffff;
-// Workgroups that keep the GPU busy: 256 compute units, of which each holds two of the wide kernel's or one of the few-rows kernel's.
+// Workgroups that keep the GPU's 256 compute units busy: each holds two of the wide kernel's, one of the few-rows kernel's.
 constexpr int kWantWide = 512;
-constexpr int kWantFew = 512;
+constexpr int kWantFew = 256;
 
 bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool whole16(int64_t stride, int elem) { return (stride * elem) % 16 == 0; }
@@ -106,7 +106,7 @@ int check_attend(const skipconv_cache* c, const skipconv_attend* a) {
 // The kernel and the cut of a launch, from the shapes alone (the lengths are on the device).
 struct Plan {
   bool few;
-  int log_rows, keys, target, min_chunk, units;
+  int log_rows, keys, target, min_chunk, units, slots;
   size_t part_o, part_ml;
 };
 
@@ -120,13 +120,26 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim);
   // sum over the sequences of ceil(rows / 2^log_rows), at most
   const int64_t tiles = (rows >> p->log_rows) + std::min<int64_t>(c->batch, c->tokens);
-  const int want = p->few ? kWantFew : kWantWide;
-  p->target = p->few || tiles * c->kv_heads < want ? (want + c->kv_heads - 1) / c->kv_heads : 0;
-  p->min_chunk = p->few ? 2 * p->keys * sc::few_waves_of(elem, c->head_dim) : 4 * p->keys;
-  const int64_t units = (tiles + p->target) * c->kv_heads;
+  int64_t units;
+  if (p->few) {
+    // Equal shares of all keys, but a workgroup an item where no item can have keys for more than four tiles a wave: then the join's
+    // launch costs more than it saves.
+    const int waves = sc::few_waves_of(elem, c->head_dim);
+    const int64_t room = (int64_t)c->table_width * c->page_size, reach = a->window < 0 ? room : (int64_t)a->window + most;
+    const bool shared = std::min(room, reach) > 4ll * p->keys * waves;
+    p->target = shared ? kWantFew : 0;
+    p->min_chunk = 2 * waves;
+    units = shared ? kWantFew : tiles * c->kv_heads;
+    p->slots = shared ? 2 * kWantFew : 0;
+  } else {
+    p->target = tiles * c->kv_heads < kWantWide ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
+    p->min_chunk = 4 * p->keys;
+    units = (tiles + p->target) * c->kv_heads;
+    p->slots = p->target ? (int)std::min<int64_t>(units, kMostRows) : 0;
+  }
   if (units > kMostRows) return fail(SKIPCONV_E_UNSUPPORTED, "attend: too many rows");
   p->units = (int)units;
-  const size_t parts = p->target ? (size_t)units << p->log_rows : 0;
+  const size_t parts = (size_t)p->slots << p->log_rows;
   p->part_o = parts * c->head_dim * 4;
   p->part_ml = parts * 2 * 4;
   return SKIPCONV_OK;
@@ -239,6 +252,7 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
   p.window = a->window < 0 ? -1 : a->window;
   p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
   p.log_rows = plan.log_rows, p.keys = plan.keys, p.target = plan.target, p.min_chunk = plan.min_chunk, p.units = plan.units;
+  p.slots = plan.slots;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;
   if (plan.few) {
@@ -253,7 +267,7 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
     const int uniform = c->page_size % rows == 0 && reach < (1ll << 31) && page_bytes < (1ll << 32);
     e = elem == 2 ? sc::launch_attend_wide_bf16(p, uniform, s) : sc::launch_attend_wide_f32(p, uniform, s);
   }
-  if (e == hipSuccess && plan.target) e = sc::launch_attend_join(p, elem, s);
+  if (e == hipSuccess && plan.slots) e = sc::launch_attend_join(p, elem, s);
   return hip_result(e, "attend launch");
 }
 

@@ -80,14 +80,14 @@ __device__ __forceinline__ Sequence sequence_of(const CacheView& c, int b) {
 
 // ---- units of work ----
 //
-// Rows of one key head: a sequence's n new tokens x `group` query heads, the token slowest. They
-// are cut into tiles of 2^log_rows; the keys that a tile may see are cut into `splits` chunks where
-// a launch's tiles alone would leave compute units idle. Every workgroup derives the same cut from
-// the lengths on the device (no host copy of them exists), by a scan over the sequences.
-// Unit index: sequences in order; within one: key head, tile (the last one, which sees most keys
-// under a causal mask, first), chunk.
+// Rows of one key head: a sequence's n new tokens x `group` query heads, the token slowest. They are cut into tiles of 2^log_rows;
+// an item is one tile with one key head and all the keys that its rows may see. Every workgroup derives the same cut of the items'
+// keys from the lengths on the device (no host copy of them exists), by a scan over the sequences.
+//   wide kernel: an item is `parts` units, more than one where a launch's items alone would leave compute units idle;
+//   few-rows kernel: an item is as many units as it has key tiles, and each workgroup takes an equal share of all units in a row.
+// Unit index: sequences in order; within one: key head, tile (the last one, which sees most keys under a causal mask, first), keys.
 struct Shape {
-  int tiles, splits, chunk, span;
+  int tiles, parts, chunk, span;  // row tiles; units of an item; keys of a unit; keys that an item may have
 };
 
 __device__ __forceinline__ Shape shape_of(const AttendParams& p, const Sequence& s) {
@@ -96,66 +96,73 @@ __device__ __forceinline__ Shape shape_of(const AttendParams& p, const Sequence&
   o.tiles = (s.n * p.group + rows - 1) >> p.log_rows;
   const int reach = p.causal ? min(s.n, (rows - 1) / p.group + 2) : s.n;  // tokens that a tile spans
   o.span = p.window < 0 ? s.len : (int)min((int64_t)s.len, (int64_t)p.window + reach);
-  o.splits = o.tiles > 0 ? 1 : 0;
+  o.parts = o.tiles > 0 ? 1 : 0;
   o.chunk = kMostKeys;
   return o;
 }
 
-// Keys that a chunk should have; 0: nothing is split.
-__device__ __forceinline__ int chunk_goal(const AttendParams& p) {
-  if (p.target <= 0) return 0;
+// The sum of `f` over the batch's sequences; called by whole waves.
+template <typename F>
+__device__ __forceinline__ int64_t sum_over_batch(const AttendParams& p, F f) {
   const int lane = threadIdx.x & 63;
   int64_t total = 0;
-  for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
-    if (b0 + lane < p.c.batch) {
-      const Shape o = shape_of(p, sequence_of(p.c, b0 + lane));
-      total += (int64_t)o.tiles * o.span;
-    }
-  }
+  for (int b0 = 0; b0 < p.c.batch; b0 += 64)
+    if (b0 + lane < p.c.batch) total += f(sequence_of(p.c, b0 + lane));
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  return total;
+}
+
+// Keys that a unit of the wide kernel should have; 0: nothing is split.
+__device__ __forceinline__ int chunk_goal(const AttendParams& p) {
+  if (p.target <= 0) return 0;
+  const int64_t total = sum_over_batch(p, [&p](const Sequence& s) {
+    const Shape o = shape_of(p, s);
+    return (int64_t)o.tiles * o.span;
+  });
   return max(p.min_chunk, (int)min(ceil((double)total / (double)p.target), (double)kMostKeys));
 }
 
+// The cut of a sequence: by the wide kernel's goal, or (SHARES) into key tiles, where those are shared. A span begins anywhere, the
+// first tile at a whole one.
+template <bool SHARES>
 __device__ __forceinline__ Shape cut_of(const AttendParams& p, const Sequence& s, int goal) {
   Shape o = shape_of(p, s);
-  if (goal > 0 && o.tiles > 0 && o.span > goal) {
-    o.splits = (int)((uint32_t)(o.span + goal - 1) / (uint32_t)goal);
-    const uint32_t each = (uint32_t)(o.span + p.keys - 1 + o.splits - 1) / (uint32_t)o.splits;  // the first key is rounded down to a tile
-    o.chunk = (int)((each + p.keys - 1) & ~(uint32_t)(p.keys - 1));
+  const uint32_t most = (uint32_t)o.span + (uint32_t)p.keys - 1;
+  if constexpr (SHARES) {
+    if (p.target > 0 && o.tiles > 0) {
+      o.parts = max(1, (int)((most + p.keys - 1) / (uint32_t)p.keys));
+      o.chunk = p.keys;
+    }
+  } else if (goal > 0 && o.tiles > 0 && o.span > goal) {
+    o.parts = (int)((uint32_t)(o.span + goal - 1) / (uint32_t)goal);
+    o.chunk = (int)(((most + o.parts - 1) / (uint32_t)o.parts + p.keys - 1) & ~(uint32_t)(p.keys - 1));
   }
   return o;
 }
 
-struct Unit {
-  int b, start, n, len;  // sequence
-  int head;              // key head
-  int row0;              // first row of the tile
-  int lo, hi;            // keys [lo, hi) of this chunk, lo a multiple of the key tile
-  int splits;            // chunks of the tile
-};
-
-// Finds the sequence whose units hold index `at` (`by` 0), or whose rows hold row `at` (`by` 1): its number, extents, cut and
-// the index of its first unit. False where there is none. Called by whole waves.
-__device__ __forceinline__ bool find_units(const AttendParams& p, int at, int by, int* b, Sequence* seq, Shape* cut, int* first) {
+// Finds the sequence whose units hold index `at` (by_row false), or whose rows hold row `at`: its number, extents, cut and the index
+// of its first unit. False where there is none. Called by whole waves.
+template <bool SHARES>
+__device__ __forceinline__ bool find_units(const AttendParams& p, int64_t at, bool by_row, int* b, Sequence* seq, Shape* cut, int64_t* first) {
   const int lane = threadIdx.x & 63;
-  const int goal = chunk_goal(p);
+  const int goal = SHARES ? 0 : chunk_goal(p);
   int64_t base = 0;
   for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
     Sequence s = {0, 0, 0};
     Shape o = {0, 0, 0, 0};
     if (b0 + lane < p.c.batch) {
       s = sequence_of(p.c, b0 + lane);
-      o = cut_of(p, s, goal);
+      o = cut_of<SHARES>(p, s, goal);
     }
-    const int64_t mine = (int64_t)o.tiles * o.splits * p.kv_heads;
+    const int64_t mine = (int64_t)o.tiles * o.parts * p.kv_heads;
     int64_t upto = mine;  // inclusive scan
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int64_t t = __shfl_up(upto, d);
       if (lane >= d) upto += t;
     }
-    const uint64_t past = __ballot(by ? at >= s.start && at < s.start + s.n : base + upto > at);
+    const uint64_t past = __ballot(by_row ? at >= s.start && at < s.start + s.n : base + upto > at);
     if (past) {
       const int src = (int)__ffsll((unsigned long long)past) - 1;
       *b = b0 + src;
@@ -163,9 +170,10 @@ __device__ __forceinline__ bool find_units(const AttendParams& p, int at, int by
       seq->n = uniform(__shfl(s.n, src));
       seq->len = uniform(__shfl(s.len, src));
       cut->tiles = uniform(__shfl(o.tiles, src));
-      cut->splits = uniform(__shfl(o.splits, src));
+      cut->parts = uniform(__shfl(o.parts, src));
       cut->chunk = uniform(__shfl(o.chunk, src));
-      *first = uniform((int)min(base + __shfl(upto - mine, src), (int64_t)0x7fffffff));
+      const int64_t f = base + __shfl(upto - mine, src);
+      *first = ((int64_t)uniform((int)(f >> 32)) << 32) | (uint32_t)uniform((int)f);
       return true;
     }
     base += __shfl(upto, 63);
@@ -173,25 +181,77 @@ __device__ __forceinline__ bool find_units(const AttendParams& p, int at, int by
   return false;
 }
 
-__device__ __forceinline__ bool unit_of(const AttendParams& p, int at, Unit* u) {
-  Sequence s;
-  Shape o;
-  int first;
-  if (!find_units(p, at, 0, &u->b, &s, &o, &first)) return false;
-  u->start = s.start, u->n = s.n, u->len = s.len;
-  const int rel = at - first, per = o.tiles * o.splits;
-  u->head = rel / per;
-  const int r = rel - u->head * per, t = r / o.splits, split = r - t * o.splits;
-  u->row0 = (o.tiles - 1 - t) << p.log_rows;
-  u->splits = o.splits;
+// Shares of the few-rows kernel: workgroup w of n takes the units [at(w), at(w + 1)) of `all`, the first `rest` workgroups one more than the
+// others; one unit each where items are not shared.
+struct Shares {
+  int64_t all, each;
+  int n, rest;
+  __device__ __forceinline__ int64_t at(int w) const { return w * each + min(w, rest); }
+  __device__ __forceinline__ int holder(int64_t unit) const {
+    const int64_t larger = rest * (each + 1);
+    return unit < larger ? (int)divide(unit, each + 1) : rest + (int)divide(unit - larger, each);
+  }
+  // The quotient; by the short division where both sides allow it (64-bit divisions are long programs).
+  __device__ __forceinline__ static int64_t divide(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+  }
+};
+__device__ __forceinline__ Shares shares_of(const AttendParams& p) {
+  Shares s;
+  s.all = p.kv_heads * sum_over_batch(p, [&p](const Sequence& q) {
+            const Shape o = cut_of<true>(p, q, 0);
+            return (int64_t)o.tiles * o.parts;
+          });
+  const int64_t most = Shares::divide(s.all, max(1, p.min_chunk));
+  s.n = p.target > 0 ? (int)max((int64_t)1, min((int64_t)p.target, most)) : (int)min(max(s.all, (int64_t)1), (int64_t)p.units);
+  s.each = Shares::divide(s.all, s.n);
+  s.rest = (int)(s.all - s.each * s.n);
+  return s;
+}
+
+struct Unit {
+  int b, start, n, len;  // sequence
+  int head;              // key head
+  int tile;              // row tile, counted from the last one
+  int tiles, part, parts, chunk;  // of the sequence and head; of the item; keys of a unit
+  int row0;              // first row of the tile
+  int lo, hi;            // keys [lo, hi) from this unit on (hi: the item's end), lo a multiple of the key tile
+};
+
+// Fills in the rows and keys of an item's unit `part`.
+__device__ __forceinline__ void enter_item(const AttendParams& p, Unit* u) {
+  u->row0 = (u->tiles - 1 - u->tile) << p.log_rows;
   // keys that the tile's rows see: up to the last row's end, from the first row's begin
   const int t0 = u->row0 / p.group, t1 = min(u->row0 + (1 << p.log_rows) - 1, u->n * p.group - 1) / p.group;
   const int p0 = u->len - u->n;
-  const int hi = p.causal ? min(p0 + t1, u->len - 1) + 1 : u->len;
   const int lo = p.window < 0 ? 0 : max(0, p0 + (p.causal ? t0 : 0) - p.window);
-  const int64_t from = (int64_t)(lo & ~(p.keys - 1)) + (int64_t)split * o.chunk;
+  const int64_t from = (int64_t)(lo & ~(p.keys - 1)) + (int64_t)u->part * u->chunk;
+  u->hi = p.causal ? min(p0 + t1, u->len - 1) + 1 : u->len;
   u->lo = (int)min(from, (int64_t)kMostKeys);
-  u->hi = (int)min((int64_t)hi, from + o.chunk);
+}
+
+template <bool SHARES>
+__device__ __forceinline__ bool unit_of(const AttendParams& p, int64_t at, Unit* u) {
+  Sequence s;
+  Shape o;
+  int64_t first;
+  if (!find_units<SHARES>(p, at, false, &u->b, &s, &o, &first)) return false;
+  u->start = s.start, u->n = s.n, u->len = s.len;
+  const int64_t rel = at - first, item = Shares::divide(rel, o.parts);
+  u->part = (int)(rel - item * o.parts);
+  u->tiles = o.tiles, u->parts = o.parts, u->chunk = o.chunk;
+  u->head = (int)Shares::divide(item, o.tiles);
+  u->tile = (int)(item - (int64_t)u->head * o.tiles);
+  enter_item(p, u);
+  return true;
+}
+
+// The item after u's, at index `at`: another tile or head of the sequence, or another sequence's first.
+__device__ __forceinline__ bool next_item(const AttendParams& p, int64_t at, Unit* u) {
+  if (++u->tile == u->tiles) u->tile = 0, ++u->head;
+  if (u->head == p.kv_heads) return unit_of<true>(p, at, u);
+  u->part = 0;
+  enter_item(p, u);
   return true;
 }
 

@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
   __shared__ alignas(16) char lds[4 * TL::kBytes];  // keys, values; two buffers
 
   Unit u;
-  if (!unit_of(p, (int)blockIdx.x, &u)) return;
+  if (!unit_of<false>(p, blockIdx.x, &u)) return;
+  u.hi = (int)min((int64_t)u.hi, (int64_t)u.lo + u.chunk);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int rows = u.n * p.group;
@@ -455,7 +456,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
     const int row = row0 + 32 * n + col;
     const float total = sum_across32(sum[n]);
     if (row >= rows) continue;
-    if (u.splits > 1) {
+    if (u.parts > 1) {
       const int64_t at = (int64_t)blockIdx.x * ROWS + (row - u.row0);
       float* to = p.part_o + at * p.dim;
 #pragma unroll

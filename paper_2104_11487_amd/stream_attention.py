@@ -3,7 +3,7 @@ cache of keys and values, and attention over it (include/skipconv.h, the C names
 
 A 1 x 1 ``SkipConv`` layer's activation output, N x H x W x (heads * head_dim), viewed as
 N*H*W x heads x head_dim, is a tensor of tokens that these calls take as it lies. Work is enqueued on the current torch
-stream of the tensors' device; nothing is copied to the host.
+stream of the tensors' device; nothing is copied to the host. An object's calls are not thread-safe.
 
     rotary = Rotary(axis_frequencies((11, 11, 10)), head_dim=64)
     cache = PagedCache.empty(pages=256, page_size=64, kv_heads=2, head_dim=64)
@@ -14,7 +14,6 @@ stream of the tensors' device; nothing is copied to the host.
 from __future__ import annotations
 
 import ctypes
-import math
 from typing import Optional, Sequence
 
 import torch
@@ -69,16 +68,31 @@ def _need(ok: bool, message: str) -> None:
         raise ValueError(message)
 
 
-def _stream(device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+# The current stream's handle of a device (by index), without a Stream object around it.
+_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _heads_of(x: torch.Tensor, name: str, tokens: Optional[int], heads: Optional[int], dim: int, dtype, device) -> None:
-    s = x.shape
-    if len(s) != 3 or s[2] != dim or (tokens is not None and s[0] != tokens) or (heads is not None and s[1] != heads) \
-            or x.dtype != dtype or x.device != device or (x.stride(2) != 1 and x.numel() > 0):
-        want = ["tokens" if tokens is None else tokens, "heads" if heads is None else heads, dim]
-        raise ValueError(f"{name} must be a {dtype} tensor {want} on {device} with a packed last dimension")
+def _refuse(x, name: str, tokens, heads, dim, dtype, index: int):
+    want = ["tokens" if tokens is None else tokens, "heads" if heads is None else heads, dim]
+    raise ValueError(f"{name} must be a {dtype} tensor {want} on GPU {index} with a packed last dimension; "
+                     f"got {x.dtype} {list(x.shape)} with strides {x.stride()} on {x.device}")
+
+
+def _heads_of(x: torch.Tensor, name: str, tokens: Optional[int], heads: Optional[int], dim: int, dtype, index: int):
+    """Checks a tensor of heads; returns its tokens, heads and their strides."""
+    shape = x.shape
+    if len(shape) != 3:
+        _refuse(x, name, tokens, heads, dim, dtype, index)
+    t, h, d = shape
+    st, sh, sd = x.stride()
+    if d != dim or (tokens is not None and t != tokens) or (heads is not None and h != heads) or x.dtype is not dtype \
+            or x.get_device() != index or (sd != 1 and x.numel() > 0):
+        _refuse(x, name, tokens, heads, dim, dtype, index)
+    return t, h, st, sh
+
+
+def _like(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 class Rotary:
@@ -97,27 +111,37 @@ class Rotary:
         self.axes, self.pairs = self.freq.shape
         _need(1 <= self.axes <= 8 and 1 <= self.pairs <= head_dim // 2, "freq must have 1..8 axes and 1..head_dim / 2 pairs")
         self.head_dim, self.pairing, self.device = head_dim, pairing, freq.device
+        self._index = freq.get_device()
         self._desc = [skipconv_rotary(None, self.freq.data_ptr(), self.axes, self.pairs, _PAIRING[pairing], i) for i in (0, 1)]
+        self._ref = [ctypes.byref(d) for d in self._desc]
+        self._call = _S.lib().skipconv_rotate
 
     def desc(self, pos: torch.Tensor, tokens: int, inverse: bool = False) -> skipconv_rotary:
-        """The C description for these positions."""
-        if pos.dtype != torch.int32 or pos.device != self.device or tuple(pos.shape) != (tokens, self.axes) or not pos.is_contiguous():
+        """The C description for these positions (the object's own, valid until the next call of it)."""
+        if pos.dtype is not torch.int32 or pos.get_device() != self._index or pos.shape != (tokens, self.axes) or not pos.is_contiguous():
             raise ValueError(f"pos must be a contiguous int32 tensor {[tokens, self.axes]} on {self.device}")
-        d = self._desc[bool(inverse)]
+        d = self._desc[inverse]
         d.pos = pos.data_ptr()
         return d
 
     def rotate(self, x: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False) -> torch.Tensor:
         """x turned by its tokens' positions, into `out` (which may be x itself) or a new tensor."""
-        _need(x.dtype in _DTYPE, "x must be float32 or bfloat16")
-        _heads_of(x, "x", None, None, self.head_dim, x.dtype, self.device)
-        tokens, heads, dim = x.shape
+        dtype = x.dtype
+        code = _DTYPE.get(dtype)
+        if code is None:
+            raise ValueError("x must be float32 or bfloat16")
+        dim, index = self.head_dim, self._index
+        tokens, heads, xt, xh = _heads_of(x, "x", None, None, dim, dtype, index)
+        inverse = 1 if inverse else 0
+        self.desc(pos, tokens, inverse)
         if out is None:
-            out = torch.empty((tokens, heads, dim), dtype=x.dtype, device=x.device)
-        elif out is not x:
-            _heads_of(out, "out", tokens, heads, dim, x.dtype, x.device)
-        skipconv_rotate(self.desc(pos, tokens, inverse), tokens, heads, dim, _DTYPE[x.dtype], x.data_ptr(), x.stride(0), x.stride(1),
-                        out.data_ptr(), out.stride(0), out.stride(1), _stream(x.device))
+            out = _like(x)
+            yt, yh = heads * dim, dim
+        else:
+            _, _, yt, yh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
+        rc = self._call(self._ref[inverse], tokens, heads, dim, code, x.data_ptr(), xt, xh, out.data_ptr(), yt, yh, _stream(index))
+        if rc:
+            _S._check(rc)
         return out
 
     def backward(self, grad: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -160,6 +184,10 @@ class CacheBatch:
         _need(max_new >= 0, "max_new must be >= 0")
         self.page_table, self.row_start, self.kv_len, self.max_new = page_table, row_start, kv_len, int(max_new)
         self.sequences, self.device = n, device
+        self._index = kv_len.get_device()
+        # what a description of the cache takes from here
+        self._fields = (page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr())
+        self._width = page_table.shape[1]
 
 
 class PagedCache:
@@ -176,13 +204,16 @@ class PagedCache:
         _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "the pages' last dimension must be packed")
         self.k_pages, self.v_pages = k_pages, v_pages
         self.pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
         c = skipconv_cache()
         c.k_pages, c.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
         c.k_page, c.k_head, c.k_slot = k_pages.stride()[:3]
         c.v_page, c.v_head, c.v_slot = v_pages.stride()[:3]
         c.pages, c.page_size, c.kv_heads, c.head_dim, c.dtype = self.pages, self.page_size, self.kv_heads, self.head_dim, _DTYPE[self.dtype]
-        self._c = c
+        self._c, self._ref = c, ctypes.byref(c)
+        lib = _S.lib()
+        self._append, self._attend = lib.skipconv_cache_append, lib.skipconv_cache_attend
+        self._need = {}  # workspace bytes of attend(), by the shapes that decide them
 
     @classmethod
     def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
@@ -191,37 +222,40 @@ class PagedCache:
         return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
 
     def desc(self, batch: CacheBatch, tokens: int) -> skipconv_cache:
-        """The C description for a batch."""
-        _need(batch.device == self.device, "the batch is on another device than the cache")
+        """The C description for a batch (the object's own, valid until the next call of it)."""
+        if batch._index != self._index:
+            raise ValueError("the batch is on another device than the cache")
         c = self._c
-        c.page_table, c.row_start, c.kv_len = batch.page_table.data_ptr(), batch.row_start.data_ptr(), batch.kv_len.data_ptr()
-        c.tokens, c.batch, c.table_width = tokens, batch.sequences, batch.page_table.shape[1]
+        c.page_table, c.row_start, c.kv_len = batch._fields
+        c.tokens, c.batch, c.table_width = tokens, batch.sequences, batch._width
         return c
 
     def append(self, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, rotary: Optional[Rotary] = None,
                pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens' keys and values (tokens x kv_heads x head_dim) into the cache, the keys turned by `rotary` at
         `pos` (int32, tokens x axes). With `q` (tokens x heads x head_dim): also returns it turned, in `q_out` (may be q) or a new tensor."""
-        tokens = k.shape[0]
-        _heads_of(k, "k", None, self.kv_heads, self.head_dim, self.dtype, self.device)
-        _heads_of(v, "v", tokens, self.kv_heads, self.head_dim, self.dtype, self.device)
-        a = skipconv_append()
-        a.k, a.k_token, a.k_head = k.data_ptr(), k.stride(0), k.stride(1)
-        a.v, a.v_token, a.v_head = v.data_ptr(), v.stride(0), v.stride(1)
+        dim, dtype, index = self.head_dim, self.dtype, self._index
+        tokens, _, kt, kh = _heads_of(k, "k", None, self.kv_heads, dim, dtype, index)
+        _, _, vt, vh = _heads_of(v, "v", tokens, self.kv_heads, dim, dtype, index)
+        a = skipconv_append(k.data_ptr(), v.data_ptr(), None, None, kt, kh, vt, vh)
         if rotary is not None:
-            _need(pos is not None and rotary.head_dim == self.head_dim, "a rotation needs pos and the cache's head_dim")
-            r = rotary.desc(pos, tokens)
-            a.rotary = ctypes.pointer(r)
+            if pos is None or rotary.head_dim != dim:
+                raise ValueError("a rotation needs pos and the cache's head_dim")
+            a.rotary = ctypes.pointer(rotary.desc(pos, tokens, 0))
         if q is not None:
-            _need(rotary is not None, "queries are only turned: pass rotary and pos")
-            _heads_of(q, "q", tokens, None, self.head_dim, self.dtype, self.device)
+            if rotary is None:
+                raise ValueError("queries are only turned: pass rotary and pos")
+            _, heads, a.q_token, a.q_head = _heads_of(q, "q", tokens, None, dim, dtype, index)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            elif q_out is not q:
-                _heads_of(q_out, "q_out", tokens, q.shape[1], self.head_dim, self.dtype, self.device)
-            a.q, a.q_token, a.q_head, a.q_heads = q.data_ptr(), q.stride(0), q.stride(1), q.shape[1]
-            a.q_out, a.q_out_token, a.q_out_head = q_out.data_ptr(), q_out.stride(0), q_out.stride(1)
-        skipconv_cache_append(self.desc(batch, tokens), a, _stream(self.device))
+                q_out = _like(q)
+                a.q_out_token, a.q_out_head = heads * dim, dim
+            else:
+                _, _, a.q_out_token, a.q_out_head = _heads_of(q_out, "q_out", tokens, heads, dim, dtype, index)
+            a.q, a.q_out, a.q_heads = q.data_ptr(), q_out.data_ptr(), heads
+        self.desc(batch, tokens)
+        rc = self._append(self._ref, ctypes.byref(a), _stream(index))
+        if rc:
+            _S._check(rc)
         return q_out
 
     def attend(self, q: torch.Tensor, batch: CacheBatch, causal: bool = True, window: int = -1, scale: Optional[float] = None,
@@ -233,17 +267,25 @@ class PagedCache:
         tokens x heads x head_dim (zeros for a row that sees nothing), with return_lse also the float32 log of the
         sum of exponentials, tokens x heads (-inf there). Rows of no sequence are not written.
         """
-        _heads_of(q, "q", None, None, self.head_dim, self.dtype, self.device)
-        tokens, heads, dim = q.shape
+        dim, dtype, index = self.head_dim, self.dtype, self._index
+        tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
         if out is None:
-            out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+            out = _like(q)
+            ot, oh = heads * dim, dim
         else:
-            _heads_of(out, "out", tokens, heads, dim, self.dtype, self.device)
+            _, _, ot, oh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
         lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
-        a = skipconv_attend(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, q.stride(0), q.stride(1), out.stride(0),
-                            out.stride(1), heads, 1 if causal else 0, window, 1.0 / math.sqrt(dim) if scale is None else scale, batch.max_new)
+        a = skipconv_attend(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, qt, qh, ot, oh, heads, 1 if causal else 0,
+                            window, dim ** -0.5 if scale is None else scale, batch.max_new)
         c = self.desc(batch, tokens)
-        need = skipconv_attend_workspace(c, a)
+        shapes = (tokens, heads, batch.sequences, batch._width, window, batch.max_new)
+        need = self._need.get(shapes)
+        if need is None:
+            need = skipconv_attend_workspace(c, a)
+            if len(self._need) < 4096:
+                self._need[shapes] = need
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        skipconv_cache_attend(c, a, ws.data_ptr() if need else None, need, _stream(self.device))
+        rc = self._attend(self._ref, ctypes.byref(a), ws.data_ptr() if need else None, need, _stream(index))
+        if rc:
+            _S._check(rc)
         return (out, lse) if return_lse else out

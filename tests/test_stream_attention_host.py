@@ -200,7 +200,7 @@ def test_attend_refusals(kw, code):
 
 
 def test_attend_workspace():
-    lib, c, a, n = S.lib(), _cache(), _attend(), ctypes.c_size_t()
+    lib, c, a, n = S.lib(), _cache(table_width=1024), _attend(), ctypes.c_size_t()  # 16384 keys a sequence: split
     assert lib.skipconv_attend_workspace(ctypes.byref(c), ctypes.byref(a), ctypes.byref(n)) == S.SKIPCONV_OK
     assert n.value > 0
     assert lib.skipconv_cache_attend(ctypes.byref(c), ctypes.byref(a), A, n.value - 1, None) == SMALL
@@ -208,5 +208,7 @@ def test_attend_workspace():
     assert lib.skipconv_cache_attend(ctypes.byref(c), ctypes.byref(a), None, n.value, None) == INVALID
     assert lib.skipconv_attend_workspace(ctypes.byref(c), ctypes.byref(a), None) == INVALID
     assert lib.skipconv_attend_workspace(None, ctypes.byref(a), ctypes.byref(n)) == INVALID
+    short = _cache()  # 512 keys a sequence at most: one workgroup an item
+    assert lib.skipconv_attend_workspace(ctypes.byref(short), ctypes.byref(a), ctypes.byref(n)) == S.SKIPCONV_OK and n.value == 0
     c = _cache(tokens=1 << 20, batch=4)  # rows enough to fill the GPU: nothing is split
     assert lib.skipconv_attend_workspace(ctypes.byref(c), ctypes.byref(a), ctypes.byref(n)) == S.SKIPCONV_OK and n.value == 0
