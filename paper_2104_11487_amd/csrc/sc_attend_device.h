@@ -101,30 +101,13 @@ __device__ __forceinline__ Shape shape_of(const AttendParams& p, const Sequence&
   return o;
 }
 
-// The sum of `f` over the batch's sequences; called by whole waves.
-template <typename F>
-__device__ __forceinline__ int64_t sum_over_batch(const AttendParams& p, F f) {
-  const int lane = threadIdx.x & 63;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < p.c.batch; b0 += 64)
-    if (b0 + lane < p.c.batch) total += f(sequence_of(p.c, b0 + lane));
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-  return total;
+// The quotient; by the short division where both sides allow it (64-bit divisions are long programs).
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// Keys that a unit of the wide kernel should have; 0: nothing is split.
-__device__ __forceinline__ int chunk_goal(const AttendParams& p) {
-  if (p.target <= 0) return 0;
-  const int64_t total = sum_over_batch(p, [&p](const Sequence& s) {
-    const Shape o = shape_of(p, s);
-    return (int64_t)o.tiles * o.span;
-  });
-  return max(p.min_chunk, (int)min(ceil((double)total / (double)p.target), (double)kMostKeys));
-}
-
-// The cut of a sequence: by the wide kernel's goal, or (SHARES) into key tiles, where those are shared. A span begins anywhere, the
-// first tile at a whole one.
+// The cut of a sequence: by the wide kernel's goal (keys that a unit should have; 0: nothing is split), or (SHARES) into key tiles, where
+// those are shared. A span begins anywhere, the first tile at a whole one.
 template <bool SHARES>
 __device__ __forceinline__ Shape cut_of(const AttendParams& p, const Sequence& s, int goal) {
   Shape o = shape_of(p, s);
@@ -141,45 +124,76 @@ __device__ __forceinline__ Shape cut_of(const AttendParams& p, const Sequence& s
   return o;
 }
 
-// Finds the sequence whose units hold index `at` (by_row false), or whose rows hold row `at`: its number, extents, cut and the index
-// of its first unit. False where there is none. Called by whole waves.
+__device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
+  return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+// A wave's view of the batch's units: lane i holds sequence i, and where its units end; sequences from the 65th on are gone through by 64s.
 template <bool SHARES>
-__device__ __forceinline__ bool find_units(const AttendParams& p, int64_t at, bool by_row, int* b, Sequence* seq, Shape* cut, int64_t* first) {
-  const int lane = threadIdx.x & 63;
-  const int goal = SHARES ? 0 : chunk_goal(p);
-  int64_t base = 0;
-  for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
-    Sequence s = {0, 0, 0};
-    Shape o = {0, 0, 0, 0};
-    if (b0 + lane < p.c.batch) {
-      s = sequence_of(p.c, b0 + lane);
-      o = cut_of<SHARES>(p, s, goal);
+struct Units {
+  const AttendParams& p;
+  Sequence s;
+  Shape o;
+  int64_t upto, all;  // units of the sequences up to the lane's; of the batch
+  int goal;
+
+  __device__ __forceinline__ explicit Units(const AttendParams& q) : p(q), goal(0) {
+    s = load(0);
+    if constexpr (!SHARES) {
+      if (p.target > 0) {
+        Shape x = shape_of(p, s);
+        int64_t total = (int64_t)x.tiles * x.span;
+        for (int b0 = 64; b0 < p.c.batch; b0 += 64) x = shape_of(p, load(b0)), total += (int64_t)x.tiles * x.span;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+        goal = max(p.min_chunk, (int)min(ceil((double)total / (double)p.target), (double)kMostKeys));
+      }
     }
-    const int64_t mine = (int64_t)o.tiles * o.parts * p.kv_heads;
-    int64_t upto = mine;  // inclusive scan
+    o = cut_of<SHARES>(p, s, goal);
+    upto = scan(o);
+    all = from_lane(upto, 63);
+    for (int b0 = 64; b0 < p.c.batch; b0 += 64) all += from_lane(scan(cut_of<SHARES>(p, load(b0), goal)), 63);
+  }
+  __device__ __forceinline__ Sequence load(int b0) const {
+    const int b = b0 + (threadIdx.x & 63);
+    return b < p.c.batch ? sequence_of(p.c, b) : Sequence{0, 0, 0};
+  }
+  __device__ __forceinline__ int64_t scan(const Shape& x) const {  // inclusive, over the wave
+    int64_t v = (int64_t)x.tiles * x.parts * p.kv_heads;
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int64_t t = __shfl_up(upto, d);
-      if (lane >= d) upto += t;
+      const int64_t t = __shfl_up(v, d);
+      if (lane >= d) v += t;
     }
-    const uint64_t past = __ballot(by_row ? at >= s.start && at < s.start + s.n : base + upto > at);
-    if (past) {
-      const int src = (int)__ffsll((unsigned long long)past) - 1;
-      *b = b0 + src;
-      seq->start = uniform(__shfl(s.start, src));
-      seq->n = uniform(__shfl(s.n, src));
-      seq->len = uniform(__shfl(s.len, src));
-      cut->tiles = uniform(__shfl(o.tiles, src));
-      cut->parts = uniform(__shfl(o.parts, src));
-      cut->chunk = uniform(__shfl(o.chunk, src));
-      const int64_t f = base + __shfl(upto - mine, src);
-      *first = ((int64_t)uniform((int)(f >> 32)) << 32) | (uint32_t)uniform((int)f);
-      return true;
-    }
-    base += __shfl(upto, 63);
+    return v;
   }
-  return false;
-}
+  // The sequence whose units hold index `at` (by_row false), or whose rows hold row `at`: its number, extents, cut and the index of its
+  // first unit. False where there is none.
+  __device__ __forceinline__ bool find(int64_t at, bool by_row, int* b, Sequence* seq, Shape* cut, int64_t* first) const {
+    int64_t base = 0;
+    for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
+      const Sequence x = b0 ? load(b0) : s;
+      const Shape y = b0 ? cut_of<SHARES>(p, x, goal) : o;
+      const int64_t end = b0 ? scan(y) : upto;
+      const uint64_t past = __ballot(by_row ? at >= x.start && at < x.start + x.n : base + end > at);
+      if (past) {
+        const int src = (int)__ffsll((unsigned long long)past) - 1;
+        *b = b0 + src;
+        seq->start = __builtin_amdgcn_readlane(x.start, src);
+        seq->n = __builtin_amdgcn_readlane(x.n, src);
+        seq->len = __builtin_amdgcn_readlane(x.len, src);
+        cut->tiles = __builtin_amdgcn_readlane(y.tiles, src);
+        cut->parts = __builtin_amdgcn_readlane(y.parts, src);
+        cut->chunk = __builtin_amdgcn_readlane(y.chunk, src);
+        *first = base + from_lane(end, src) - (int64_t)cut->tiles * cut->parts * p.kv_heads;
+        return true;
+      }
+      base += from_lane(end, 63);
+    }
+    return false;
+  }
+};
 
 // Shares of the few-rows kernel: workgroup w of n takes the units [at(w), at(w + 1)) of `all`, the first `rest` workgroups one more than the
 // others; one unit each where items are not shared.
@@ -191,21 +205,14 @@ struct Shares {
     const int64_t larger = rest * (each + 1);
     return unit < larger ? (int)divide(unit, each + 1) : rest + (int)divide(unit - larger, each);
   }
-  // The quotient; by the short division where both sides allow it (64-bit divisions are long programs).
-  __device__ __forceinline__ static int64_t divide(int64_t a, int64_t b) {
-    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-  }
 };
-__device__ __forceinline__ Shares shares_of(const AttendParams& p) {
+__device__ __forceinline__ Shares shares_of(const AttendParams& p, int64_t all) {
   Shares s;
-  s.all = p.kv_heads * sum_over_batch(p, [&p](const Sequence& q) {
-            const Shape o = cut_of<true>(p, q, 0);
-            return (int64_t)o.tiles * o.parts;
-          });
-  const int64_t most = Shares::divide(s.all, max(1, p.min_chunk));
-  s.n = p.target > 0 ? (int)max((int64_t)1, min((int64_t)p.target, most)) : (int)min(max(s.all, (int64_t)1), (int64_t)p.units);
-  s.each = Shares::divide(s.all, s.n);
-  s.rest = (int)(s.all - s.each * s.n);
+  s.all = all;
+  const int64_t most = divide(all, max(1, p.min_chunk));
+  s.n = p.target > 0 ? (int)max((int64_t)1, min((int64_t)p.target, most)) : (int)min(max(all, (int64_t)1), (int64_t)p.units);
+  s.each = divide(all, s.n);
+  s.rest = (int)(all - s.each * s.n);
   return s;
 }
 
@@ -231,27 +238,28 @@ __device__ __forceinline__ void enter_item(const AttendParams& p, Unit* u) {
 }
 
 template <bool SHARES>
-__device__ __forceinline__ bool unit_of(const AttendParams& p, int64_t at, Unit* u) {
+__device__ __forceinline__ bool unit_of(const Units<SHARES>& units, int64_t at, Unit* u) {
+  const AttendParams& p = units.p;
   Sequence s;
   Shape o;
   int64_t first;
-  if (!find_units<SHARES>(p, at, false, &u->b, &s, &o, &first)) return false;
+  if (!units.find(at, false, &u->b, &s, &o, &first)) return false;
   u->start = s.start, u->n = s.n, u->len = s.len;
-  const int64_t rel = at - first, item = Shares::divide(rel, o.parts);
+  const int64_t rel = at - first, item = divide(rel, o.parts);
   u->part = (int)(rel - item * o.parts);
   u->tiles = o.tiles, u->parts = o.parts, u->chunk = o.chunk;
-  u->head = (int)Shares::divide(item, o.tiles);
+  u->head = (int)divide(item, o.tiles);
   u->tile = (int)(item - (int64_t)u->head * o.tiles);
   enter_item(p, u);
   return true;
 }
 
 // The item after u's, at index `at`: another tile or head of the sequence, or another sequence's first.
-__device__ __forceinline__ bool next_item(const AttendParams& p, int64_t at, Unit* u) {
+__device__ __forceinline__ bool next_item(const Units<true>& units, int64_t at, Unit* u) {
   if (++u->tile == u->tiles) u->tile = 0, ++u->head;
-  if (u->head == p.kv_heads) return unit_of<true>(p, at, u);
+  if (u->head == units.p.kv_heads) return unit_of(units, at, u);
   u->part = 0;
-  enter_item(p, u);
+  enter_item(units.p, u);
   return true;
 }
 

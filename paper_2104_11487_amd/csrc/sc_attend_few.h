@@ -9,6 +9,8 @@
 // Products as in the wide kernel (sc_attend_wide.h), transposed, on 16 x 16 tiles.
 #pragma once
 
+#include <type_traits>
+
 #include "sc_attend_tile.h"
 
 #pragma clang fp contract(off)
@@ -36,7 +38,8 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
   constexpr int kBuffers = NW * kWaveBytes, kJoin = NW * ROWS * (JP + 2) * 4;
   __shared__ alignas(16) char lds[kBuffers > kJoin ? kBuffers : kJoin];
 
-  const Shares shares = shares_of(p);
+  const Units<true> batch(p);
+  const Shares shares = shares_of(p, batch.all);
   if ((int)blockIdx.x >= shares.n) return;
   const int64_t end = shares.at(blockIdx.x + 1);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -45,7 +48,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
 
   const int64_t first_unit = shares.at(blockIdx.x);
   Unit u;
-  if (first_unit >= end || !unit_of<true>(p, first_unit, &u)) return;
+  if (first_unit >= end || !unit_of(batch, first_unit, &u)) return;
   for (int64_t at = first_unit;;) {
     const int units = (int)min(end - at, (int64_t)(u.parts - u.part));  // of this item
     const bool whole = units == u.parts, begins = at == first_unit;
@@ -103,14 +106,9 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     const int krow = TL::swizzle(col) & (TL::kChunks - 1);
     const int vr = 4 * quad + (col >> 2), vc = (col & 3) >> 1;
 
-    for (int it = 0; it < count; ++it) {
-      const int key0 = begin + it * kStep;
-      char* kt = mine + (it & 1) * 2 * TL::kBytes;
-      char* vt = kt + TL::kBytes;
-      if (it + 1 < count) wait_loads<LoneStager<T, TL, KEYS>::kOps>();  // the younger tile's copies stay in flight
-      else wait_loads<0>();
-      const bool edge = key0 < all_lo || key0 + KEYS - 1 > all_hi;
-
+    // One tile's work. edge: some row does not see some of its keys.
+    auto tile = [&](auto edge_, int key0, const char* kt, const char* vt) {
+      constexpr bool edge = edge_;
       floatx4 s[NB][NS];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -134,7 +132,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
         }
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        if (edge) {
+        if constexpr (edge) {
 #pragma unroll
           for (int j = 0; j < NS; ++j)
 #pragma unroll
@@ -180,8 +178,8 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
                         pack2(s[n][NS - 1][2], s[n][NS - 1][3])};
           pf[n] = __builtin_bit_cast(bf16x8, w);
         }
-        uint32_t mask[2][2] = {{~0u, ~0u}, {~0u, ~0u}};
-        if (edge) {
+        uint32_t mask[2][2];
+        if constexpr (edge) {
 #pragma unroll
           for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -197,7 +195,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
           for (int e = 0; e < 2; ++e) {
             const int r = 16 * e + vr, c = (2 * d + vc) ^ (TL::swizzle(r) & (TL::kChunks - 1));
             q[e] = read_column4(vt + r * TL::kRowBytes + c * 16 + (lane & 1) * 8);
-            if (edge) {
+            if constexpr (edge) {
               q[e][0] = finite2(q[e][0], mask[e][0], &odd);
               q[e][1] = finite2(q[e][1], mask[e][1], &odd);
             }
@@ -215,7 +213,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
           for (int d = 0; d < ND; ++d) {
             const int e = 16 * d + col, c = (e >> 2) ^ (TL::swizzle(key) & (TL::kChunks - 1));
             float a = *reinterpret_cast<const float*>(vt + key * TL::kRowBytes + c * 16 + (e & 3) * 4);
-            if (edge) a = finite1(a, keep, &odd);
+            if constexpr (edge) a = finite1(a, keep, &odd);
 #pragma unroll
             for (int n = 0; n < NB; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[n][0][r], o[n][d], 0, 0, 0);
           }
@@ -242,6 +240,16 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
             }
         }
       }
+    };
+
+    for (int it = 0; it < count; ++it) {
+      const int key0 = begin + it * kStep;
+      char* kt = mine + (it & 1) * 2 * TL::kBytes;
+      char* vt = kt + TL::kBytes;
+      if (it + 1 < count) wait_loads<LoneStager<T, TL, KEYS>::kOps>();  // the younger tile's copies stay in flight
+      else wait_loads<0>();
+      if (key0 >= all_lo && key0 + KEYS - 1 <= all_hi) tile(std::false_type{}, key0, kt, vt);
+      else tile(std::true_type{}, key0, kt, vt);
       // this tile's buffers are free: the fragments read from them have reached their products
       if (it + 2 < count) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -294,7 +302,7 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
           p.lse[(int64_t)(u.start + t) * p.q_heads + h] = total == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
       }
     }
-    if (at >= end || !next_item(p, at, &u)) break;
+    if (at >= end || !next_item(batch, at, &u)) break;
     __syncthreads();  // the join's reads come before the next item's copies
   }
 }

@@ -22,7 +22,8 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   Sequence s;
   Shape o;
   int64_t first;
-  if (!find_units<SHARES>(p, token, true, &b, &s, &o, &first)) return;
+  const Units<SHARES> units(p);
+  if (!units.find(token, true, &b, &s, &o, &first)) return;
   const int head = h / p.group, row = (token - s.start) * p.group + (h - head * p.group);
   const int tile = row >> p.log_rows, rows = 1 << p.log_rows;
   const int64_t unit = first + ((int64_t)head * o.tiles + (o.tiles - 1 - tile)) * o.parts;
@@ -31,7 +32,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   if constexpr (SHARES) {
     // workgroups w0 .. w1 held the item's units; each one's part is its first (slot 2 w), but where the share began before the item,
     // which only the first of them can, its last (2 w + 1)
-    const Shares all = shares_of(p);
+    const Shares all = shares_of(p, units.all);
     const int w0 = all.holder(unit), w1 = all.holder(unit + o.parts - 1);
     parts = w1 - w0 + 1, step = 2;
     slot0 = 2 * (int64_t)w0;

@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
   __shared__ alignas(16) char lds[4 * TL::kBytes];  // keys, values; two buffers
 
   Unit u;
-  if (!unit_of<false>(p, blockIdx.x, &u)) return;
+  if (!unit_of(Units<false>(p), blockIdx.x, &u)) return;
   u.hi = (int)min((int64_t)u.hi, (int64_t)u.lo + u.chunk);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
