@@ -132,8 +132,13 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
     units = shared ? kWantFew : tiles * c->kv_heads;
     p->slots = shared ? 2 * kWantFew : 0;
   } else {
-    p->target = tiles * c->kv_heads < kWantWide ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
-    p->min_chunk = 4 * p->keys;
+    // A unit's keys are split where the items leave compute units idle and a chunk still outweighs the join (about 8 us): a block of
+    // 32 keys takes a workgroup some 0.4 us for bf16 heads of 128, 4 us for fp32.
+    const int64_t room = (int64_t)c->table_width * c->page_size, reach = a->window < 0 ? room : (int64_t)a->window + most;
+    const int blocks = elem == 2 ? 16 * 128 / std::max(64, c->head_dim) : std::max(1, 3 * 96 / c->head_dim);
+    p->min_chunk = std::max(32 * blocks, p->keys);
+    const bool split = tiles * c->kv_heads < kWantWide && std::min(room, reach) > 2 * p->min_chunk;
+    p->target = split ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
     units = (tiles + p->target) * c->kv_heads;
     p->slots = p->target ? (int)std::min<int64_t>(units, kMostRows) : 0;
   }

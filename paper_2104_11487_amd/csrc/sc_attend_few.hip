@@ -9,11 +9,86 @@ namespace {
 
 constexpr int kJoinWaves = 4;
 
-// One workgroup a row (token, query head): its parts' references, sums and outputs, joined in the order of their keys. The parts' weights
-// go to LDS, 256 at a time; the parts are dealt to groups of dim / 4 lanes (a power of two), whose shares are then added in order.
+// Where a row's parts lie in the workspace.
+struct Parts {
+  int64_t slot0;
+  int count, step, skip, in_tile;
+  __device__ __forceinline__ int64_t at(int i, int log_rows) const { return ((slot0 + (int64_t)i * step + (i == 0 ? skip : 0)) << log_rows) + in_tile; }
+};
+
+// The parts of row (token, query head h), of which the sequence and its cut are known; count 0: the row was not split.
 // SHARES: the parts of the few-rows kernel, otherwise those of the wide kernel.
+template <bool SHARES>
+__device__ __forceinline__ Parts parts_of(const AttendParams& p, const Units<SHARES>& units, const Sequence& s, const Shape& o, int64_t first, int token, int h) {
+  const int head = h / p.group, row = (token - s.start) * p.group + (h - head * p.group), tile = row >> p.log_rows;
+  const int64_t unit = first + ((int64_t)head * o.tiles + (o.tiles - 1 - tile)) * o.parts;
+  Parts r = {unit, o.parts, 1, 0, row - (tile << p.log_rows)};
+  if constexpr (SHARES) {
+    // workgroups w0 .. w1 held the item's units; each one's part is its first (slot 2 w), but where the share began before the item,
+    // which only the first of them can, its last (2 w + 1)
+    const Shares all = shares_of(p, units.all);
+    const int w0 = all.holder(unit), w1 = all.holder(unit + o.parts - 1);
+    r.count = w1 - w0 + 1, r.step = 2;
+    r.slot0 = 2 * (int64_t)w0;
+    r.skip = all.at(w0) < unit ? 1 : 0;
+  }
+  if (r.count <= 1 || r.slot0 + (int64_t)r.count * r.step > p.slots) r.count = 0;
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(const AttendParams& p, int token, int h, int e, const floatx4& v, float top, float total) {
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  char* to = p.out + ((int64_t)token * p.o_token + (int64_t)h * p.o_head) * (int64_t)sizeof(T);
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to + e * 2) = u32x2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
+  else *reinterpret_cast<floatx4*>(to + e * 4) = floatx4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
+  if (p.lse && e == 0)
+    p.lse[(int64_t)token * p.q_heads + h] = total == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+}
+
+// Many rows: each takes `width` lanes (dim / 4, a power of two), which go through its parts in the order of their keys.
 template <typename T, bool SHARES>
-__global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendParams p) {
+__global__ void __launch_bounds__(64 * kJoinWaves) attend_join_rows_kernel(AttendParams p, int width) {
+  const Units<SHARES> units(p);
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), mine = lane / width, e = (lane - mine * width) * 4;
+  const int rows = 64 / width, all = p.c.tokens * p.q_heads;
+  const int row0 = ((int)blockIdx.x * kJoinWaves + wave) * rows;
+  Parts parts = {0, 0, 1, 0, 0};
+  Sequence s;
+  Shape o;
+  int64_t first = 0;
+  int b, known = -1;
+  bool held = false;
+  for (int i = 0; i < rows && row0 + i < all; ++i) {
+    const int token = (row0 + i) / p.q_heads;
+    if (token != known) held = units.find(token, true, &b, &s, &o, &first), known = token;
+    if (!held || o.parts <= 1) continue;
+    const Parts r = parts_of(p, units, s, o, first, token, row0 + i - token * p.q_heads);
+    if (i == mine) parts = r;
+  }
+  if (parts.count == 0 || e >= p.dim) return;
+  float top = kNegInf;
+  for (int i = 0; i < parts.count; ++i) top = fmaxf(top, p.part_ml[parts.at(i, p.log_rows) * 2]);
+  floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
+  float total = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < parts.count; ++i) {
+    const int64_t at = parts.at(i, p.log_rows);
+    const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + at * 2);
+    const floatx4 x = *reinterpret_cast<const floatx4*>(p.part_o + at * p.dim + e);
+    const float f = join_weight(ml.x, top);
+    total += ml.y * f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += x[k] * f;
+  }
+  const int token = (row0 + mine) / p.q_heads;
+  store_row<T>(p, token, row0 + mine - token * p.q_heads, e, v, top, total);
+}
+
+// Few rows, one a workgroup: the parts' weights go to LDS, 256 at a time; the parts are dealt to groups of `width` lanes, whose
+// shares are then added in order.
+template <typename T, bool SHARES>
+__global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendParams p, int width) {
   constexpr int kThreads = 64 * kJoinWaves;
   __shared__ floatx4 shares[kThreads];
   __shared__ float weights[kThreads], tops[kJoinWaves], sums[kJoinWaves];
@@ -24,31 +99,13 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   int64_t first;
   const Units<SHARES> units(p);
   if (!units.find(token, true, &b, &s, &o, &first)) return;
-  const int head = h / p.group, row = (token - s.start) * p.group + (h - head * p.group);
-  const int tile = row >> p.log_rows, rows = 1 << p.log_rows;
-  const int64_t unit = first + ((int64_t)head * o.tiles + (o.tiles - 1 - tile)) * o.parts;
-  int64_t slot0 = unit;  // the first part's slot; the next ones follow, `step` apart
-  int parts = o.parts, step = 1, skip = 0;
-  if constexpr (SHARES) {
-    // workgroups w0 .. w1 held the item's units; each one's part is its first (slot 2 w), but where the share began before the item,
-    // which only the first of them can, its last (2 w + 1)
-    const Shares all = shares_of(p, units.all);
-    const int w0 = all.holder(unit), w1 = all.holder(unit + o.parts - 1);
-    parts = w1 - w0 + 1, step = 2;
-    slot0 = 2 * (int64_t)w0;
-    skip = all.at(w0) < unit ? 1 : 0;
-  }
-  if (parts <= 1 || slot0 + (int64_t)parts * step > p.slots) return;
-  const int in_tile = row - (tile << p.log_rows);
-  auto part_at = [&](int i) { return (slot0 + (int64_t)i * step + (i == 0 ? skip : 0)) * rows + in_tile; };
+  const Parts parts = parts_of(p, units, s, o, first, token, h);
+  if (parts.count == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-
-  int width = 8;
-  while (width * 4 < p.dim) width *= 2;  // lanes of a group: 8..64
   const int group = tid / width, groups = kThreads / width, e = (tid & (width - 1)) * 4;
 
   float top = kNegInf;
-  for (int i = tid; i < parts; i += kThreads) top = fmaxf(top, p.part_ml[part_at(i) * 2]);
+  for (int i = tid; i < parts.count; i += kThreads) top = fmaxf(top, p.part_ml[parts.at(i, p.log_rows) * 2]);
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   if (lane == 0) tops[wave] = top;
@@ -58,11 +115,11 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
 
   floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
   float total = 0.0f;
-  for (int i0 = 0; i0 < parts; i0 += kThreads) {
-    const int n = min(parts - i0, kThreads);
+  for (int i0 = 0; i0 < parts.count; i0 += kThreads) {
+    const int n = min(parts.count - i0, kThreads);
     if (i0 > 0) __syncthreads();
     if (tid < n) {
-      const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + part_at(i0 + tid) * 2);
+      const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + parts.at(i0 + tid, p.log_rows) * 2);
       weights[tid] = join_weight(ml.x, top);
       total += ml.y * weights[tid];
     }
@@ -70,7 +127,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
     if (e < p.dim) {
 #pragma unroll 4
       for (int i = group; i < n; i += groups) {
-        const floatx4 y = *reinterpret_cast<const floatx4*>(p.part_o + part_at(i0 + i) * p.dim + e);
+        const floatx4 y = *reinterpret_cast<const floatx4*>(p.part_o + parts.at(i0 + i, p.log_rows) * p.dim + e);
         const float f = weights[i];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] += y[k] * f;
@@ -86,17 +143,27 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   total = 0.0f;
 #pragma unroll
   for (int w = 0; w < kJoinWaves; ++w) total += sums[w];
-  for (int g = 1; g < min(groups, parts); ++g) {
+  for (int g = 1; g < min(groups, parts.count); ++g) {
     const floatx4 x = shares[g * width + tid];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] += x[k];
   }
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  char* to = p.out + ((int64_t)token * p.o_token + (int64_t)h * p.o_head) * (int64_t)sizeof(T);
-  if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2*>(to + e * 2) = u32x2{pack2(v[0] * inv, v[1] * inv), pack2(v[2] * inv, v[3] * inv)};
-  else *reinterpret_cast<floatx4*>(to + e * 4) = floatx4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
-  if (p.lse && e == 0)
-    p.lse[(int64_t)token * p.q_heads + h] = total == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
+  store_row<T>(p, token, h, e, v, top, total);
+}
+
+template <typename T, bool SHARES>
+void launch_join(const AttendParams& p, hipStream_t stream) {
+  const int rows = p.c.tokens * p.q_heads;
+  int width = 8;
+  while (width * 4 < p.dim) width *= 2;  // lanes of a row: 8..64
+  // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 128 parts); then lane groups, of
+  // which many rows of few parts need no exchange.
+  if (rows < 512) {
+    attend_join_kernel<T, SHARES><<<dim3((unsigned)rows), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
+  } else {
+    const int each = kJoinWaves * (64 / width);
+    attend_join_rows_kernel<T, SHARES><<<dim3((unsigned)((rows + each - 1) / each)), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
+  }
 }
 
 }  // namespace
@@ -109,14 +176,13 @@ int few_waves_of(int elem_bytes, int dim) {
 hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream) { return launch_few_dim<uint16_t>(p, stream); }
 
 hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream) {
-  const dim3 grid((unsigned)(p.c.tokens * p.q_heads)), block(64 * kJoinWaves);
-  const bool shares = p.log_rows != kLogWideRows && p.log_rows != kLogWideRows + 1;
+  const bool shares = p.log_rows < kLogWideRows;
   if (elem_bytes == 2) {
-    if (shares) attend_join_kernel<uint16_t, true><<<grid, block, 0, stream>>>(p);
-    else attend_join_kernel<uint16_t, false><<<grid, block, 0, stream>>>(p);
+    if (shares) launch_join<uint16_t, true>(p, stream);
+    else launch_join<uint16_t, false>(p, stream);
   } else {
-    if (shares) attend_join_kernel<float, true><<<grid, block, 0, stream>>>(p);
-    else attend_join_kernel<float, false><<<grid, block, 0, stream>>>(p);
+    if (shares) launch_join<float, true>(p, stream);
+    else launch_join<float, false>(p, stream);
   }
   return hipGetLastError();
 }

@@ -183,18 +183,39 @@ __device__ __forceinline__ u32x2 read_column4(uint32_t lds_at) {
 }
 __device__ __forceinline__ u32x2 read_column4(const char* at) { return read_column4((uint32_t)(uintptr_t)SC_LDS(at, const char)); }
 
-// Of two packed bf16 values: those outside the mask become zero, and those that are infinite or NaN too, which sets *odd.
+// Of two packed bf16 values those that are infinite or NaN become zero.
+__device__ __forceinline__ uint32_t finite2(uint32_t v) {
+  if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+  if ((v & 0x7f800000u) == 0x7f800000u) v &= 0x0000ffffu;
+  return v;
+}
+__device__ __forceinline__ float finite1(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.0f : v; }
+
+// Of 16 bytes of values: whether one is infinite or NaN (its exponent is all ones, which a carry shows); with those zero.
+template <typename T>
+__device__ __forceinline__ int not_finite(uint4 v) {
+  const uint32_t mask = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, one = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+  const uint32_t x = ((v.x & mask) + one) | ((v.y & mask) + one) | ((v.z & mask) + one) | ((v.w & mask) + one);
+  return (x & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u)) != 0;
+}
+template <typename T>
+__device__ __forceinline__ uint4 finite_of(uint4 v) {
+  if constexpr (sizeof(T) == 2) return uint4{finite2(v.x), finite2(v.y), finite2(v.z), finite2(v.w)};
+  else return uint4{__float_as_uint(finite1(__uint_as_float(v.x))), __float_as_uint(finite1(__uint_as_float(v.y))),
+                    __float_as_uint(finite1(__uint_as_float(v.z))), __float_as_uint(finite1(__uint_as_float(v.w)))};
+}
+
+// Of two bf16 values (a float): those outside the mask become zero too, and one inside it that is not finite sets *odd.
 __device__ __forceinline__ uint32_t finite2(uint32_t v, uint32_t mask, int* odd) {
   v &= mask;
-  if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u, *odd = 1;
-  if ((v & 0x7f800000u) == 0x7f800000u) v &= 0x0000ffffu, *odd = 1;
-  return v;
+  const uint32_t f = finite2(v);
+  if (f != v) *odd = 1;
+  return f;
 }
 __device__ __forceinline__ float finite1(float v, bool keep, int* odd) {
   if (!keep) return 0.0f;
-  if ((__float_as_uint(v) & 0x7f800000u) != 0x7f800000u) return v;
-  *odd = 1;
-  return 0.0f;
+  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) *odd = 1;
+  return finite1(v);
 }
 
 }  // namespace sc

@@ -37,7 +37,7 @@ constexpr int kWideWaves = 4;
 constexpr float kSlack = 8.0f;  // powers of two that an exponential may exceed one by
 
 constexpr int wide_waves_per_simd(int elem, int dim, int blocks) {  // that the registers are planned for
-  return dim * elem <= 256 ? 2 : 1;
+  return dim * elem <= (elem == 2 ? 256 : 384) ? 2 : 1;
 }
 
 typedef uint32_t u32x4_lds __attribute__((ext_vector_type(4)));
@@ -129,9 +129,8 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
     for (int i = threadIdx.x; i < 4 * TL::kBytes / 16; i += 64 * NW) reinterpret_cast<uint4*>(lds)[i] = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
   }
-  // keys that every row of the unit sees are [all_lo, all_hi]; that a row of the wave sees, [any_lo, any_hi]
-  const int all_lo = seen_by(p, u, u.row0 + ROWS - 1).lo, all_hi = seen_by(p, u, u.row0).hi;
-  const int any_lo = seen_by(p, u, row0).lo, any_hi = row0 < rows ? seen_by(p, u, row0 + WROWS - 1).hi : -1;
+  // keys that every row of the unit sees: [all_lo, all_hi]
+  const int all_lo = seen_by(p, u, u.row0 + ROWS - 1).lo, all_hi = min(seen_by(p, u, u.row0).hi, u.hi - 1);
 
   floatx16 o[NR][ND];
   float ref[NR], base[NR], sum[NR];  // base: what exponents are taken relative to, the reference or 0 before there is one
@@ -219,7 +218,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         const float next = fmaxf(ref[n], top.at[n]);
-        const float keep = next == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref[n] - next);
+        const float keep = ref[n] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref[n] - next);  // 1: nothing to rescale yet
         ref[n] = next;
         base[n] = next == kNegInf ? 0.0f : next;
         sum[n] *= keep;
@@ -232,8 +231,8 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
   };
   auto exponent = [&](float x, int n) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, p.scale_log2, -base[n])); };
 
-  // A block whose keys every row sees, and the scores of the next one (keys at `kt`, values at `vt`).
-  auto whole_block = [&](int kt, int vt, Scores& s, Scores& next) {
+  // A block's exponentials and values, and the scores of the next one (keys at `kt`, values at `vt`).
+  auto run_block = [&](int kt, int vt, Scores& s, Scores& next) {
     if constexpr (kHalf) {
       // Laid out by hand: each slot is one fragment's products, with the LDS reads of the one PRE slots later and a share of the
       // vector unit's work (this block's exponentials, then the next one's largest score) to run beside it.
@@ -308,95 +307,68 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
     }
   };
 
-  // A block of which some row does not see some key (values at `vt`). A masked key's exponential is zero, but zero times an
-  // infinity or a NaN is not: values of keys that no row of the wave sees are cleared, and those that are not finite leave the
-  // product and are added to the rows that see their key.
-  auto edge_block = [&](int key0, int vt, Scores& s) {
-#pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[n][r] = exponent(s[n][r], n);
-        sum[n] += s[n][r];
-      }
-    int odd = 0;
-    if constexpr (kHalf) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint4 w[NR];
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          const floatx16& x = s[n];
-          const int r = 8 * k;
-          w[n] = uint4{pack2(x[r], x[r + 1]), pack2(x[r + 2], x[r + 3]), pack2(x[r + 4], x[r + 5]), pack2(x[r + 6], x[r + 7])};
-        }
-        uint32_t mask[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = key0 + 16 * k + 8 * (i >> 1) + 4 * half + 2 * (i & 1);
-          mask[i] = (key >= any_lo && key <= any_hi ? 0xffffu : 0u) | (key + 1 >= any_lo && key + 1 <= any_hi ? 0xffff0000u : 0u);
-        }
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          u32x4_lds v = value_piece(k, d, vt);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = finite2(v[i], mask[i], &odd);
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-            o[n][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[n]), o[n][d], 0, 0, 0);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int key = key0 + key_of(r);
-        const bool keep = key >= any_lo && key <= any_hi;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          const float v = finite1(value1(key_of(r), d, vt), keep, &odd);
-#pragma unroll
-          for (int n = 0; n < NR; ++n) o[n][d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[n][r], o[n][d], 0, 0, 0);
-        }
-      }
-    }
-    if (__any(odd)) {
-      const int from = max(key0, any_lo), to = min(key0 + 31, any_hi);
-      for (int key = from; key <= to; ++key) {
-        const int r = key - key0, sw = TL::swizzle(r) & (TL::kChunks - 1);
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int e = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
-            const char* at = lds + 2 * TL::kBytes + vt + r * TL::kRowBytes + (((e / TL::kElems) ^ sw) << 4) + (e % TL::kElems) * (int)sizeof(T);
-            float v;
-            if constexpr (kHalf) v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
-            else v = *reinterpret_cast<const float*>(at);
-            if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) {
-#pragma unroll
-              for (int n = 0; n < NR; ++n)
-                if (key >= seen[n].lo && key <= seen[n].hi) o[n][d][i] += v;
-            }
-          }
-      }
-    }
-  };
-
   // Keys run one block ahead of values: with the values of tile i (keys i * KEYS ..) come the keys 32 further on, both in buffer i & 1.
   constexpr int kBlock = 32 * TL::kRowBytes;
   char* const keys = lds;
   char* const values = lds + 2 * TL::kBytes;
   Stager<T, TL, NW, UNI, 32> stager(p, u, wave, lane, chunks);
   Scores s0, s1;
+  const int first_key = seen_by(p, u, u.row0).lo;  // of the unit
+  // A tile of which some row does not see some key. A masked key's exponential is zero, but zero times an infinity or a NaN is not: the
+  // values of keys that no row of the unit sees are cleared in LDS, and those that are not finite are added to the rows
+  // that see their key and cleared too.
+  auto settle = [&](int key0, int buf) {
+    uint4* const rows_of = reinterpret_cast<uint4*>(values + buf * TL::kBytes);
+    int odd = 0;
+    for (int i = threadIdx.x; i < KEYS * TL::kChunks; i += 64 * NW) {
+      const int key = key0 + i / TL::kChunks;
+      if (key < first_key || key >= u.hi) rows_of[i] = uint4{0u, 0u, 0u, 0u};
+      else odd |= not_finite<T>(rows_of[i]);
+    }
+    if (!__syncthreads_or(odd)) return;
+#pragma unroll 1
+    for (int key = max(key0, first_key); key < min(key0 + KEYS, u.hi); ++key) {
+      const int r = key - key0, sw = TL::swizzle(r) & (TL::kChunks - 1);
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int e = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
+          const char* at = values + buf * TL::kBytes + r * TL::kRowBytes + (((e / TL::kElems) ^ sw) << 4) + (e % TL::kElems) * (int)sizeof(T);
+          float v;
+          if constexpr (kHalf) v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
+          else v = *reinterpret_cast<const float*>(at);
+          if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+              if (key >= seen[n].lo && key <= seen[n].hi) o[n][d][i] += v;
+          }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < KEYS * TL::kChunks; i += 64 * NW) rows_of[i] = finite_of<T>(rows_of[i]);
+    __syncthreads();
+  };
   auto arrive = [&](int key0, int buf) {  // this tile's copies have landed; the next one's leave
     wait_loads<0>();
     __syncthreads();
+    if (key0 < all_lo || key0 + KEYS - 1 > all_hi) settle(key0, buf);
     if (key0 + KEYS < u.hi) {
       stager.copy(keys + (buf ^ 1) * TL::kBytes, values + (buf ^ 1) * TL::kBytes);
       stager.find(key0 + 2 * KEYS + 32);
     }
   };
-  auto all_see = [&](int key, int n) { return key >= all_lo && key + n - 1 <= all_hi && key + n <= u.hi; };
+  auto all_see = [&](int key) { return key >= all_lo && key + 31 <= all_hi; };
+  // The block at `at` of the tile, keys from key0 on, and the scores and reference of the next one.
+  auto block = [&](int key0, int at, Scores& s, Scores& next) {
+    Tops top = run_block(at, at, s, next);
+    if (key0 + 32 >= u.hi) return;
+    if (!all_see(key0 + 32)) {
+      hide(next, key0 + 32);
+      top = largest(next);
+    }
+    refer(top);
+  };
   if (u.lo < u.hi) {  // the first block's scores, from keys in the other buffer
     stager.find(u.lo);
     stager.template copy<1>(keys + TL::kBytes, values);
@@ -406,49 +378,37 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
     wait_loads<2 * TL::kLoads>();  // the first tile's copies may be outstanding
     __syncthreads();
     score_block(TL::kBytes, s0);
-    if (!all_see(u.lo, 32)) hide(s0, u.lo);
+    if (!all_see(u.lo)) hide(s0, u.lo);
     refer(largest(s0));
   }
-  int key0 = u.lo, buf = 0;
-  while (key0 < u.hi) {
-    // the tiles that all rows see, two a round so that a buffer's address is a constant
-    while (buf == 0 && all_see(key0, 2 * KEYS) && key0 + 2 * KEYS < u.hi) {
-      Tops top;
+  if constexpr (kHalf) {  // two tiles a round, so that a buffer's address is a constant
+    for (int key0 = u.lo; key0 < u.hi; key0 += 2 * KEYS) {
       arrive(key0, 0);
+      block(key0, 0, s0, s1);
+      if (key0 + 32 >= u.hi) break;
       if constexpr (NB == 2) {
-        refer(whole_block(0, 0, s0, s1));
-        refer(whole_block(kBlock, kBlock, s1, s0));
+        block(key0 + 32, kBlock, s1, s0);
+        if (key0 + KEYS >= u.hi) break;
         arrive(key0 + KEYS, 1);
-        refer(whole_block(TL::kBytes, TL::kBytes, s0, s1));
-        top = whole_block(TL::kBytes + kBlock, TL::kBytes + kBlock, s1, s0);
+        block(key0 + KEYS, TL::kBytes, s0, s1);
+        if (key0 + KEYS + 32 >= u.hi) break;
+        block(key0 + KEYS + 32, TL::kBytes + kBlock, s1, s0);
       } else {
-        refer(whole_block(0, 0, s0, s1));
         arrive(key0 + KEYS, 1);
-        top = whole_block(TL::kBytes, TL::kBytes, s1, s0);
+        block(key0 + KEYS, TL::kBytes, s1, s0);
       }
-      key0 += 2 * KEYS;
-      if (!all_see(key0, 32)) {
-        hide(s0, key0);
-        top = largest(s0);
-      }
-      refer(top);
     }
-    arrive(key0, buf);
+  } else {  // the registers of one tile's code
+    int buf = 0;
+    for (int key0 = u.lo; key0 < u.hi; key0 += KEYS, buf ^= 1) {
+      arrive(key0, buf);
 #pragma unroll 1
-    for (int j = 0; j < NB && key0 + 32 * j < u.hi; ++j) {
-      const int key = key0 + 32 * j, at = buf * TL::kBytes + j * kBlock;
-      const bool more = key + 32 < u.hi;
-      if (more) score_block(at, s1);
-      if (key <= any_hi && key + 32 > any_lo) edge_block(key, at, s0);
-      if (more) {
-        if (!all_see(key + 32, 32)) hide(s1, key + 32);
-        refer(largest(s1));
+      for (int j = 0; j < NB && key0 + 32 * j < u.hi; ++j) {
+        block(key0 + 32 * j, buf * TL::kBytes + j * kBlock, s0, s1);
 #pragma unroll
         for (int n = 0; n < NR; ++n) s0[n] = s1[n];
       }
     }
-    key0 += KEYS;
-    buf ^= 1;
   }
 
 #pragma unroll
