@@ -115,8 +115,9 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   const int64_t rows = c->tokens * group;  // of one key head
   const int64_t most = a->max_new > 0 ? std::min<int64_t>(a->max_new, c->tokens) : c->tokens;
   p->few = most * group <= 32;
-  p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1)
-                       : sc::kLogWideRows + (elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128);
+  // 256 rows a unit read LDS less than 128, but only where they are enough to fill the GPU
+  const bool twice = elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128 && (rows >> (sc::kLogWideRows + 1)) * c->kv_heads >= kWantWide / 2;
+  p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1) : sc::kLogWideRows + twice;
   p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim);
   // sum over the sequences of ceil(rows / 2^log_rows), at most
   const int64_t tiles = (rows >> p->log_rows) + std::min<int64_t>(c->batch, c->tokens);
@@ -132,12 +133,11 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
     units = shared ? kWantFew : tiles * c->kv_heads;
     p->slots = shared ? 2 * kWantFew : 0;
   } else {
-    // A unit's keys are split where the items leave compute units idle and a chunk still outweighs the join (about 8 us): a block of
-    // 32 keys takes a workgroup some 0.4 us for bf16 heads of 128, 4 us for fp32.
+    // A unit's keys are split where the items leave compute units idle and a chunk still outweighs the join (about 7 us): a block of
+    // 32 keys takes a workgroup some 0.6 us for bf16, 4 us for fp32 heads of 128.
     const int64_t room = (int64_t)c->table_width * c->page_size, reach = a->window < 0 ? room : (int64_t)a->window + most;
-    const int blocks = elem == 2 ? 16 * 128 / std::max(64, c->head_dim) : std::max(1, 3 * 96 / c->head_dim);
-    p->min_chunk = std::max(32 * blocks, p->keys);
-    const bool split = tiles * c->kv_heads < kWantWide && std::min(room, reach) > 2 * p->min_chunk;
+    p->min_chunk = elem == 2 ? 256 : std::max(p->keys, 32 * std::max(1, 3 * 96 / c->head_dim));
+    const bool split = tiles * c->kv_heads < kWantWide && std::min(room, reach) > 3 * p->min_chunk;
     p->target = split ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
     units = (tiles + p->target) * c->kv_heads;
     p->slots = p->target ? (int)std::min<int64_t>(units, kMostRows) : 0;
