@@ -128,6 +128,17 @@ __device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {
   return ((int64_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 
+// Inclusive sum over the wave's lanes by data-parallel moves (within rows of 16 lanes, then the rows' last lanes onwards).
+__device__ __forceinline__ int scan32(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast 31 into rows 2 and 3
+  return v;
+}
+
 // A wave's view of the batch's units: lane i holds sequence i, and where its units end; sequences from the 65th on are gone through by 64s.
 template <bool SHARES>
 struct Units {
@@ -160,6 +171,7 @@ struct Units {
   }
   __device__ __forceinline__ int64_t scan(const Shape& x) const {  // inclusive, over the wave
     int64_t v = (int64_t)x.tiles * x.parts * p.kv_heads;
+    if (!__any(v >> 25)) return scan32((int)v);
     const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
