@@ -114,7 +114,14 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   const int elem = c->dtype == SKIPCONV_BF16 ? 2 : 4, group = a->q_heads / c->kv_heads;
   const int64_t rows = c->tokens * group;  // of one key head
   const int64_t most = a->max_new > 0 ? std::min<int64_t>(a->max_new, c->tokens) : c->tokens;
+  const int64_t room = (int64_t)c->table_width * c->page_size;
+  const int64_t reach = std::min(room, a->window < 0 ? room : (int64_t)a->window + most);  // keys that an item may have
+  const int few_waves = sc::few_waves_of(elem, c->head_dim);
+  const int64_t alone = 4ll * sc::few_keys_of(elem) * few_waves;  // four tiles a wave
   p->few = most * group <= 32;
+  // fp32 heads of up to 96 over short caches: the few-rows kernel's small units fill the GPU sooner (24 .. 256 tokens over 200, heads of
+  // 64: 25 -> 14 us)
+  if (elem == 4 && c->head_dim <= 96 && reach <= alone && ((rows >> (sc::kLogFewRows + 1)) + c->batch) * c->kv_heads <= 2048) p->few = true;
   // 256 rows a unit read LDS less than 128, but only where they are enough to fill the GPU
   const bool twice = elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128 && (rows >> (sc::kLogWideRows + 1)) * c->kv_heads >= kWantWide / 2;
   p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1) : sc::kLogWideRows + twice;
@@ -125,19 +132,16 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   if (p->few) {
     // Equal shares of all keys, but a workgroup an item where no item can have keys for more than four tiles a wave: then the join's
     // launch costs more than it saves.
-    const int waves = sc::few_waves_of(elem, c->head_dim);
-    const int64_t room = (int64_t)c->table_width * c->page_size, reach = a->window < 0 ? room : (int64_t)a->window + most;
-    const bool shared = std::min(room, reach) > 4ll * p->keys * waves;
+    const bool shared = reach > alone;
     p->target = shared ? kWantFew : 0;
-    p->min_chunk = 2 * waves;
+    p->min_chunk = 2 * few_waves;
     units = shared ? kWantFew : tiles * c->kv_heads;
     p->slots = shared ? 2 * kWantFew : 0;
   } else {
     // A unit's keys are split where the items leave compute units idle and a chunk still outweighs the join (about 7 us): a block of
     // 32 keys takes a workgroup some 0.6 us for bf16, 4 us for fp32 heads of 128.
-    const int64_t room = (int64_t)c->table_width * c->page_size, reach = a->window < 0 ? room : (int64_t)a->window + most;
     p->min_chunk = elem == 2 ? 256 : std::max(p->keys, 32 * std::max(1, 3 * 96 / c->head_dim));
-    const bool split = tiles * c->kv_heads < kWantWide && std::min(room, reach) > 3 * p->min_chunk;
+    const bool split = tiles * c->kv_heads < kWantWide && reach > 3 * p->min_chunk;
     p->target = split ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
     units = (tiles + p->target) * c->kv_heads;
     p->slots = p->target ? (int)std::min<int64_t>(units, kMostRows) : 0;
