@@ -486,3 +486,40 @@ def test_refusals():
         assert e.value.code == S.SKIPCONV_E_INVALID_ARG
     out, lse = cache.attend(q, A.CacheBatch(ints(0, 1)[None], ints(0, 1), ints(0)), return_lse=True)
     assert not out.any() and torch.isneginf(lse).all()
+
+
+def test_frames_of_skip_conv_layers():
+    """The example's path: Skip-Conv projections, append and attention frame by frame with a window of frames that rolls, against the
+    oracle on the layers' own activation outputs."""
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "frame_attention.py")
+    spec = importlib.util.spec_from_file_location("frame_attention", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    rng = _rng(49)
+    n, h, w, c, dim, heads, kv_heads, history = 2, 8, 12, 32, 32, 4, 2, 2
+    weights = [_stored(rng.standard_normal((k * dim, c, 1, 1)) * (2 / c) ** 0.5, "bf16")[0] for k in (heads, kv_heads, kv_heads)]
+    model = example.FrameAttention(weights, n=n, h=h, w=w, head_dim=dim, history=history, eps=0.5, block=4, page_size=32)
+    base = rng.random((n, h, w, c))
+    past = []
+    for t in range(5):
+        frame = base.copy()
+        frame[:, t:t + 3, 2 * t:2 * t + 4] = rng.random((n, min(3, h - t), 4, c))
+        out = model.step(_stored(frame, "bf16")[0])
+        q, k, v = (layer.activation().double().cpu().numpy().reshape(n * h * w, -1, dim) for layer in model.layers)
+        pos, freq = model.pos.cpu().numpy(), model.rotary.freq.cpu().double().numpy()
+        assert (pos[:, 0] == t).all()
+        turn = lambda x: torch.from_numpy(O.rotate(x, pos, freq)).bfloat16().double().numpy()  # noqa: E731
+        past.append((turn(k), v))
+        past = past[-(history + 1):]
+        keys, values = (np.concatenate([p[i].reshape(n, h * w, kv_heads, dim) for p in past], 1) for i in (0, 1))
+        length = np.full(n, keys.shape[1])
+        pages = lambda x: x.transpose(0, 2, 1, 3)  # noqa: E731  (one page a stream)
+        want = O.attend(turn(q), pages(keys), pages(values), np.arange(n)[:, None], np.arange(n + 1) * h * w, length, False, -1)
+        # keys and queries that a rounding of the turned value takes to its neighbour move a score by up to 2^-8 of each term
+        o, _, b = want
+        got = out.double().cpu().numpy().reshape(n * h * w, heads, dim)
+        bound = 2.0 ** -8 * np.abs(o) + b["weight"] * (2.0 ** -8 + np.expm1(2 * 2.0 ** -8 * b["size"])[..., None] * 2)
+        assert (np.abs(got - o) <= 1.25 * bound).all()
