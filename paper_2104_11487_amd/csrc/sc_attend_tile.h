@@ -47,22 +47,24 @@ struct Tile {
   }
 };
 
+__device__ __forceinline__ uint32_t lds_base(char* to) { return (uint32_t)uniform((int)(uintptr_t)SC_LDS(to, char)); }
+
 // Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane, without a
 // wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
 // takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register is written, and
 // the addresses are read when the instruction issues; M0, the destination's base, is set in the same statement.
 __device__ __forceinline__ void copy16(const char* base, uint32_t off, char* to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(off), "s"(base)
+               ::"s"(lds_base(to)), "v"(off), "s"(base)
                : "memory");
 }
 __device__ __forceinline__ void copy16(const char* from, char* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base(to)), "v"(from) : "memory");
 }
 
 // The same, 4 bytes a lane from each lane's own address.
 __device__ __forceinline__ void copy4(const void* from, char* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"((uint32_t)(uintptr_t)SC_LDS(to, char)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base(to)), "v"(from) : "memory");
 }
 
 // A wave's share of the copies of one tile of keys and one of values (of the keys `lag` before), in two steps, so that page

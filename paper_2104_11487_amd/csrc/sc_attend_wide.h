@@ -382,21 +382,22 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
     refer(largest(s0));
   }
   if constexpr (kHalf) {  // two tiles a round, so that a buffer's address is a constant
-    auto tile = [&](auto which, int key0) {  // false: it was the last one
-      constexpr int B = which;
-      arrive(key0, B);
-      bool more = true;
-      unrolled<NB>([&](auto index) {
-        constexpr int j = index, at = B * TL::kBytes + j * kBlock;
-        if (!more) return;
-        if constexpr ((NB == 1 ? B : j) % 2 == 0) block(key0 + 32 * j, at, s0, s1);
-        else block(key0 + 32 * j, at, s1, s0);
-        more = key0 + 32 * (j + 1) < u.hi;
-      });
-      return more;
-    };
-    for (int key0 = u.lo; key0 < u.hi; key0 += 2 * KEYS)
-      if (!tile(std::integral_constant<int, 0>{}, key0) || !tile(std::integral_constant<int, 1>{}, key0 + KEYS)) break;
+    for (int key0 = u.lo; key0 < u.hi; key0 += 2 * KEYS) {
+      arrive(key0, 0);
+      block(key0, 0, s0, s1);
+      if (key0 + 32 >= u.hi) break;
+      if constexpr (NB == 2) {
+        block(key0 + 32, kBlock, s1, s0);
+        if (key0 + KEYS >= u.hi) break;
+        arrive(key0 + KEYS, 1);
+        block(key0 + KEYS, TL::kBytes, s0, s1);
+        if (key0 + KEYS + 32 >= u.hi) break;
+        block(key0 + KEYS + 32, TL::kBytes + kBlock, s1, s0);
+      } else {
+        arrive(key0 + KEYS, 1);
+        block(key0 + KEYS, TL::kBytes, s1, s0);
+      }
+    }
   } else {  // the registers of one tile's code
     int buf = 0;
     for (int key0 = u.lo; key0 < u.hi; key0 += KEYS, buf ^= 1) {
