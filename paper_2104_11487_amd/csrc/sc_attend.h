@@ -73,8 +73,11 @@ constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel; bf16 h
 constexpr int kWideDoubleDim = 64;
 constexpr int kLogFewRows = 4;      // rows of a block of the few-rows kernel, which takes one or two
 
-// Rows of a key tile. The wide kernel's: two buffers of keys and values take 64 KB where the head allows 32 rows or more.
-inline int wide_keys_of(int elem_bytes, int dim) { return dim * elem_bytes > 256 ? 32 : 64; }
+// Rows of a key tile. The wide kernel's: two buffers of keys and values take 64 KB of a workgroup's half of LDS, or more where the head
+// allows no fewer than 32 rows; units of 128 rows get 64 at most. For those of 256 rows, which have long to go, a tile of 64 keys would
+// wait for copies twice as often (4096 tokens over 12288 of a window, heads of 64: 441 instead of 434 us); for the others the longer
+// first wait shows (12 tokens over 1500, heads of 64: 14.8 -> 16.3 us).
+constexpr int wide_keys_of(int elem_bytes, int dim, int blocks) { return dim * elem_bytes > 256 ? 32 : blocks == 2 ? 128 : 64; }
 inline int few_keys_of(int elem_bytes) { return elem_bytes == 2 ? 32 : 16; }
 int few_waves_of(int elem_bytes, int dim);  // waves of a workgroup of the few-rows kernel
 

@@ -125,7 +125,7 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   // 256 rows a unit read LDS less than 128, but only where they are enough to fill the GPU
   const bool twice = elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128 && (rows >> (sc::kLogWideRows + 1)) * c->kv_heads >= kWantWide / 2;
   p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1) : sc::kLogWideRows + twice;
-  p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim);
+  p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim, 1 + twice);
   // sum over the sequences of ceil(rows / 2^log_rows), at most
   const int64_t tiles = (rows >> p->log_rows) + std::min<int64_t>(c->batch, c->tokens);
   int64_t units;

@@ -14,7 +14,7 @@
 // more, which after the first tiles is seldom.
 //
 // Every 32 x 32 x 16 product reads a fragment of 1 KB from LDS, which at 128 bytes a cycle and 32 cycles a product on each of four SIMDs
-// is all that LDS gives; two row blocks a wave halve that (4096 tokens over 12288, heads of 64: 472 -> 426 us), but with heads of 128
+// is all that LDS gives; two row blocks a wave halve that (4096 tokens over 12288, heads of 64: 517 -> 441 us), but with heads of 128
 // they leave one wave a SIMD, whose vector work no longer runs beside its products (8192 tokens over 24576: 1522 -> 1987 us).
 #pragma once
 
@@ -26,12 +26,6 @@
 #pragma clang fp contract(off)
 
 namespace sc {
-
-// Keys of a tile: two buffers of keys and values take 64 KB where the head allows 32 rows or more of it.
-template <typename T, int DP>
-constexpr int wide_keys() {
-  return pow2_at_least(DP * (int)sizeof(T)) >= 512 ? 32 : 64;
-}
 
 constexpr int kWideWaves = 4;
 constexpr float kSlack = 8.0f;  // powers of two that an exponential may exceed one by
@@ -95,7 +89,7 @@ struct SlotPlan {
 template <typename T, int DP, int NR, bool UNI>
 __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T), DP, NR)) attend_wide_kernel(AttendParams p) {
   constexpr bool kHalf = sizeof(T) == 2;
-  constexpr int NW = kWideWaves, WROWS = 32 * NR, ROWS = WROWS * NW, KEYS = wide_keys<T, DP>();
+  constexpr int NW = kWideWaves, WROWS = 32 * NR, ROWS = WROWS * NW, KEYS = wide_keys_of((int)sizeof(T), DP, NR);
   constexpr int NB = KEYS / 32, ND = DP / 32;  // blocks of 32 keys of a tile; of 32 dimensions
   using TL = Tile<T, DP, KEYS, NW, true>;
   constexpr int QF = kHalf ? DP / 16 : DP / 8;  // 16-byte pieces of a row that a lane holds
@@ -386,7 +380,22 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
       arrive(key0, 0);
       block(key0, 0, s0, s1);
       if (key0 + 32 >= u.hi) break;
-      if constexpr (NB == 2) {
+      if constexpr (NB == 4) {
+        block(key0 + 32, kBlock, s1, s0);
+        if (key0 + 64 >= u.hi) break;
+        block(key0 + 64, 2 * kBlock, s0, s1);
+        if (key0 + 96 >= u.hi) break;
+        block(key0 + 96, 3 * kBlock, s1, s0);
+        if (key0 + KEYS >= u.hi) break;
+        arrive(key0 + KEYS, 1);
+        block(key0 + KEYS, TL::kBytes, s0, s1);
+        if (key0 + KEYS + 32 >= u.hi) break;
+        block(key0 + KEYS + 32, TL::kBytes + kBlock, s1, s0);
+        if (key0 + KEYS + 64 >= u.hi) break;
+        block(key0 + KEYS + 64, TL::kBytes + 2 * kBlock, s0, s1);
+        if (key0 + KEYS + 96 >= u.hi) break;
+        block(key0 + KEYS + 96, TL::kBytes + 3 * kBlock, s1, s0);
+      } else if constexpr (NB == 2) {
         block(key0 + 32, kBlock, s1, s0);
         if (key0 + KEYS >= u.hi) break;
         arrive(key0 + KEYS, 1);
@@ -451,7 +460,7 @@ __global__ void __launch_bounds__(64 * kWideWaves, wide_waves_per_simd(sizeof(T)
 template <typename T, int DP, int NR>
 hipError_t launch_wide(const AttendParams& p, int uniform_pages, hipStream_t stream) {
   const dim3 grid((unsigned)p.units), block(64 * kWideWaves);
-  if (p.keys != wide_keys<T, DP>()) return hipErrorInvalidValue;
+  if (p.keys != wide_keys_of((int)sizeof(T), DP, NR)) return hipErrorInvalidValue;
   if (uniform_pages) attend_wide_kernel<T, DP, NR, true><<<grid, block, 0, stream>>>(p);
   else attend_wide_kernel<T, DP, NR, false><<<grid, block, 0, stream>>>(p);
   return hipGetLastError();
