@@ -61,9 +61,9 @@ struct AttendParams {
   float scale_log2;  // scale * log2(e)
   int log_rows;      // a unit's rows (new tokens x query heads of one key head): 2^log_rows
   int keys;          // rows of a key tile: chunks are whole tiles
-  // wide kernel: units wanted per key head (0: an item's keys are never split) and fewest keys of a unit where they are;
-  // few-rows kernel: workgroups, and fewest key tiles of one
-  int target, min_chunk;
+  int target;        // workgroups that share all key tiles; 0: one an item
+  int min_chunk;     // fewest key tiles of a share
+  int slack;         // key tiles that a workgroup may have more than its equal share for the sake of taking them from one item
   int units;         // workgroups of the launch
   int slots;         // parts in the workspace, of 2^log_rows rows
 };
@@ -71,13 +71,17 @@ struct AttendParams {
 constexpr int kMostKeys = 1 << 30;  // positions of a sequence stay below it
 constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel; bf16 heads of up to kWideDoubleDim also take twice as many
 constexpr int kWideDoubleDim = 64;
-constexpr int kLogFewRows = 4;      // rows of a block of the few-rows kernel, which takes one or two
+constexpr int kLogFewRows = 4;      // rows of a unit of the few-rows kernel; fp32 heads of up to kFewDoubleDim also take twice as many
+constexpr int kFewDoubleDim = 96;
+constexpr int kFewHalfDim = 64;     // largest bf16 head of the few-rows kernel
 
 // Rows of a key tile. The wide kernel's: two buffers of keys and values take 64 KB of a workgroup's half of LDS, or more where the head
 // allows no fewer than 32 rows; units of 128 rows get 64 at most. For those of 256 rows, which have long to go, a tile of 64 keys would
 // wait for copies twice as often (4096 tokens over 12288 of a window, heads of 64: 441 instead of 434 us); for the others the longer
 // first wait shows (12 tokens over 1500, heads of 64: 14.8 -> 16.3 us).
 constexpr int wide_keys_of(int elem_bytes, int dim, int blocks) { return dim * elem_bytes > 256 ? 32 : blocks == 2 ? 128 : 64; }
+// Workgroups of the wide kernel that a compute unit holds (registers, then LDS).
+constexpr int wide_groups_of(int elem_bytes, int dim) { return (dim + 31) / 32 * 32 * elem_bytes <= (elem_bytes == 2 ? 256 : 384) ? 2 : 1; }
 inline int few_keys_of(int elem_bytes) { return elem_bytes == 2 ? 32 : 16; }
 int few_waves_of(int elem_bytes, int dim);  // waves of a workgroup of the few-rows kernel
 

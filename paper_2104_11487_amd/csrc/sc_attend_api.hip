@@ -106,7 +106,7 @@ int check_attend(const skipconv_cache* c, const skipconv_attend* a) {
 // The kernel and the cut of a launch, from the shapes alone (the lengths are on the device).
 struct Plan {
   bool few;
-  int log_rows, keys, target, min_chunk, units, slots;
+  int log_rows, keys, target, min_chunk, slack, units, slots;
   size_t part_o, part_ml;
 };
 
@@ -117,35 +117,42 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   const int64_t room = (int64_t)c->table_width * c->page_size;
   const int64_t reach = std::min(room, a->window < 0 ? room : (int64_t)a->window + most);  // keys that an item may have
   const int few_waves = sc::few_waves_of(elem, c->head_dim);
-  const int64_t alone = 4ll * sc::few_keys_of(elem) * few_waves;  // four tiles a wave
-  p->few = most * group <= 32;
-  // fp32 heads of up to 96 over short caches: the few-rows kernel's small units fill the GPU sooner (24 .. 256 tokens over 200, heads of
-  // 64: 25 -> 14 us)
-  if (elem == 4 && c->head_dim <= 96 && reach <= alone && ((rows >> (sc::kLogFewRows + 1)) + c->batch) * c->kv_heads <= 2048) p->few = true;
+  // Where no item has keys for more than four tiles a wave of the few-rows kernel, a workgroup takes one item: a join's launch would
+  // cost more than shares save.
+  const bool brief = reach <= 4ll * sc::few_keys_of(elem) * few_waves;
+  // Items of a launch with 2^log_rows rows a tile, at most.
+  const auto items = [&](int log_rows) { return ((rows >> log_rows) + std::min<int64_t>(c->batch, c->tokens)) * c->kv_heads; };
+  // The few-rows kernel. bf16 heads of more than 64 leave it four waves, and the wide kernel's two workgroups a compute unit stream as
+  // fast (one token of 64 sequences of up to 16384, heads of 128: both 227 us) and start sooner (over 3000: 62 -> 52 us). Up to 64,
+  // and fp32, which has less to gain from many rows: up to 32 rows a sequence and key head (fp32, heads of 64, one token of 19 sequences
+  // over 4016: 41 -> 23 us); where keys are brief, any number of rows that a workgroup a compute unit holds (bf16, heads of 64, 24 tokens
+  // over 300: 10.2 -> 8.2 us; fp32: 14 -> 11 us), and for fp32 heads of up to 96 with two row blocks a wave some more (172 tokens of 5
+  // sequences over 384, heads of 64: 35 -> 17 us).
+  const bool blocks2 = elem == 4 && c->head_dim <= sc::kFewDoubleDim && brief && items(sc::kLogFewRows) > kWantFew && most * group > 16;
+  p->few = (elem == 4 || c->head_dim <= sc::kFewHalfDim) &&
+           (most * group <= 32 || (brief && c->head_dim <= 128 && items(sc::kLogFewRows) <= kWantFew) || (blocks2 && items(sc::kLogFewRows + 1) <= 2048));
   // 256 rows a unit read LDS less than 128, but only where they are enough to fill the GPU
   const bool twice = elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128 && (rows >> (sc::kLogWideRows + 1)) * c->kv_heads >= kWantWide / 2;
-  p->log_rows = p->few ? (most * group <= 16 ? sc::kLogFewRows : sc::kLogFewRows + 1) : sc::kLogWideRows + twice;
+  p->log_rows = p->few ? sc::kLogFewRows + blocks2 : sc::kLogWideRows + twice;
   p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim, 1 + twice);
-  // sum over the sequences of ceil(rows / 2^log_rows), at most
-  const int64_t tiles = (rows >> p->log_rows) + std::min<int64_t>(c->batch, c->tokens);
-  int64_t units;
+  int64_t units = items(p->log_rows);
   if (p->few) {
-    // Equal shares of all keys, but a workgroup an item where no item can have keys for more than four tiles a wave: then the join's
-    // launch costs more than it saves.
-    const bool shared = reach > alone;
-    p->target = shared ? kWantFew : 0;
+    p->target = brief ? 0 : kWantFew;
     p->min_chunk = 2 * few_waves;
-    units = shared ? kWantFew : tiles * c->kv_heads;
-    p->slots = shared ? 2 * kWantFew : 0;
+    p->slack = 0;
+    p->slots = 2 * p->target;
   } else {
-    // A unit's keys are split where the items leave compute units idle and a chunk still outweighs the join (about 7 us): a block of
-    // 32 keys takes a workgroup some 0.6 us for bf16, 4 us for fp32 heads of 128.
-    p->min_chunk = elem == 2 ? 256 : std::max(p->keys, 32 * std::max(1, 3 * 96 / c->head_dim));
-    const bool split = tiles * c->kv_heads < kWantWide && reach > 3 * p->min_chunk;
-    p->target = split ? (kWantWide + c->kv_heads - 1) / c->kv_heads : 0;
-    units = (tiles + p->target) * c->kv_heads;
-    p->slots = p->target ? (int)std::min<int64_t>(units, kMostRows) : 0;
+    // Keys are shared where the items leave compute units idle and a share still outweighs the join (about 7 us): a block of 32 keys
+    // takes a workgroup some 0.6 us for bf16, 4 us for fp32 heads of 128. Ending one item and beginning another takes one about 4 us,
+    // the slack that whole units are worth (4 sequences of 12 tokens over 8000, heads of 64: 32 -> 29 us).
+    const int least = elem == 2 ? 256 : std::max(p->keys, 32 * std::max(1, 3 * 96 / c->head_dim));
+    const bool shared = units < kWantWide && reach > 3 * least;
+    p->target = shared ? 256 * sc::wide_groups_of(elem, c->head_dim) : 0;
+    p->min_chunk = least / p->keys;
+    p->slack = shared ? (elem == 2 ? 256 : 64) / p->keys : 0;
+    p->slots = 2 * p->target;
   }
+  if (p->target) units = p->target;
   if (units > kMostRows) return fail(SKIPCONV_E_UNSUPPORTED, "attend: too many rows");
   p->units = (int)units;
   const size_t parts = (size_t)p->slots << p->log_rows;
@@ -260,7 +267,7 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
   p.causal = a->causal;
   p.window = a->window < 0 ? -1 : a->window;
   p.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
-  p.log_rows = plan.log_rows, p.keys = plan.keys, p.target = plan.target, p.min_chunk = plan.min_chunk, p.units = plan.units;
+  p.log_rows = plan.log_rows, p.keys = plan.keys, p.target = plan.target, p.min_chunk = plan.min_chunk, p.slack = plan.slack, p.units = plan.units;
   p.slots = plan.slots;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e;

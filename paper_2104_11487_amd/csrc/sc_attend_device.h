@@ -82,9 +82,11 @@ __device__ __forceinline__ Sequence sequence_of(const CacheView& c, int b) {
 //
 // Rows of one key head: a sequence's n new tokens x `group` query heads, the token slowest. They are cut into tiles of 2^log_rows;
 // an item is one tile with one key head and all the keys that its rows may see. Every workgroup derives the same cut of the items'
-// keys from the lengths on the device (no host copy of them exists), by a scan over the sequences.
-//   wide kernel: an item is `parts` units, more than one where a launch's items alone would leave compute units idle;
-//   few-rows kernel: an item is as many units as it has key tiles, and each workgroup takes an equal share of all units in a row.
+// keys from the lengths on the device (no host copy of them exists), by a scan over the sequences. An item is
+//   one unit, where the launch does not share keys;
+//   else as many units as it has key tiles, of which each workgroup takes an equal share in a row, wherever that begins and ends;
+//   or units of some key tiles, one a workgroup, where that loses little to equal shares: a workgroup whose share ends inside one item
+//   and begins inside another pays twice for an item's begin and end.
 // Unit index: sequences in order; within one: key head, tile (the last one, which sees most keys under a causal mask, first), keys.
 struct Shape {
   int tiles, parts, chunk, span;  // row tiles; units of an item; keys of a unit; keys that an item may have
@@ -106,20 +108,12 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
   return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
-// The cut of a sequence: by the wide kernel's goal (keys that a unit should have; 0: nothing is split), or (SHARES) into key tiles, where
-// those are shared. A span begins anywhere, the first tile at a whole one.
-template <bool SHARES>
-__device__ __forceinline__ Shape cut_of(const AttendParams& p, const Sequence& s, int goal) {
+// The cut of a sequence: into key tiles where keys are shared. A span begins anywhere, the first tile at a whole one.
+__device__ __forceinline__ Shape cut_of(const AttendParams& p, const Sequence& s) {
   Shape o = shape_of(p, s);
-  const uint32_t most = (uint32_t)o.span + (uint32_t)p.keys - 1;
-  if constexpr (SHARES) {
-    if (p.target > 0 && o.tiles > 0) {
-      o.parts = max(1, (int)((most + p.keys - 1) / (uint32_t)p.keys));
-      o.chunk = p.keys;
-    }
-  } else if (goal > 0 && o.tiles > 0 && o.span > goal) {
-    o.parts = (int)((uint32_t)(o.span + goal - 1) / (uint32_t)goal);
-    o.chunk = (int)(((most + o.parts - 1) / (uint32_t)o.parts + p.keys - 1) & ~(uint32_t)(p.keys - 1));
+  if (p.target > 0 && o.tiles > 0) {
+    o.parts = max(1, (int)(((uint32_t)o.span + 2 * (uint32_t)p.keys - 2) / (uint32_t)p.keys));
+    o.chunk = p.keys;
   }
   return o;
 }
@@ -140,30 +134,36 @@ __device__ __forceinline__ int scan32(int v) {
 }
 
 // A wave's view of the batch's units: lane i holds sequence i, and where its units end; sequences from the 65th on are gone through by 64s.
-template <bool SHARES>
 struct Units {
   const AttendParams& p;
   Sequence s;
   Shape o;
   int64_t upto, all;  // units of the sequences up to the lane's; of the batch
-  int goal;
+  bool single;        // a workgroup takes one unit
 
-  __device__ __forceinline__ explicit Units(const AttendParams& q) : p(q), goal(0) {
+  __device__ __forceinline__ explicit Units(const AttendParams& q) : p(q), single(q.target == 0) {
     s = load(0);
-    if constexpr (!SHARES) {
-      if (p.target > 0) {
-        Shape x = shape_of(p, s);
-        int64_t total = (int64_t)x.tiles * x.span;
-        for (int b0 = 64; b0 < p.c.batch; b0 += 64) x = shape_of(p, load(b0)), total += (int64_t)x.tiles * x.span;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-        goal = max(p.min_chunk, (int)min(ceil((double)total / (double)p.target), (double)kMostKeys));
-      }
-    }
-    o = cut_of<SHARES>(p, s, goal);
+    o = cut_of(p, s);
     upto = scan(o);
     all = from_lane(upto, 63);
-    for (int b0 = 64; b0 < p.c.batch; b0 += 64) all += from_lane(scan(cut_of<SHARES>(p, load(b0), goal)), 63);
+    for (int b0 = 64; b0 < p.c.batch; b0 += 64) all += from_lane(scan(cut_of(p, load(b0))), 63);
+    if (p.slack > 0 && p.c.batch <= 64 && all < (1 << 24)) whole_units();
+  }
+  // Looks for the least number of key tiles a unit at which the units are no more than the workgroups, from equal shares' up to `slack` more.
+  __device__ __forceinline__ void whole_units() {
+    const int items = o.tiles * p.kv_heads, least = max(p.min_chunk, (int)(((uint32_t)all + p.target - 1) / (uint32_t)p.target));
+    int each = least;
+#pragma unroll 1
+    for (int i = 0; i < 3 && each <= least + p.slack; ++i) {
+      const int parts = (int)(((uint32_t)o.parts + each - 1) / (uint32_t)each);
+      const int sum = scan32(items * parts), n = __builtin_amdgcn_readlane(sum, 63);
+      if (n <= p.target) {
+        o.parts = parts, o.chunk = (int)min((int64_t)each * p.keys, (int64_t)kMostKeys);
+        upto = sum, all = n, single = true;
+        return;
+      }
+      each = max(each + 1, (int)(((uint32_t)each * (uint32_t)n + p.target - 1) / (uint32_t)p.target));
+    }
   }
   __device__ __forceinline__ Sequence load(int b0) const {
     const int b = b0 + (threadIdx.x & 63);
@@ -186,7 +186,7 @@ struct Units {
     int64_t base = 0;
     for (int b0 = 0; b0 < p.c.batch; b0 += 64) {
       const Sequence x = b0 ? load(b0) : s;
-      const Shape y = b0 ? cut_of<SHARES>(p, x, goal) : o;
+      const Shape y = b0 ? cut_of(p, x) : o;
       const int64_t end = b0 ? scan(y) : upto;
       const uint64_t past = __ballot(by_row ? at >= x.start && at < x.start + x.n : base + end > at);
       if (past) {
@@ -207,24 +207,26 @@ struct Units {
   }
 };
 
-// Shares of the few-rows kernel: workgroup w of n takes the units [at(w), at(w + 1)) of `all`, the first `rest` workgroups one more than the
-// others; one unit each where items are not shared.
+// Workgroup w of n takes the units [at(w), at(w + 1)) of `all`, the first `rest` workgroups one more than the others; one each where a
+// workgroup takes one.
 struct Shares {
   int64_t all, each;
   int n, rest;
-  __device__ __forceinline__ int64_t at(int w) const { return w * each + min(w, rest); }
+  bool single;
+  __device__ __forceinline__ int64_t at(int w) const { return single ? w : w * each + min(w, rest); }
   __device__ __forceinline__ int holder(int64_t unit) const {
+    if (__builtin_expect(single, 1)) return (int)unit;
     const int64_t larger = rest * (each + 1);
     return unit < larger ? (int)divide(unit, each + 1) : rest + (int)divide(unit - larger, each);
   }
 };
-__device__ __forceinline__ Shares shares_of(const AttendParams& p, int64_t all) {
-  Shares s;
-  s.all = all;
-  const int64_t most = divide(all, max(1, p.min_chunk));
-  s.n = p.target > 0 ? (int)max((int64_t)1, min((int64_t)p.target, most)) : (int)min(max(all, (int64_t)1), (int64_t)p.units);
-  s.each = divide(all, s.n);
-  s.rest = (int)(all - s.each * s.n);
+__device__ __forceinline__ Shares shares_of(const Units& units) {
+  Shares s = {units.all, 1, (int)min(units.all, (int64_t)units.p.units), 0, units.single};
+  if (__builtin_expect(!units.single, 0)) {
+    s.n = (int)max((int64_t)1, min((int64_t)units.p.target, divide(s.all, max(1, units.p.min_chunk))));
+    s.each = divide(s.all, s.n);
+    s.rest = (int)(s.all - s.each * s.n);
+  }
   return s;
 }
 
@@ -249,8 +251,7 @@ __device__ __forceinline__ void enter_item(const AttendParams& p, Unit* u) {
   u->lo = (int)min(from, (int64_t)kMostKeys);
 }
 
-template <bool SHARES>
-__device__ __forceinline__ bool unit_of(const Units<SHARES>& units, int64_t at, Unit* u) {
+__device__ __forceinline__ bool unit_of(const Units& units, int64_t at, Unit* u) {
   const AttendParams& p = units.p;
   Sequence s;
   Shape o;
@@ -267,7 +268,7 @@ __device__ __forceinline__ bool unit_of(const Units<SHARES>& units, int64_t at, 
 }
 
 // The item after u's, at index `at`: another tile or head of the sequence, or another sequence's first.
-__device__ __forceinline__ bool next_item(const Units<true>& units, int64_t at, Unit* u) {
+__device__ __forceinline__ bool next_item(const Units& units, int64_t at, Unit* u) {
   if (++u->tile == u->tiles) u->tile = 0, ++u->head;
   if (u->head == units.p.kv_heads) return unit_of(units, at, u);
   u->part = 0;

@@ -1,12 +1,18 @@
-// Attention over the paged cache for few rows (the next token of each sequence, or a few of them): the cache's bytes bound it.
+// Attention over the paged cache for few rows of a key head (the next token of each sequence, or a few of them) or brief keys:
+// the cache's bytes bound it where those are many, the launch and the loads' latency where they are not. Measured: fp32 heads of 32,
+// one token of 103 sequences over 7959: 92 us, 4.6 TB/s; bf16 heads of 64, one token over 777 keys: 9.8 us.
 //
-// One workgroup a compute unit; each takes an equal share of all the key tiles of the launch, from wherever in an item its share
-// begins to wherever in a later one it ends, so that sequences of all lengths end together. For the keys of one item, each wave
+// One workgroup a compute unit. Where no item has keys for more than four tiles a wave it takes one item; otherwise each takes an
+// equal share of all the key tiles of the launch, from wherever in an item its share begins to wherever in a later one it ends, so that
+// sequences of all lengths end together. For the keys of one item, each wave
 // walks key tiles of its own (every n-th) with its own buffers in LDS and its own running reference and sum, so the loop has no barrier:
 // while a tile is in the products the next one's copies are in flight, and the copies after that leave as soon as its buffer is
 // free. At the item's end the waves' outputs are joined in LDS, in wave order; an item that several workgroups shared is joined by a
 // second launch, in the order of its keys.
-// Products as in the wide kernel (sc_attend_wide.h), transposed, on 16 x 16 tiles.
+// Products as in the wide kernel (sc_attend_wide.h), transposed, on 16 x 16 tiles: 16 rows a unit. A second row block in the same wave
+// (NB) reads keys once for 32 rows but doubles the registers and the vector work behind each tile; two units side by side find the
+// second reading in the caches (bf16 heads of 64, 4 tokens of 8 rows over 12000: 33 us with two blocks, 25 with one), so it is
+// left to fp32 heads of up to 96 over brief keys, where it saves rounds of workgroups.
 #pragma once
 
 #include <type_traits>
@@ -38,13 +44,14 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
   constexpr int kBuffers = NW * kWaveBytes, kJoin = NW * ROWS * (JP + 2) * 4;
   __shared__ alignas(16) char lds[kBuffers > kJoin ? kBuffers : kJoin];
 
-  const Units<true> batch(p);
-  const Shares shares = shares_of(p, batch.all);
+  const Units batch(p);
+  const Shares shares = shares_of(batch);
   if ((int)blockIdx.x >= shares.n) return;
   const int64_t end = shares.at(blockIdx.x + 1);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
   const int col = lane & 15, quad = lane >> 4, chunks = p.dim / TL::kElems;
   char* mine = lds + wave * kWaveBytes;
+  const uint32_t mine_at = (uint32_t)(uintptr_t)SC_LDS(lds, char) + wave * kWaveBytes;
 
   const int64_t first_unit = shares.at(blockIdx.x);
   Unit u;
@@ -66,15 +73,16 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
     const int count = begin < u.hi ? (u.hi - begin + kStep - 1) / kStep : 0;  // tiles of this wave
     // Page numbers are looked up three tiles ahead, copies run two tiles ahead.
     const LoneStager<T, TL, KEYS> stager(p, u, lane, chunks);
-    char* const entries = mine + 4 * TL::kBytes;
+    const char* const entries = mine + 4 * TL::kBytes;
+    const uint32_t entries_at = mine_at + 4 * TL::kBytes;
     if (count > 0) {
-      stager.find(begin, entries);
-      if (count > 1) stager.find(begin + kStep, entries + 256);
+      stager.find(begin, entries_at);
+      if (count > 1) stager.find(begin + kStep, entries_at + 256);
       wait_loads<0>();
-      stager.copy(begin, entries, mine, mine + TL::kBytes);
+      stager.copy(begin, entries, mine_at, mine_at + TL::kBytes);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (count > 2) stager.find(begin + 2 * kStep, entries);
-      if (count > 1) stager.copy(begin + kStep, entries + 256, mine + 2 * TL::kBytes, mine + 3 * TL::kBytes);
+      if (count > 2) stager.find(begin + 2 * kStep, entries_at);
+      if (count > 1) stager.copy(begin + kStep, entries + 256, mine_at + 2 * TL::kBytes, mine_at + 3 * TL::kBytes);
     }
 
     // the rows' queries, in the operand's layout
@@ -244,8 +252,9 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
 
     for (int it = 0; it < count; ++it) {
       const int key0 = begin + it * kStep;
-      char* kt = mine + (it & 1) * 2 * TL::kBytes;
-      char* vt = kt + TL::kBytes;
+      const int tile_at = (it & 1) * 2 * TL::kBytes;
+      const char* const kt = mine + tile_at;
+      const char* const vt = kt + TL::kBytes;
       if (it + 1 < count) wait_loads<LoneStager<T, TL, KEYS>::kOps>();  // the younger tile's copies stay in flight
       else wait_loads<0>();
       if (key0 >= all_lo && key0 + KEYS - 1 <= all_hi) tile(std::false_type{}, key0, kt, vt);
@@ -253,8 +262,8 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
       // this tile's buffers are free: the fragments read from them have reached their products
       if (it + 2 < count) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (it + 3 < count) stager.find(key0 + 3 * kStep, entries + ((it + 1) & 1) * 256);
-        stager.copy(key0 + 2 * kStep, entries + (it & 1) * 256, kt, vt);
+        if (it + 3 < count) stager.find(key0 + 3 * kStep, entries_at + ((it + 1) & 1) * 256);
+        stager.copy(key0 + 2 * kStep, entries + (it & 1) * 256, mine_at + tile_at, mine_at + tile_at + TL::kBytes);
       }
     }
 
@@ -310,21 +319,31 @@ __global__ void __launch_bounds__((64 * few_waves<T, DP>())) attend_few_kernel(A
 template <typename T, int DP>
 hipError_t launch_few(const AttendParams& p, hipStream_t stream) {
   const dim3 grid((unsigned)p.units), block(64 * few_waves<T, DP>());
-  if (p.keys != (sizeof(T) == 2 ? 32 : 16)) return hipErrorInvalidValue;
-  if (p.log_rows == kLogFewRows) attend_few_kernel<T, DP, 1><<<grid, block, 0, stream>>>(p);
-  else if (p.log_rows == kLogFewRows + 1) attend_few_kernel<T, DP, 2><<<grid, block, 0, stream>>>(p);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  if (p.keys != few_keys_of((int)sizeof(T))) return hipErrorInvalidValue;
+  if (p.log_rows == kLogFewRows) {
+    attend_few_kernel<T, DP, 1><<<grid, block, 0, stream>>>(p);
+    return hipGetLastError();
+  }
+  if constexpr (sizeof(T) == 4 && DP <= kFewDoubleDim) {
+    if (p.log_rows == kLogFewRows + 1) {
+      attend_few_kernel<T, DP, 2><<<grid, block, 0, stream>>>(p);
+      return hipGetLastError();
+    }
+  }
+  return hipErrorInvalidValue;
 }
 
 template <typename T>
 hipError_t launch_few_dim(const AttendParams& p, hipStream_t stream) {
   if (p.dim <= 32) return launch_few<T, 32>(p, stream);
   if (p.dim <= 64) return launch_few<T, 64>(p, stream);
-  if (p.dim <= 96) return launch_few<T, 96>(p, stream);
-  if (p.dim <= 128) return launch_few<T, 128>(p, stream);
-  if (p.dim <= 192) return launch_few<T, 192>(p, stream);
-  return launch_few<T, 256>(p, stream);
+  if constexpr (sizeof(T) == 4) {
+    if (p.dim <= 96) return launch_few<T, 96>(p, stream);
+    if (p.dim <= 128) return launch_few<T, 128>(p, stream);
+    if (p.dim <= 192) return launch_few<T, 192>(p, stream);
+    return launch_few<T, 256>(p, stream);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace sc

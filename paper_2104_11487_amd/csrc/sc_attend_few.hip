@@ -12,27 +12,20 @@ constexpr int kJoinWaves = 4;
 // Where a row's parts lie in the workspace.
 struct Parts {
   int64_t slot0;
-  int count, step, skip, in_tile;
-  __device__ __forceinline__ int64_t at(int i, int log_rows) const { return ((slot0 + (int64_t)i * step + (i == 0 ? skip : 0)) << log_rows) + in_tile; }
+  int count, skip, in_tile;
+  __device__ __forceinline__ int64_t at(int i, int log_rows) const { return ((slot0 + 2 * (int64_t)i + (i == 0 ? skip : 0)) << log_rows) + in_tile; }
 };
 
 // The parts of row (token, query head h), of which the sequence and its cut are known; count 0: the row was not split.
-// SHARES: the parts of the few-rows kernel, otherwise those of the wide kernel.
-template <bool SHARES>
-__device__ __forceinline__ Parts parts_of(const AttendParams& p, const Units<SHARES>& units, const Sequence& s, const Shape& o, int64_t first, int token, int h) {
+__device__ __forceinline__ Parts parts_of(const AttendParams& p, const Units& units, const Sequence& s, const Shape& o, int64_t first, int token, int h) {
   const int head = h / p.group, row = (token - s.start) * p.group + (h - head * p.group), tile = row >> p.log_rows;
   const int64_t unit = first + ((int64_t)head * o.tiles + (o.tiles - 1 - tile)) * o.parts;
-  Parts r = {unit, o.parts, 1, 0, row - (tile << p.log_rows)};
-  if constexpr (SHARES) {
-    // workgroups w0 .. w1 held the item's units; each one's part is its first (slot 2 w), but where the share began before the item,
-    // which only the first of them can, its last (2 w + 1)
-    const Shares all = shares_of(p, units.all);
-    const int w0 = all.holder(unit), w1 = all.holder(unit + o.parts - 1);
-    r.count = w1 - w0 + 1, r.step = 2;
-    r.slot0 = 2 * (int64_t)w0;
-    r.skip = all.at(w0) < unit ? 1 : 0;
-  }
-  if (r.count <= 1 || r.slot0 + (int64_t)r.count * r.step > p.slots) r.count = 0;
+  // workgroups w0 .. w1 held the item's units; each one's part is its first (slot 2 w), but where the share began before the item,
+  // which only the first of them can, its last (2 w + 1)
+  const Shares all = shares_of(units);
+  const int w0 = all.holder(unit), w1 = all.holder(unit + o.parts - 1);
+  Parts r = {2 * (int64_t)w0, w1 - w0 + 1, all.at(w0) < unit ? 1 : 0, row - (tile << p.log_rows)};
+  if (r.count <= 1 || r.slot0 + 2 * (int64_t)r.count > p.slots) r.count = 0;
   return r;
 }
 
@@ -47,13 +40,13 @@ __device__ __forceinline__ void store_row(const AttendParams& p, int token, int 
 }
 
 // Many rows: each takes `width` lanes (dim / 4, a power of two), which go through its parts in the order of their keys.
-template <typename T, bool SHARES>
+template <typename T>
 __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_rows_kernel(AttendParams p, int width) {
-  const Units<SHARES> units(p);
+  const Units units(p);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), mine = lane / width, e = (lane - mine * width) * 4;
   const int rows = 64 / width, all = p.c.tokens * p.q_heads;
   const int row0 = ((int)blockIdx.x * kJoinWaves + wave) * rows;
-  Parts parts = {0, 0, 1, 0, 0};
+  Parts parts = {0, 0, 0, 0};
   Sequence s;
   Shape o;
   int64_t first = 0;
@@ -87,7 +80,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_rows_kernel(Atten
 
 // Few rows, one a workgroup: the parts' weights go to LDS, 256 at a time; the parts are dealt to groups of `width` lanes, whose
 // shares are then added in order.
-template <typename T, bool SHARES>
+template <typename T>
 __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendParams p, int width) {
   constexpr int kThreads = 64 * kJoinWaves;
   __shared__ floatx4 shares[kThreads];
@@ -97,7 +90,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   Sequence s;
   Shape o;
   int64_t first;
-  const Units<SHARES> units(p);
+  const Units units(p);
   if (!units.find(token, true, &b, &s, &o, &first)) return;
   const Parts parts = parts_of(p, units, s, o, first, token, h);
   if (parts.count == 0) return;
@@ -151,7 +144,7 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   store_row<T>(p, token, h, e, v, top, total);
 }
 
-template <typename T, bool SHARES>
+template <typename T>
 void launch_join(const AttendParams& p, hipStream_t stream) {
   const int rows = p.c.tokens * p.q_heads;
   int width = 8;
@@ -159,10 +152,10 @@ void launch_join(const AttendParams& p, hipStream_t stream) {
   // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 128 parts); then lane groups, of
   // which many rows of few parts need no exchange.
   if (rows < 512) {
-    attend_join_kernel<T, SHARES><<<dim3((unsigned)rows), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
+    attend_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
   } else {
     const int each = kJoinWaves * (64 / width);
-    attend_join_rows_kernel<T, SHARES><<<dim3((unsigned)((rows + each - 1) / each)), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
+    attend_join_rows_kernel<T><<<dim3((unsigned)((rows + each - 1) / each)), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
   }
 }
 
@@ -176,14 +169,8 @@ int few_waves_of(int elem_bytes, int dim) {
 hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream) { return launch_few_dim<uint16_t>(p, stream); }
 
 hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream) {
-  const bool shares = p.log_rows < kLogWideRows;
-  if (elem_bytes == 2) {
-    if (shares) launch_join<uint16_t, true>(p, stream);
-    else launch_join<uint16_t, false>(p, stream);
-  } else {
-    if (shares) launch_join<float, true>(p, stream);
-    else launch_join<float, false>(p, stream);
-  }
+  if (elem_bytes == 2) launch_join<uint16_t>(p, stream);
+  else launch_join<float>(p, stream);
   return hipGetLastError();
 }
 

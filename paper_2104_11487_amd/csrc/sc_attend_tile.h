@@ -19,6 +19,7 @@ constexpr int pow2_at_least(int v) {
   return p;
 }
 
+// The LDS address of what a pointer to a __shared__ array names.
 #define SC_LDS(ptr, type) ((__attribute__((address_space(3))) type*)(ptr))
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
@@ -47,24 +48,22 @@ struct Tile {
   }
 };
 
-__device__ __forceinline__ uint32_t lds_base(char* to) { return (uint32_t)uniform((int)(uintptr_t)SC_LDS(to, char)); }
-
-// Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane, without a
+// Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane (alike in all lanes), without a
 // wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
 // takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register is written, and
 // the addresses are read when the instruction issues; M0, the destination's base, is set in the same statement.
-__device__ __forceinline__ void copy16(const char* base, uint32_t off, char* to) {
+__device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               ::"s"(lds_base(to)), "v"(off), "s"(base)
+               ::"s"(uniform((int)to)), "v"(off), "s"(base)
                : "memory");
 }
-__device__ __forceinline__ void copy16(const char* from, char* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_base(to)), "v"(from) : "memory");
+__device__ __forceinline__ void copy16(const char* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory");
 }
 
 // The same, 4 bytes a lane from each lane's own address.
-__device__ __forceinline__ void copy4(const void* from, char* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_base(to)), "v"(from) : "memory");
+__device__ __forceinline__ void copy4(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory");
 }
 
 // A wave's share of the copies of one tile of keys and one of values (of the keys `lag` before), in two steps, so that page
@@ -113,7 +112,7 @@ struct Stager {
 
   // FULL: the head fills its chunks, so every lane copies. PARTS: 1 keys, 2 values, 3 both.
   template <bool FULL, int PARTS>
-  __device__ __forceinline__ void copy_rows(char* keys, char* values) const {
+  __device__ __forceinline__ void copy_rows(uint32_t keys, uint32_t values) const {
     uint64_t row0 = 0;
     if constexpr (UNI) row0 = (uint64_t)base + (uint64_t)(uint32_t)page_of_entry(c, entry[0]) * page_bytes + (uint64_t)(uint32_t)slot[0] * slot_bytes;
     const int lo = (int)(uint32_t)row0, hi = (int)(uint32_t)(row0 >> 32);
@@ -123,7 +122,7 @@ struct Stager {
       const bool val = i >= TL::kLoads;
       if (!(PARTS & (val ? 2 : 1))) continue;
       const int64_t slot_stride = val ? c.v_slot : c.k_slot, page_stride = val ? c.v_page : c.k_page;
-      char* to = (val ? values : keys) + (t * NW + wave) * 1024;
+      const uint32_t to = (val ? values : keys) + (t * NW + wave) * 1024;
       if constexpr (UNI) {
         const uint64_t first = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32) | (uint32_t)__builtin_amdgcn_readlane(lo, i);
         const uint32_t off = (uint32_t)((lane / TL::kChunks) * (int)slot_stride * (int)sizeof(T) + chunk_of(t) * 16);
@@ -135,7 +134,7 @@ struct Stager {
     }
   }
   template <int PARTS = 3>
-  __device__ __forceinline__ void copy(char* keys, char* values) const {
+  __device__ __forceinline__ void copy(uint32_t keys, uint32_t values) const {
     if (chunks == TL::kChunks) copy_rows<true, PARTS>(keys, values);
     else copy_rows<false, PARTS>(keys, values);
   }
@@ -155,10 +154,10 @@ struct LoneStager {
       : c(p.c), b(u.b), lane(l), chunks(n), kb(c.k + (int64_t)u.head * c.k_head * (int64_t)sizeof(T)),
         vb(c.v + (int64_t)u.head * c.v_head * (int64_t)sizeof(T)) {}
 
-  __device__ __forceinline__ void find(int key0, char* entries) const {
+  __device__ __forceinline__ void find(int key0, uint32_t entries) const {
     copy4(c.table + (int64_t)b * c.width + min(page_of(c, key0 + (lane & (KEYS - 1))), c.width - 1), entries);
   }
-  __device__ __forceinline__ void copy(int key0, const char* entries, char* keys, char* values) const {
+  __device__ __forceinline__ void copy(int key0, const char* entries, uint32_t keys, uint32_t values) const {
     const char* from[2 * TL::kLoads];
 #pragma unroll
     for (int t = 0; t < TL::kLoads; ++t) {
