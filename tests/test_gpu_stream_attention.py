@@ -391,6 +391,25 @@ def test_keys_split_over_workgroups(dtype, new, kv):
             _compare(out, lse, want, dtype, 64)
 
 
+@pytest.mark.parametrize("case", [(90, 1, 1500, 4, 2, 128, "bf16"), (70, 9, 1200, 6, 3, 80, "bf16"), (70, 2, 900, 8, 2, 256, "bf16"), (100, 1, 1300, 2, 1, 32, "bf16"),
+                                  (20, 5, 2500, 4, 4, 96, "bf16"), (66, 17, 500, 4, 2, 64, "f32"), (70, 12, 400, 3, 1, 256, "f32"), (70, 2, 700, 4, 2, 128, "f32"),
+                                  (2, 1000, 1000, 64, 8, 32, "bf16")], ids=lambda c: "-".join(map(str, c)))
+def test_keys_shared_by_workgroups(case):
+    """Sequences of all lengths, some empty, none of which has a whole number of shares: a workgroup's keys begin and end inside them."""
+    count, new, kv, heads, kv_heads, dim, dtype = case
+    rng = _rng(46 + count + dim)
+    lens = [(new, kv), (0, 5), (min(new, 3), 3)]
+    while len(lens) < count + 1:
+        n = int(rng.integers(0, new + 1))
+        lens.append((n, int(rng.integers(n, kv + 1))))
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, kv_heads, dim, 16, dtype)
+    for mask in ((True, -1), (False, kv // 2)):
+        want = O.attend(q64, k64, v64, table, starts, length, *mask)
+        for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+            say(f"[shares] {case} mask={mask} max_new={hint}")
+            _compare(out, lse, want, dtype, dim)
+
+
 def test_scale_strides_and_out():
     rng = _rng(45)
     cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(20, 90), (3, 64)], 4, 2, 64, 16, "bf16")
