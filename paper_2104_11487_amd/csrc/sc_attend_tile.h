@@ -48,8 +48,8 @@ struct Tile {
   }
 };
 
-// Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane (alike in all lanes), without a
-// wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
+// Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane (`to` alike
+// in all lanes), without a wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
 // takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register is written, and
 // the addresses are read when the instruction issues; M0, the destination's base, is set in the same statement.
 __device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t to) {
@@ -72,7 +72,7 @@ __device__ __forceinline__ void copy4(const void* from, uint32_t to) {
 // UNI: the rows of each load lie in one page (page sizes that are a multiple of kGroup). Then lane i finds the address of
 // load i's first row (keys, then values), all loads in one go, and the copies take it as their scalar base: their
 // lanes' offsets to it never change. Otherwise each lane finds its own row's.
-template <typename T, typename TL, int NW, bool UNI, int LAG = 0>
+template <typename T, typename TL, int NW, bool UNI, int LAG>
 struct Stager {
   const CacheView& c;
   const int b, lane, wave, chunks;
@@ -80,7 +80,7 @@ struct Stager {
   const char* vb;
   const char* base;                   // UNI: those of this lane's load
   uint32_t page_bytes, slot_bytes;
-  static constexpr int kFound = UNI ? 1 : LAG ? 2 * TL::kLoads : TL::kLoads;  // rows that a lane looks up
+  static constexpr int kFound = UNI ? 1 : 2 * TL::kLoads;  // rows that a lane looks up
   int entry[kFound], slot[kFound];
 
   __device__ __forceinline__ Stager(const AttendParams& p, const Unit& u, int w, int l, int n)
@@ -128,7 +128,7 @@ struct Stager {
         const uint32_t off = (uint32_t)((lane / TL::kChunks) * (int)slot_stride * (int)sizeof(T) + chunk_of(t) * 16);
         if (FULL || chunk_of(t) < chunks) copy16(reinterpret_cast<const char*>(first), off, to);
       } else {
-        const char* from = (val ? vb : kb) + ((int64_t)page_of_entry(c, entry[i % kFound]) * page_stride + (int64_t)slot[i % kFound] * slot_stride) * (int64_t)sizeof(T) + chunk_of(t) * 16;
+        const char* from = (val ? vb : kb) + ((int64_t)page_of_entry(c, entry[i]) * page_stride + (int64_t)slot[i] * slot_stride) * (int64_t)sizeof(T) + chunk_of(t) * 16;
         if (FULL || chunk_of(t) < chunks) copy16(from, to);
       }
     }
