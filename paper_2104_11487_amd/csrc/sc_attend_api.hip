@@ -122,8 +122,8 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   const bool brief = reach <= 4ll * sc::few_keys_of(elem) * few_waves;
   // Items of a launch with 2^log_rows rows a tile, at most.
   const auto items = [&](int log_rows) { return ((rows >> log_rows) + std::min<int64_t>(c->batch, c->tokens)) * c->kv_heads; };
-  // The few-rows kernel. bf16 heads of more than 64 leave it four waves, and the wide kernel's two workgroups a compute unit stream as
-  // fast (one token of 64 sequences of up to 16384, heads of 128: both 227 us) and start sooner (over 3000: 62 -> 52 us). Up to 64,
+  // The few-rows kernel. bf16 heads of more than 64 leave it four waves, and the wide kernel's two workgroups a compute unit stream
+  // faster (one token of 64 sequences of up to 16384, heads of 128: 226 -> 220 us) and start sooner (over 3000: 69 -> 52 us). Up to 64,
   // and fp32, which has less to gain from many rows: up to 32 rows a sequence and key head (fp32, heads of 64, one token of 19 sequences
   // over 4016: 41 -> 23 us); where keys are brief, any number of rows that a workgroup a compute unit holds (bf16, heads of 64, 24 tokens
   // over 300: 10.2 -> 8.2 us; fp32: 14 -> 11 us), and for fp32 heads of up to 96 with two row blocks a wave some more (172 tokens of 5
