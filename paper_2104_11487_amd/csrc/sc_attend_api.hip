@@ -128,9 +128,12 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   // over 4016: 41 -> 23 us); where keys are brief, any number of rows that a workgroup a compute unit holds (bf16, heads of 64, 24 tokens
   // over 300: 10.2 -> 8.2 us; fp32: 14 -> 11 us), and for fp32 heads of up to 96 with two row blocks a wave some more (172 tokens of 5
   // sequences over 384, heads of 64: 35 -> 17 us).
+  // But bf16 items that take a second round of workgroups for a few tiles each fit the wide kernel's compute units at once (one token of
+  // 39 sequences of up to 218, 8 heads of 64: 13.7 -> 9.5 us).
+  const bool second_round = elem == 2 && reach <= 256 && items(sc::kLogFewRows) > kWantFew;
   const bool blocks2 = elem == 4 && c->head_dim <= sc::kFewDoubleDim && brief && items(sc::kLogFewRows) > kWantFew && most * group > 16;
   p->few = (elem == 4 || c->head_dim <= sc::kFewHalfDim) &&
-           (most * group <= 32 || (brief && c->head_dim <= 128 && items(sc::kLogFewRows) <= kWantFew) || (blocks2 && items(sc::kLogFewRows + 1) <= 2048));
+           ((most * group <= 32 && !second_round) || (brief && c->head_dim <= 128 && items(sc::kLogFewRows) <= kWantFew) || (blocks2 && items(sc::kLogFewRows + 1) <= 2048));
   // 256 rows a unit read LDS less than 128, but only where they are enough to fill the GPU
   const bool twice = elem == 2 && c->head_dim <= sc::kWideDoubleDim && most * group > 128 && (rows >> (sc::kLogWideRows + 1)) * c->kv_heads >= kWantWide / 2;
   p->log_rows = p->few ? sc::kLogFewRows + blocks2 : sc::kLogWideRows + twice;
