@@ -72,6 +72,7 @@ constexpr int kMostKeys = 1 << 30;  // positions of a sequence stay below it
 constexpr int kLogWideRows = 7;     // rows of a unit of the wide kernel; bf16 heads of up to kWideDoubleDim also take twice as many
 constexpr int kWideDoubleDim = 64;
 constexpr int kLogFewRows = 4;      // rows of a unit of the few-rows kernel; fp32 heads of up to kFewDoubleDim also take twice as many
+constexpr int kMostShared = 512;    // workgroups that share a launch's keys, at most
 constexpr int kFewDoubleDim = 96;
 constexpr int kFewHalfDim = 64;     // largest bf16 head of the few-rows kernel
 

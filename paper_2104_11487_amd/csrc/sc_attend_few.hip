@@ -7,7 +7,11 @@ namespace sc {
 
 namespace {
 
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 4;  // waves of a workgroup that joins many rows
+// Of one that joins a row: a thread for each of its parts, which are no more than the workgroups that share keys. 16 waves start later
+// (one token over 262141, heads of 128: 61 instead of 62 us, but over 4000 16.4 instead of 15.1).
+constexpr int kRowWaves = 8;
+static_assert(64 * kRowWaves >= kMostShared, "a thread a part");
 
 // Where a row's parts lie in the workspace.
 struct Parts {
@@ -78,13 +82,13 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_rows_kernel(Atten
   store_row<T>(p, token, row0 + mine - token * p.q_heads, e, v, top, total);
 }
 
-// Few rows, one a workgroup: the parts' weights go to LDS, 256 at a time; the parts are dealt to groups of `width` lanes, whose
-// shares are then added in order.
+// Few rows, one a workgroup: its parts are dealt to groups of `width` lanes, which load their first ones before the weights are known.
+// Their shares are added in a fixed order, within each wave and then over the waves.
 template <typename T>
-__global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendParams p, int width) {
-  constexpr int kThreads = 64 * kJoinWaves;
+__global__ void __launch_bounds__(64 * kRowWaves) attend_join_kernel(AttendParams p, int width) {
+  constexpr int kThreads = 64 * kRowWaves, kHeld = 8;
   __shared__ floatx4 shares[kThreads];
-  __shared__ float weights[kThreads], tops[kJoinWaves], sums[kJoinWaves];
+  __shared__ float weights[kThreads], tops[kRowWaves], sums[kRowWaves];
   const int token = (int)blockIdx.x / p.q_heads, h = (int)blockIdx.x - token * p.q_heads;
   int b;
   Sequence s;
@@ -96,48 +100,56 @@ __global__ void __launch_bounds__(64 * kJoinWaves) attend_join_kernel(AttendPara
   if (parts.count == 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int group = tid / width, groups = kThreads / width, e = (tid & (width - 1)) * 4;
+  const auto part = [&](int i) {
+    return i < parts.count && e < p.dim ? *reinterpret_cast<const floatx4*>(p.part_o + parts.at(i, p.log_rows) * p.dim + e) : floatx4{};
+  };
+  floatx4 held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = part(group + j * groups);
+  floatx2 ml{kNegInf, 0.0f};
+  if (tid < parts.count) ml = *reinterpret_cast<const floatx2*>(p.part_ml + parts.at(tid, p.log_rows) * 2);
 
-  float top = kNegInf;
-  for (int i = tid; i < parts.count; i += kThreads) top = fmaxf(top, p.part_ml[parts.at(i, p.log_rows) * 2]);
+  float top = ml.x;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   if (lane == 0) tops[wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
-
-  floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
-  float total = 0.0f;
-  for (int i0 = 0; i0 < parts.count; i0 += kThreads) {
-    const int n = min(parts.count - i0, kThreads);
-    if (i0 > 0) __syncthreads();
-    if (tid < n) {
-      const floatx2 ml = *reinterpret_cast<const floatx2*>(p.part_ml + parts.at(i0 + tid, p.log_rows) * 2);
-      weights[tid] = join_weight(ml.x, top);
-      total += ml.y * weights[tid];
-    }
-    __syncthreads();
-    if (e < p.dim) {
-#pragma unroll 4
-      for (int i = group; i < n; i += groups) {
-        const floatx4 y = *reinterpret_cast<const floatx4*>(p.part_o + parts.at(i0 + i, p.log_rows) * p.dim + e);
-        const float f = weights[i];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += y[k] * f;
-      }
-    }
-  }
-  shares[tid] = v;
+  for (int w = 0; w < kRowWaves; ++w) top = fmaxf(top, tops[w]);
+  const float weight = tid < parts.count ? join_weight(ml.x, top) : 0.0f;
+  float total = tid < parts.count ? ml.y * weight : 0.0f;
+  weights[tid] = weight;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
   if (lane == 0) sums[wave] = total;
   __syncthreads();
-  if (group > 0 || e >= p.dim) return;
-  total = 0.0f;
+
+  floatx4 v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int w = 0; w < kJoinWaves; ++w) total += sums[w];
-  for (int g = 1; g < min(groups, parts.count); ++g) {
-    const floatx4 x = shares[g * width + tid];
+  for (int j = 0; j < kHeld; ++j) {
+    if (group + j * groups >= parts.count) break;
+    const float f = weights[group + j * groups];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += held[j][k] * f;
+  }
+#pragma unroll 4
+  for (int i = group + kHeld * groups; i < parts.count; i += groups) {
+    const floatx4 y = part(i);
+    const float f = weights[i];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += y[k] * f;
+  }
+  for (int d = width; d < 64; d <<= 1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] += __shfl_xor(v[k], d);
+  if (lane < width) shares[wave * width + lane] = v;
+  __syncthreads();
+  if (tid >= width || e >= p.dim) return;
+  total = 0.0f, v = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) {
+    const floatx4 x = shares[w * width + tid];
+    total += sums[w];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] += x[k];
   }
@@ -152,7 +164,7 @@ void launch_join(const AttendParams& p, hipStream_t stream) {
   // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 128 parts); then lane groups, of
   // which many rows of few parts need no exchange.
   if (rows < 512) {
-    attend_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
+    attend_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kRowWaves), 0, stream>>>(p, width);
   } else {
     const int each = kJoinWaves * (64 / width);
     attend_join_rows_kernel<T><<<dim3((unsigned)((rows + each - 1) / each)), dim3(64 * kJoinWaves), 0, stream>>>(p, width);
@@ -169,6 +181,7 @@ int few_waves_of(int elem_bytes, int dim) {
 hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream) { return launch_few_dim<uint16_t>(p, stream); }
 
 hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream) {
+  if (p.target > kMostShared) return hipErrorInvalidValue;
   if (elem_bytes == 2) launch_join<uint16_t>(p, stream);
   else launch_join<float>(p, stream);
   return hipGetLastError();
