@@ -139,9 +139,14 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
   p->log_rows = p->few ? sc::kLogFewRows + blocks2 : sc::kLogWideRows + twice;
   p->keys = p->few ? sc::few_keys_of(elem) : sc::wide_keys_of(elem, c->head_dim, 1 + twice);
   int64_t units = items(p->log_rows);
+  // Workgroups that share keys: `want`, or as many as all items' keys are least shares.
+  const auto shares = [&](int want) {
+    const int64_t tiles = (reach + 2 * p->keys - 2) / p->keys;
+    return (int)std::min<int64_t>(want, units * ((tiles + p->min_chunk - 1) / p->min_chunk));
+  };
   if (p->few) {
-    p->target = brief ? 0 : kWantFew;
     p->min_chunk = 2 * few_waves;
+    p->target = brief ? 0 : shares(kWantFew);
     p->slack = 0;
     p->slots = 2 * p->target;
   } else {
@@ -150,8 +155,8 @@ int plan_attend(const skipconv_cache* c, const skipconv_attend* a, Plan* p) {
     // the slack that whole units are worth (4 sequences of 12 tokens over 8000, heads of 64: 32 -> 29 us).
     const int least = elem == 2 ? 256 : std::max(p->keys, 32 * std::max(1, 3 * 96 / c->head_dim));
     const bool shared = units < kWantWide && reach > 3 * least;
-    p->target = shared ? 256 * sc::wide_groups_of(elem, c->head_dim) : 0;
     p->min_chunk = least / p->keys;
+    p->target = shared ? shares(256 * sc::wide_groups_of(elem, c->head_dim)) : 0;
     p->slack = shared ? (elem == 2 ? 256 : 64) / p->keys : 0;
     p->slots = 2 * p->target;
   }
