@@ -50,20 +50,22 @@ struct Tile {
 
 // Copies 16 bytes a lane from `base` + off (base alike in all lanes; or from each lane's own address) into LDS at `to` + 16 lane (`to` alike
 // in all lanes), without a wait: wait_loads and a barrier (or the wave's own use) come before the data is read. Written as assembly because the compiler
-// takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register is written, and
-// the addresses are read when the instruction issues; M0, the destination's base, is set in the same statement.
+// takes every later LDS read for a reader of such a copy and would wait for all that are in flight. No register but M0, the destination's base, is
+// written, and the addresses are read when the instruction issues. The wait states that the compiler would put between instructions are the
+// statement's own matter, as it knows nothing of what comes before: one between M0 and the load that reads it, and five between a vector instruction
+// that writes a scalar register (the base comes from v_readlane) and the load that reads that: the move and four idle ones.
 __device__ __forceinline__ void copy16(const char* base, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2"
                ::"s"(uniform((int)to)), "v"(off), "s"(base)
-               : "memory");
+               : "memory", "m0");
 }
 __device__ __forceinline__ void copy16(const char* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory", "m0");
 }
 
 // The same, 4 bytes a lane from each lane's own address.
 __device__ __forceinline__ void copy4(const void* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(uniform((int)to)), "v"(from) : "memory", "m0");
 }
 
 // A wave's share of the copies of one tile of keys and one of values (of the keys `lag` before), in two steps, so that page
