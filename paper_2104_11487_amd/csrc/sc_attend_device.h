@@ -239,13 +239,17 @@ struct Unit {
   int lo, hi;            // keys [lo, hi) from this unit on (hi: the item's end), lo a multiple of the key tile
 };
 
+// The first key that a row at position `at` may see (it may lie before the sequence's begin: no difference is formed that the window
+// could take past 32 bits).
+__device__ __forceinline__ int first_seen(const AttendParams& p, int at) { return p.window >= 0 && at > p.window ? at - p.window : 0; }
+
 // Fills in the rows and keys of an item's unit `part`.
 __device__ __forceinline__ void enter_item(const AttendParams& p, Unit* u) {
   u->row0 = (u->tiles - 1 - u->tile) << p.log_rows;
   // keys that the tile's rows see: up to the last row's end, from the first row's begin
   const int t0 = u->row0 / p.group, t1 = min(u->row0 + (1 << p.log_rows) - 1, u->n * p.group - 1) / p.group;
   const int p0 = u->len - u->n;
-  const int lo = p.window < 0 ? 0 : max(0, p0 + (p.causal ? t0 : 0) - p.window);
+  const int lo = first_seen(p, p0 + (p.causal ? t0 : 0));
   const int64_t from = (int64_t)(lo & ~(p.keys - 1)) + (int64_t)u->part * u->chunk;
   u->hi = p.causal ? min(p0 + t1, u->len - 1) + 1 : u->len;
   u->lo = (int)min(from, (int64_t)kMostKeys);
@@ -284,7 +288,7 @@ __device__ __forceinline__ Seen seen_by(const AttendParams& p, const Unit& u, in
   const int t = min(row, u.n * p.group - 1) / p.group, p0 = u.len - u.n;
   Seen s;
   s.hi = p.causal ? min(p0 + t, u.len - 1) : u.len - 1;
-  s.lo = p.window < 0 ? 0 : max(0, p0 + (p.causal ? t : 0) - p.window);
+  s.lo = first_seen(p, p0 + (p.causal ? t : 0));
   return s;
 }
 

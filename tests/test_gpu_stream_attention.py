@@ -321,6 +321,19 @@ def test_more_rows_than_tokens(dtype, new):
             _compare(out, lse, want, dtype, 64)
 
 
+@pytest.mark.parametrize("window", [(1 << 30) - 1, (1 << 31) - 4, (1 << 31) - 1])
+@pytest.mark.parametrize("dtype,new,kv", [("bf16", 6, 4), ("bf16", 50, 30), ("bf16", 300, 200), ("f32", 6, 4), ("f32", 50, 30)])
+def test_windows_past_every_length(dtype, new, kv, window):
+    """A window that no sequence is as long as hides nothing, also where rows lie before the sequence's begin."""
+    rng = _rng(50)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, kv), (2, 9), (4, 1)], 4, 2, 64, 16, dtype)
+    for causal in (True, False):
+        want = O.attend(q64, k64, v64, table, starts, length, causal, window)
+        for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=causal, window=window):
+            say(f"[window] {dtype} new={new} kv={kv} window={window} causal={causal} max_new={hint}")
+            _compare(out, lse, want, dtype, 64)
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,lens,heads", [("bf16", [(3, 100), (1, 70)], 4), ("bf16", [(90, 150)], 4), ("f32", [(3, 100), (1, 70)], 4), ("f32", [(90, 150)], 4)])
 def test_what_a_row_does_not_see_does_not_reach_it(dtype, lens, heads, value):
