@@ -23,6 +23,7 @@ from . import skipconv as _S
 SKIPCONV_PAIR_HALVES, SKIPCONV_PAIR_ADJACENT = 0, 1
 _PAIRING = {"halves": SKIPCONV_PAIR_HALVES, "adjacent": SKIPCONV_PAIR_ADJACENT}
 _DTYPE = {torch.float32: _S.SKIPCONV_F32, torch.bfloat16: _S.SKIPCONV_BF16}
+_MOST = 0x7fffffff  # of a description's 32-bit fields, which keep the low bits of what is larger
 
 skipconv_rotary, skipconv_cache = _S.skipconv_rotary, _S.skipconv_cache
 skipconv_append, skipconv_attend = _S.skipconv_append, _S.skipconv_attend
@@ -182,7 +183,7 @@ class CacheBatch:
             if t.dtype != torch.int32 or not t.is_cuda or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on one GPU")
         _need(max_new >= 0, "max_new must be >= 0")
-        self.page_table, self.row_start, self.kv_len, self.max_new = page_table, row_start, kv_len, int(max_new)
+        self.page_table, self.row_start, self.kv_len, self.max_new = page_table, row_start, kv_len, min(int(max_new), _MOST)
         self.sequences, self.device = n, device
         self._index = kv_len.get_device()
         # what a description of the cache takes from here
@@ -274,6 +275,7 @@ class PagedCache:
             ot, oh = heads * dim, dim
         else:
             _, _, ot, oh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
+        window = -1 if window < 0 else min(window, _MOST)  # no sequence is as long as that
         lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
         a = skipconv_attend(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, qt, qh, ot, oh, heads, 1 if causal else 0,
                             window, dim ** -0.5 if scale is None else scale, batch.max_new)

@@ -334,6 +334,19 @@ def test_windows_past_every_length(dtype, new, kv, window):
             _compare(out, lse, want, dtype, 64)
 
 
+def test_numbers_past_32_bits():
+    """Windows and hints that a description's 32-bit field does not hold mean what they say."""
+    rng = _rng(51)
+    cache, _, _, q, _, table, starts, length = _filled(rng, [(6, 90), (2, 9)], 4, 2, 64, 16, "bf16")
+    batch = _device(table, starts, length)
+    for causal in (True, False):
+        whole = cache.attend(q, batch, causal=causal)
+        for window in (1 << 31, 1 << 32, (1 << 33) + 5, -(1 << 31) - 1, -(1 << 40)):
+            assert torch.equal(cache.attend(q, batch, causal=causal, window=window), whole), window
+        for most in (1 << 31, (1 << 32) + 1, 1 << 40):
+            assert torch.equal(cache.attend(q, _device(table, starts, length, max_new=most), causal=causal), whole), most
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,lens,heads", [("bf16", [(3, 100), (1, 70)], 4), ("bf16", [(90, 150)], 4), ("f32", [(3, 100), (1, 70)], 4), ("f32", [(90, 150)], 4)])
 def test_what_a_row_does_not_see_does_not_reach_it(dtype, lens, heads, value):
