@@ -69,8 +69,21 @@ def _need(ok: bool, message: str) -> None:
         raise ValueError(message)
 
 
-# The current stream's handle of a device (by index), without a Stream object around it.
+# The current stream's handle of a device (by index), without a Stream object around it; the current device's index.
 _stream = torch._C._cuda_getCurrentRawStream
+_current = torch._C._cuda_getDevice
+
+
+def _enqueue(call, index: int, *args) -> None:
+    """The call with the device's current stream as its last argument. That device is the current one meanwhile: a handle does not
+    say which device it belongs to (a default stream's is 0 on each)."""
+    if _current() == index:
+        rc = call(*args, _stream(index))
+    else:
+        with torch.cuda.device(index):
+            rc = call(*args, _stream(index))
+    if rc:
+        _S._check(rc)
 
 
 def _refuse(x, name: str, tokens, heads, dim, dtype, index: int):
@@ -140,9 +153,7 @@ class Rotary:
             yt, yh = heads * dim, dim
         else:
             _, _, yt, yh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
-        rc = self._call(self._ref[inverse], tokens, heads, dim, code, x.data_ptr(), xt, xh, out.data_ptr(), yt, yh, _stream(index))
-        if rc:
-            _S._check(rc)
+        _enqueue(self._call, index, self._ref[inverse], tokens, heads, dim, code, x.data_ptr(), xt, xh, out.data_ptr(), yt, yh)
         return out
 
     def backward(self, grad: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -242,6 +253,8 @@ class PagedCache:
         if rotary is not None:
             if pos is None or rotary.head_dim != dim:
                 raise ValueError("a rotation needs pos and the cache's head_dim")
+            if rotary._index != index:
+                raise ValueError("the rotation is on another device than the cache")
             a.rotary = ctypes.pointer(rotary.desc(pos, tokens, 0))
         if q is not None:
             if rotary is None:
@@ -254,9 +267,7 @@ class PagedCache:
                 _, _, a.q_out_token, a.q_out_head = _heads_of(q_out, "q_out", tokens, heads, dim, dtype, index)
             a.q, a.q_out, a.q_heads = q.data_ptr(), q_out.data_ptr(), heads
         self.desc(batch, tokens)
-        rc = self._append(self._ref, ctypes.byref(a), _stream(index))
-        if rc:
-            _S._check(rc)
+        _enqueue(self._append, index, self._ref, ctypes.byref(a))
         return q_out
 
     def attend(self, q: torch.Tensor, batch: CacheBatch, causal: bool = True, window: int = -1, scale: Optional[float] = None,
@@ -287,7 +298,5 @@ class PagedCache:
             if len(self._need) < 4096:
                 self._need[shapes] = need
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        rc = self._attend(self._ref, ctypes.byref(a), ws.data_ptr() if need else None, need, _stream(index))
-        if rc:
-            _S._check(rc)
+        _enqueue(self._attend, index, self._ref, ctypes.byref(a), ws.data_ptr() if need else None, need)
         return (out, lse) if return_lse else out

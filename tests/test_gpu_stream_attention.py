@@ -501,6 +501,59 @@ def test_another_stream_and_graph_replays():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), f"replay {i}"
 
 
+def test_the_tensors_device_is_current_in_every_call(monkeypatch):
+    """With another device current, a call makes the tensors' device the current one around its launch, and leaves it afterwards."""
+    rng = _rng(52)
+    cache, _, _, q, _, table, starts, length = _filled(rng, [(2, 40)], 4, 2, 64, 16, "bf16")
+    batch, rotary = _device(table, starts, length), A.Rotary(A.axis_frequencies((16, 16)), 64)
+    pos = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+    entered = []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            entered.append(self.index)
+
+        def __exit__(self, *_):
+            entered.append("left")
+    calls = (lambda: rotary.rotate(q, pos), lambda: cache.append(q[:, :2], q[:, 2:], batch, rotary=rotary, pos=pos, q=q), lambda: cache.attend(q, batch))
+    for call in calls:  # as it is: nothing to do
+        call()
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for call in calls:
+        call()
+    assert entered == []
+    monkeypatch.setattr(A, "_current", lambda: 1, raising=False)
+    for call in calls:
+        call()
+        assert entered == [0, "left"]
+        entered.clear()
+    with pytest.raises(S.SkipConvError):
+        cache.attend(q, batch, scale=0.0)
+    assert entered == [0, "left"]
+
+
+def test_a_rotation_on_another_device_is_refused():
+    """Its table would be read from a device that the cache is not on. (One device stands for two: the rotation is told another index.)"""
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
+    cache = A.PagedCache(k, k.clone())
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch, rotary, pos = A.CacheBatch(ints(0, 1)[None], ints(0, 1), ints(5)), A.Rotary(A.axis_frequencies((16, 16)), 64), ints(1, 2)[None]
+
+    class Elsewhere:
+        dtype, shape = pos.dtype, pos.shape
+        is_contiguous, data_ptr = pos.is_contiguous, pos.data_ptr
+
+        def get_device(self):
+            return 1
+    rotary._index = 1
+    kv = torch.zeros(1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="another device"):
+        cache.append(kv, kv, batch, rotary=rotary, pos=Elsewhere())
+
+
 def test_refusals():
     k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
     cache = A.PagedCache(k, k.clone())
