@@ -105,6 +105,11 @@ def _heads_of(x: torch.Tensor, name: str, tokens: Optional[int], heads: Optional
     return t, h, st, sh
 
 
+def _fixed(name: str) -> property:
+    """What a description took at construction: to be read, not replaced (the description would keep the address of a tensor that is gone)."""
+    return property(lambda self: getattr(self, name))
+
+
 def _like(x: torch.Tensor) -> torch.Tensor:
     return torch.empty_like(x, memory_format=torch.contiguous_format)
 
@@ -115,25 +120,26 @@ class Rotary:
     freq: float32 GPU tensor, axes x pairs: token t's pair j turns by the sum over the axes a of pos[t, a] * freq[a, j].
     pairing: "halves" (elements j and j + pairs of a head) or "adjacent" (2 j and 2 j + 1); elements past 2 * pairs stay.
     pos is an int32 GPU tensor, tokens x axes; x is tokens x heads x head_dim, float32 or bfloat16, of any strides with a packed
-    last dimension.
+    last dimension. The table's values may change between calls, the tensor may not.
     """
+    freq, axes, pairs, head_dim, pairing, device = map(_fixed, ("_freq", "_axes", "_pairs", "_head_dim", "_pairing", "_device"))
 
     def __init__(self, freq: torch.Tensor, head_dim: int, pairing: str = "halves"):
         _need(freq.is_cuda and freq.dtype == torch.float32 and freq.dim() == 2, "freq must be a float32 GPU tensor, axes x pairs")
         _need(pairing in _PAIRING, "pairing must be 'halves' or 'adjacent'")
-        self.freq = freq.contiguous()
-        self.axes, self.pairs = self.freq.shape
-        _need(1 <= self.axes <= 8 and 1 <= self.pairs <= head_dim // 2, "freq must have 1..8 axes and 1..head_dim / 2 pairs")
-        self.head_dim, self.pairing, self.device = head_dim, pairing, freq.device
+        self._freq = freq.contiguous()
+        self._axes, self._pairs = self._freq.shape
+        _need(1 <= self._axes <= 8 and 1 <= self._pairs <= head_dim // 2, "freq must have 1..8 axes and 1..head_dim / 2 pairs")
+        self._head_dim, self._pairing, self._device = head_dim, pairing, freq.device
         self._index = freq.get_device()
-        self._desc = [skipconv_rotary(None, self.freq.data_ptr(), self.axes, self.pairs, _PAIRING[pairing], i) for i in (0, 1)]
+        self._desc = [skipconv_rotary(None, self._freq.data_ptr(), self._axes, self._pairs, _PAIRING[pairing], i) for i in (0, 1)]
         self._ref = [ctypes.byref(d) for d in self._desc]
         self._call = _S.lib().skipconv_rotate
 
     def desc(self, pos: torch.Tensor, tokens: int, inverse: bool = False) -> skipconv_rotary:
         """The C description for these positions (the object's own, valid until the next call of it)."""
-        if pos.dtype is not torch.int32 or pos.get_device() != self._index or pos.shape != (tokens, self.axes) or not pos.is_contiguous():
-            raise ValueError(f"pos must be a contiguous int32 tensor {[tokens, self.axes]} on {self.device}")
+        if pos.dtype is not torch.int32 or pos.get_device() != self._index or pos.shape != (tokens, self._axes) or not pos.is_contiguous():
+            raise ValueError(f"pos must be a contiguous int32 tensor {[tokens, self._axes]} on {self._device}")
         d = self._desc[inverse]
         d.pos = pos.data_ptr()
         return d
@@ -144,7 +150,7 @@ class Rotary:
         code = _DTYPE.get(dtype)
         if code is None:
             raise ValueError("x must be float32 or bfloat16")
-        dim, index = self.head_dim, self._index
+        dim, index = self._head_dim, self._index
         tokens, heads, xt, xh = _heads_of(x, "x", None, None, dim, dtype, index)
         inverse = 1 if inverse else 0
         self.desc(pos, tokens, inverse)
@@ -185,8 +191,10 @@ class CacheBatch:
 
     page_table: sequences x width page numbers; row_start: sequences + 1, the first row of each sequence in the new
     tokens' tensors; kv_len: tokens of each sequence in the cache, the new ones included. max_new: the most new tokens that
-    a sequence has, where the program knows it (it selects the kernel; the results do not depend on it).
+    a sequence has, where the program knows it (it selects the kernel; the results do not depend on it). The tensors' values may change
+    between calls, the tensors may not: others take another batch.
     """
+    page_table, row_start, kv_len, sequences, device = map(_fixed, ("_page_table", "_row_start", "_kv_len", "_sequences", "_device"))
 
     def __init__(self, page_table: torch.Tensor, row_start: torch.Tensor, kv_len: torch.Tensor, max_new: int = 0):
         n, device = kv_len.shape[0], kv_len.device
@@ -194,8 +202,8 @@ class CacheBatch:
             if t.dtype != torch.int32 or not t.is_cuda or t.device != device or tuple(t.shape) != shape or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on one GPU")
         _need(max_new >= 0, "max_new must be >= 0")
-        self.page_table, self.row_start, self.kv_len, self.max_new = page_table, row_start, kv_len, min(int(max_new), _MOST)
-        self.sequences, self.device = n, device
+        self._page_table, self._row_start, self._kv_len, self.max_new = page_table, row_start, kv_len, min(int(max_new), _MOST)
+        self._sequences, self._device = n, device
         self._index = kv_len.get_device()
         # what a description of the cache takes from here
         self._fields = (page_table.data_ptr(), row_start.data_ptr(), kv_len.data_ptr())
@@ -206,22 +214,24 @@ class PagedCache:
     """Keys and values of earlier tokens in pages.
 
     k_pages, v_pages: GPU tensors, pages x kv_heads x page_size x head_dim (views of another order are taken as they lie), float32 or
-    bfloat16, 16-byte aligned rows; the caller owns them and the page numbers.
+    bfloat16, 16-byte aligned rows; the caller owns them and the page numbers. Other pages take another cache.
     """
+    k_pages, v_pages, pages, kv_heads = map(_fixed, ("_k_pages", "_v_pages", "_pages", "_kv_heads"))
+    page_size, head_dim, dtype, device = map(_fixed, ("_page_size", "_head_dim", "_dtype", "_device"))
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         _need(k_pages.dim() == 4 and k_pages.is_cuda and k_pages.dtype in _DTYPE, "k_pages must be a 4-d float32 or bfloat16 GPU tensor")
         _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device,
               "v_pages must match k_pages in shape, dtype and device")
         _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "the pages' last dimension must be packed")
-        self.k_pages, self.v_pages = k_pages, v_pages
-        self.pages, self.kv_heads, self.page_size, self.head_dim = k_pages.shape
-        self.dtype, self.device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
+        self._k_pages, self._v_pages = k_pages, v_pages
+        self._pages, self._kv_heads, self._page_size, self._head_dim = k_pages.shape
+        self._dtype, self._device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
         c = skipconv_cache()
         c.k_pages, c.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
         c.k_page, c.k_head, c.k_slot = k_pages.stride()[:3]
         c.v_page, c.v_head, c.v_slot = v_pages.stride()[:3]
-        c.pages, c.page_size, c.kv_heads, c.head_dim, c.dtype = self.pages, self.page_size, self.kv_heads, self.head_dim, _DTYPE[self.dtype]
+        c.pages, c.page_size, c.kv_heads, c.head_dim, c.dtype = self._pages, self._page_size, self._kv_heads, self._head_dim, _DTYPE[self._dtype]
         self._c, self._ref = c, ctypes.byref(c)
         lib = _S.lib()
         self._append, self._attend = lib.skipconv_cache_append, lib.skipconv_cache_attend
@@ -239,19 +249,19 @@ class PagedCache:
             raise ValueError("the batch is on another device than the cache")
         c = self._c
         c.page_table, c.row_start, c.kv_len = batch._fields
-        c.tokens, c.batch, c.table_width = tokens, batch.sequences, batch._width
+        c.tokens, c.batch, c.table_width = tokens, batch._sequences, batch._width
         return c
 
     def append(self, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, rotary: Optional[Rotary] = None,
                pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens' keys and values (tokens x kv_heads x head_dim) into the cache, the keys turned by `rotary` at
         `pos` (int32, tokens x axes). With `q` (tokens x heads x head_dim): also returns it turned, in `q_out` (may be q) or a new tensor."""
-        dim, dtype, index = self.head_dim, self.dtype, self._index
-        tokens, _, kt, kh = _heads_of(k, "k", None, self.kv_heads, dim, dtype, index)
-        _, _, vt, vh = _heads_of(v, "v", tokens, self.kv_heads, dim, dtype, index)
+        dim, dtype, index = self._head_dim, self._dtype, self._index
+        tokens, _, kt, kh = _heads_of(k, "k", None, self._kv_heads, dim, dtype, index)
+        _, _, vt, vh = _heads_of(v, "v", tokens, self._kv_heads, dim, dtype, index)
         a = skipconv_append(k.data_ptr(), v.data_ptr(), None, None, kt, kh, vt, vh)
         if rotary is not None:
-            if pos is None or rotary.head_dim != dim:
+            if pos is None or rotary._head_dim != dim:
                 raise ValueError("a rotation needs pos and the cache's head_dim")
             if rotary._index != index:
                 raise ValueError("the rotation is on another device than the cache")
@@ -279,7 +289,7 @@ class PagedCache:
         tokens x heads x head_dim (zeros for a row that sees nothing), with return_lse also the float32 log of the
         sum of exponentials, tokens x heads (-inf there). Rows of no sequence are not written.
         """
-        dim, dtype, index = self.head_dim, self.dtype, self._index
+        dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
         if out is None:
             out = _like(q)
@@ -291,7 +301,7 @@ class PagedCache:
         a = skipconv_attend(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, qt, qh, ot, oh, heads, 1 if causal else 0,
                             window, dim ** -0.5 if scale is None else scale, batch.max_new)
         c = self.desc(batch, tokens)
-        shapes = (tokens, heads, batch.sequences, batch._width, window, batch.max_new)
+        shapes = (tokens, heads, batch._sequences, batch._width, window, batch.max_new)
         need = self._need.get(shapes)
         if need is None:
             need = skipconv_attend_workspace(c, a)

@@ -535,6 +535,23 @@ def test_the_tensors_device_is_current_in_every_call(monkeypatch):
     assert entered == [0, "left"]
 
 
+def test_what_a_description_holds_is_not_replaced():
+    """Tensors and sizes whose addresses and values were taken once; their values are written in place, and the next call reads those."""
+    rng = _rng(53)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(1, 40)], 4, 2, 64, 16, "bf16")
+    batch, rotary = _device(table, starts, length), A.Rotary(A.axis_frequencies((16, 16)), 64)
+    for held, names in ((batch, ("page_table", "row_start", "kv_len", "sequences")), (rotary, ("freq", "axes", "pairs", "head_dim", "pairing")),
+                        (cache, ("k_pages", "v_pages", "pages", "kv_heads", "page_size", "head_dim", "dtype"))):
+        for name in names:
+            value = getattr(held, name)
+            with pytest.raises(AttributeError):
+                setattr(held, name, value.clone() if torch.is_tensor(value) else value)
+            assert getattr(held, name) is value
+    batch.kv_len.fill_(17)
+    out, lse = cache.attend(q, batch, return_lse=True)
+    _compare(out, lse, O.attend(q64, k64, v64, table, starts, np.array([17], np.int32)), "bf16", 64)
+
+
 def test_a_rotation_on_another_device_is_refused():
     """Its table would be read from a device that the cache is not on. (One device stands for two: the rotation is told another index.)"""
     k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
