@@ -3,7 +3,8 @@ cache of keys and values, and attention over it (include/skipconv.h, the C names
 
 A 1 x 1 ``SkipConv`` layer's activation output, N x H x W x (heads * head_dim), viewed as
 N*H*W x heads x head_dim, is a tensor of tokens that these calls take as it lies. Work is enqueued on the current torch
-stream of the tensors' device; nothing is copied to the host. An object's calls are not thread-safe.
+stream of the tensors' device; nothing is copied to the host. An object's calls are not thread-safe. ``Rotary.__call__`` runs under
+autograd; the other calls record no graph and refuse tensors that require a gradient while gradients are recorded.
 
     rotary = Rotary(axis_frequencies((11, 11, 10)), head_dim=64)
     cache = PagedCache.empty(pages=256, page_size=64, kv_heads=2, head_dim=64)
@@ -105,6 +106,16 @@ def _heads_of(x: torch.Tensor, name: str, tokens: Optional[int], heads: Optional
     return t, h, st, sh
 
 
+# Whether gradients are recorded; what a kernel wrote, for autograd's check of the tensors that it saved.
+_recording = torch.is_grad_enabled
+_written = torch._C._increment_version
+
+
+def _refuse_graph():
+    raise ValueError("this call records no gradient, and a tensor of it requires one: call it under torch.no_grad(), or rotate by "
+                     "calling the Rotary itself")
+
+
 def _fixed(name: str) -> property:
     """What a description took at construction: to be read, not replaced (the description would keep the address of a tensor that is gone)."""
     return property(lambda self: getattr(self, name))
@@ -134,6 +145,7 @@ class Rotary:
         self._index = freq.get_device()
         self._desc = [skipconv_rotary(None, self._freq.data_ptr(), self._axes, self._pairs, _PAIRING[pairing], i) for i in (0, 1)]
         self._ref = [ctypes.byref(d) for d in self._desc]
+        self._pointer = ctypes.pointer(self._desc[0])
         self._call = _S.lib().skipconv_rotate
 
     def desc(self, pos: torch.Tensor, tokens: int, inverse: bool = False) -> skipconv_rotary:
@@ -152,6 +164,8 @@ class Rotary:
             raise ValueError("x must be float32 or bfloat16")
         dim, index = self._head_dim, self._index
         tokens, heads, xt, xh = _heads_of(x, "x", None, None, dim, dtype, index)
+        if _recording() and (x.requires_grad or self._freq.requires_grad or (out is not None and out.requires_grad)):
+            _refuse_graph()
         inverse = 1 if inverse else 0
         self.desc(pos, tokens, inverse)
         if out is None:
@@ -159,6 +173,7 @@ class Rotary:
             yt, yh = heads * dim, dim
         else:
             _, _, yt, yh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
+            _written((out,))
         _enqueue(self._call, index, self._ref[inverse], tokens, heads, dim, code, x.data_ptr(), xt, xh, out.data_ptr(), yt, yh)
         return out
 
@@ -167,15 +182,18 @@ class Rotary:
         return self.rotate(grad, pos, out, inverse=True)
 
     def __call__(self, x: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
-        """rotate() under autograd."""
-        return _RotaryFunction.apply(x, pos, self)
+        """rotate() under autograd: the gradient of x. The table has none."""
+        if _recording() and self._freq.requires_grad:
+            _refuse_graph()
+        return _RotaryFunction.apply(x, pos, self._freq, self)
 
 
 class _RotaryFunction(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, pos, rotary):
+    def forward(ctx, x, pos, freq, rotary):
         ctx.rotary = rotary
-        ctx.save_for_backward(pos)
+        # the table too, so that one that changed in the meantime is refused (one made under inference mode cannot be saved)
+        ctx.save_for_backward(pos, None if freq.is_inference() else freq)
         return rotary.rotate(x, pos)
 
     @staticmethod
@@ -183,7 +201,8 @@ class _RotaryFunction(torch.autograd.Function):
     def backward(ctx, grad):
         if grad.stride(2) != 1:  # a broadcast gradient, such as a sum's
             grad = grad.contiguous()
-        return ctx.rotary.backward(grad, ctx.saved_tensors[0]), None, None
+        pos, _ = ctx.saved_tensors
+        return ctx.rotary.backward(grad, pos), None, None, None
 
 
 class CacheBatch:
@@ -224,7 +243,7 @@ class PagedCache:
         _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device,
               "v_pages must match k_pages in shape, dtype and device")
         _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "the pages' last dimension must be packed")
-        self._k_pages, self._v_pages = k_pages, v_pages
+        self._k_pages, self._v_pages = self._both = k_pages, v_pages
         self._pages, self._kv_heads, self._page_size, self._head_dim = k_pages.shape
         self._dtype, self._device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
         c = skipconv_cache()
@@ -259,13 +278,18 @@ class PagedCache:
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, _, kt, kh = _heads_of(k, "k", None, self._kv_heads, dim, dtype, index)
         _, _, vt, vh = _heads_of(v, "v", tokens, self._kv_heads, dim, dtype, index)
+        if _recording() and (k.requires_grad or v.requires_grad or self._k_pages.requires_grad or self._v_pages.requires_grad
+                             or (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad)
+                             or (rotary is not None and rotary._freq.requires_grad)):
+            _refuse_graph()
         a = skipconv_append(k.data_ptr(), v.data_ptr(), None, None, kt, kh, vt, vh)
         if rotary is not None:
             if pos is None or rotary._head_dim != dim:
                 raise ValueError("a rotation needs pos and the cache's head_dim")
             if rotary._index != index:
                 raise ValueError("the rotation is on another device than the cache")
-            a.rotary = ctypes.pointer(rotary.desc(pos, tokens, 0))
+            rotary.desc(pos, tokens, 0)
+            a.rotary = rotary._pointer
         if q is not None:
             if rotary is None:
                 raise ValueError("queries are only turned: pass rotary and pos")
@@ -275,8 +299,10 @@ class PagedCache:
                 a.q_out_token, a.q_out_head = heads * dim, dim
             else:
                 _, _, a.q_out_token, a.q_out_head = _heads_of(q_out, "q_out", tokens, heads, dim, dtype, index)
+                _written((q_out,))
             a.q, a.q_out, a.q_heads = q.data_ptr(), q_out.data_ptr(), heads
         self.desc(batch, tokens)
+        _written(self._both)
         _enqueue(self._append, index, self._ref, ctypes.byref(a))
         return q_out
 
@@ -291,11 +317,15 @@ class PagedCache:
         """
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
+        if _recording() and (q.requires_grad or self._k_pages.requires_grad or self._v_pages.requires_grad
+                             or (out is not None and out.requires_grad)):
+            _refuse_graph()
         if out is None:
             out = _like(q)
             ot, oh = heads * dim, dim
         else:
             _, _, ot, oh = _heads_of(out, "out", tokens, heads, dim, dtype, index)
+            _written((out,))
         window = -1 if window < 0 else min(window, _MOST)  # no sequence is as long as that
         lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if return_lse else None
         a = skipconv_attend(q.data_ptr(), out.data_ptr(), lse.data_ptr() if return_lse else None, qt, qh, ot, oh, heads, 1 if causal else 0,

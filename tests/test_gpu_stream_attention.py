@@ -121,6 +121,56 @@ def test_rotation_gradient():
     assert np.abs(x.grad.double().cpu().numpy() - ones).max() <= 32 * U
 
 
+def _small_call():
+    """A cache, a batch, a rotation and what their calls take."""
+    rng = _rng(54)
+    cache, _, _, q, _, table, starts, length = _filled(rng, [(2, 40)], 4, 2, 64, 16, "bf16")
+    return cache, _device(table, starts, length), A.Rotary(A.axis_frequencies((16, 16)), 64), torch.ones(2, 2, dtype=torch.int32, device="cuda"), q
+
+
+def test_no_gradient_is_lost():
+    """Calls without a graph refuse tensors that require a gradient, unless none are recorded."""
+    cache, batch, rotary, pos, q = _small_call()
+    k, v = (x.contiguous().clone() for x in (q[:, :2], q[:, 2:]))
+    out = torch.empty_like(q)
+    calls = ((lambda: rotary.rotate(q, pos), (q, rotary.freq)), (lambda: rotary.rotate(q, pos, out=out), (q, out)), (lambda: rotary.backward(q, pos), (q,)),
+             (lambda: rotary(q, pos), (rotary.freq,)), (lambda: cache.append(k, v, batch), (k, v, cache.k_pages, cache.v_pages)),
+             (lambda: cache.append(k, v, batch, rotary=rotary, pos=pos, q=q, q_out=out), (k, v, q, out, rotary.freq)),
+             (lambda: cache.attend(q, batch), (q, cache.k_pages, cache.v_pages)), (lambda: cache.attend(q, batch, out=out), (q, out)))
+    for call, tensors in calls:
+        call()
+        for x in tensors:
+            x.requires_grad_(True)
+            with pytest.raises(ValueError, match="gradient"):
+                call()
+            with torch.no_grad():
+                call()
+            x.requires_grad_(False)
+
+
+def test_what_a_call_writes_is_known_to_autograd():
+    """A tensor that autograd saved and a call wrote over afterwards is refused by the backward pass, as after any operation in place."""
+    cache, batch, rotary, pos, q = _small_call()
+    k, v = (x.contiguous().clone() for x in (q[:, :2], q[:, 2:]))
+    weight = torch.ones(1, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    out = torch.zeros_like(q)
+    calls = ((lambda: rotary.rotate(q, pos, out=q), q), (lambda: cache.append(k, v, batch), cache.k_pages), (lambda: cache.append(k, v, batch), cache.v_pages),
+             (lambda: cache.append(k, v, batch, rotary=rotary, pos=pos, q=q, q_out=q), q), (lambda: cache.attend(q, batch, out=out), out))
+    for call, written in calls:
+        loss = (weight * written).sum()  # saves `written` for the gradient of weight
+        call()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    x = torch.randn(2, 4, 64, device="cuda", requires_grad=True)
+    with torch.inference_mode():
+        other = A.Rotary(A.axis_frequencies((16, 16)), 64)
+    other(x, pos).sum().backward()
+    loss = rotary(x, pos).sum()
+    rotary.freq.mul_(2.0)  # the gradient would turn back by other angles
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
 def test_axis_frequencies():
     f = A.axis_frequencies((3, 2, 4), base=100.0).cpu().numpy()
     assert f.shape == (3, 9) and (np.count_nonzero(f, axis=0) == 1).all()
