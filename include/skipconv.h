@@ -389,8 +389,9 @@ const char* skipconv_last_error(skipconv_t h);
  * cache, and attend from each frame's new tokens to it. They keep no
  * handle: every call describes its tensors, allocates nothing, copies nothing
  * to the host and enqueues its kernels on `stream`, so it may be captured in a
- * graph. Strides are in elements; the last dimension is packed. Errors are
- * recorded for skipconv_last_error(NULL) (of the calling thread). */
+ * graph. Strides are in elements; the last dimension is packed; the stride of a
+ * dimension of one place is not looked at. Errors are recorded for
+ * skipconv_last_error(NULL) (of the calling thread). */
 
 /* Pairs of a head's elements that turn together: HALVES (j, j + pairs),
  * ADJACENT (2 j, 2 j + 1), j < pairs. */

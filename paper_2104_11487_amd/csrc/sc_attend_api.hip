@@ -28,6 +28,8 @@ constexpr int kWantFew = 256;
 
 bool on16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool whole16(int64_t stride, int elem) { return (stride * elem) % 16 == 0; }
+// The stride of a dimension of n: nothing is reached by that of one place, which a view may leave at any value.
+int64_t stride_of(int64_t n, int64_t stride) { return n > 1 ? stride : 0; }
 
 int check_rotary(const skipconv_rotary* r, int64_t tokens, int head_dim) {
   if (r->axes < 1 || r->axes > 8) return invalid("rotary: axes must be 1..8");
@@ -68,7 +70,8 @@ int check_cache(const skipconv_cache* c, bool pointers) {
   if ((int64_t)c->table_width * c->page_size > sc::kMostKeys)
     return fail(SKIPCONV_E_UNSUPPORTED, "cache: table_width * page_size must be at most 2^30");
   const int e = c->dtype == SKIPCONV_BF16 ? 2 : 4;
-  for (int64_t s : {c->k_page, c->k_head, c->k_slot, c->v_page, c->v_head, c->v_slot})
+  for (int64_t s : {stride_of(c->pages, c->k_page), stride_of(c->kv_heads, c->k_head), stride_of(c->page_size, c->k_slot),
+                    stride_of(c->pages, c->v_page), stride_of(c->kv_heads, c->v_head), stride_of(c->page_size, c->v_slot)})
     if (s < 0 || !whole16(s, e)) return invalid("cache: strides must be >= 0 and multiples of 16 bytes");
   if (!pointers) return SKIPCONV_OK;
   if (!c->k_pages || !c->v_pages || !c->page_table || !c->row_start || !c->kv_len) return invalid("cache: NULL pointer");
@@ -79,8 +82,8 @@ int check_cache(const skipconv_cache* c, bool pointers) {
 void fill_cache(sc::CacheView* v, const skipconv_cache* c) {
   v->k = static_cast<char*>(c->k_pages);
   v->v = static_cast<char*>(c->v_pages);
-  v->k_page = c->k_page, v->k_head = c->k_head, v->k_slot = c->k_slot;
-  v->v_page = c->v_page, v->v_head = c->v_head, v->v_slot = c->v_slot;
+  v->k_page = stride_of(c->pages, c->k_page), v->k_head = stride_of(c->kv_heads, c->k_head), v->k_slot = stride_of(c->page_size, c->k_slot);
+  v->v_page = stride_of(c->pages, c->v_page), v->v_head = stride_of(c->kv_heads, c->v_head), v->v_slot = stride_of(c->page_size, c->v_slot);
   v->table = c->page_table;
   v->row_start = c->row_start;
   v->kv_len = c->kv_len;
@@ -188,6 +191,8 @@ int skipconv_rotate(const skipconv_rotary* r, int64_t tokens, int32_t heads, int
   if ((tokens > 1 && y_token == 0) || (heads > 1 && y_head == 0)) return invalid("rotate: rows of y overlap");
   const int elem = dtype == SKIPCONV_BF16 ? 2 : 4;
   if (((uintptr_t)x | (uintptr_t)y) % elem != 0) return invalid("rotate: x or y is not aligned to its elements");
+  x_token = stride_of(tokens, x_token), x_head = stride_of(heads, x_head);
+  y_token = stride_of(tokens, y_token), y_head = stride_of(heads, y_head);
   sc::RotateParams p = {};
   p.src[0] = static_cast<const char*>(x), p.src_token[0] = x_token, p.src_head[0] = x_head;
   p.dst = static_cast<char*>(y), p.dst_token = y_token, p.dst_head = y_head;
@@ -217,15 +222,16 @@ int skipconv_cache_append(const skipconv_cache* c, const skipconv_append* a, voi
     return invalid("append: a tensor is not aligned to its elements");
   sc::RotateParams p = {};
   const void* src[3] = {a->q, a->k, a->v};
-  const int64_t token[3] = {a->q_token, a->k_token, a->v_token}, head[3] = {a->q_head, a->k_head, a->v_head};
+  const int64_t token[3] = {stride_of(c->tokens, a->q_token), stride_of(c->tokens, a->k_token), stride_of(c->tokens, a->v_token)};
+  const int64_t head[3] = {stride_of(heads, a->q_head), stride_of(c->kv_heads, a->k_head), stride_of(c->kv_heads, a->v_head)};
   bool wide = true;
   for (int i = a->q ? 0 : 1; i < 3; ++i) {
     p.src[i] = static_cast<const char*>(src[i]), p.src_token[i] = token[i], p.src_head[i] = head[i];
     wide = wide && on16(src[i]) && whole16(token[i], elem) && whole16(head[i], elem);
   }
   if (a->q) {
-    p.dst = static_cast<char*>(a->q_out), p.dst_token = a->q_out_token, p.dst_head = a->q_out_head;
-    wide = wide && on16(a->q_out) && whole16(a->q_out_token, elem) && whole16(a->q_out_head, elem);
+    p.dst = static_cast<char*>(a->q_out), p.dst_token = stride_of(c->tokens, a->q_out_token), p.dst_head = stride_of(heads, a->q_out_head);
+    wide = wide && on16(a->q_out) && whole16(p.dst_token, elem) && whole16(p.dst_head, elem);
   }
   p.heads[0] = heads, p.heads[1] = p.heads[2] = c->kv_heads;
   p.tokens = (int)c->tokens, p.dim = c->head_dim;
@@ -253,8 +259,9 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
   if (c->tokens == 0 || c->batch == 0) return SKIPCONV_OK;
   if (!a->q || !a->out) return invalid("attend: q or out is NULL");
   const int elem = c->dtype == SKIPCONV_BF16 ? 2 : 4, group = a->q_heads / c->kv_heads;
-  if (!on16(a->q) || !on16(a->out) || !whole16(a->q_token, elem) || !whole16(a->q_head, elem) || !whole16(a->out_token, elem) ||
-      !whole16(a->out_head, elem))
+  const int64_t q_token = stride_of(c->tokens, a->q_token), q_head = stride_of(a->q_heads, a->q_head);
+  const int64_t o_token = stride_of(c->tokens, a->out_token), o_head = stride_of(a->q_heads, a->out_head);
+  if (!on16(a->q) || !on16(a->out) || !whole16(q_token, elem) || !whole16(q_head, elem) || !whole16(o_token, elem) || !whole16(o_head, elem))
     return invalid("attend: q and out must be 16-byte aligned with strides of whole 16 bytes");
   if ((c->tokens > 1 && a->out_token == 0) || (a->q_heads > 1 && a->out_head == 0)) return invalid("attend: rows of out overlap");
   if ((uintptr_t)a->lse % 4 != 0) return invalid("attend: lse is not aligned to its elements");
@@ -266,8 +273,8 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
 
   sc::AttendParams p = {};
   fill_cache(&p.c, c);
-  p.q = static_cast<const char*>(a->q), p.q_token = a->q_token, p.q_head = a->q_head;
-  p.out = static_cast<char*>(a->out), p.o_token = a->out_token, p.o_head = a->out_head;
+  p.q = static_cast<const char*>(a->q), p.q_token = q_token, p.q_head = q_head;
+  p.out = static_cast<char*>(a->out), p.o_token = o_token, p.o_head = o_head;
   p.lse = a->lse;
   p.part_o = static_cast<float*>(workspace);
   p.part_ml = plan.part_o ? p.part_o + plan.part_o / 4 : nullptr;
@@ -286,8 +293,8 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
     int chunks = 4;
     while (chunks * 16 < ((c->head_dim + 31) / 32 * 32) * elem) chunks *= 2;
     const int rows = 64 / chunks;
-    const int64_t reach = (int64_t)rows * std::max(c->k_slot, c->v_slot) * elem;
-    const int64_t page_bytes = std::max(c->k_page, c->v_page) * elem;
+    const int64_t reach = (int64_t)rows * std::max(p.c.k_slot, p.c.v_slot) * elem;
+    const int64_t page_bytes = std::max(p.c.k_page, p.c.v_page) * elem;
     const int uniform = c->page_size % rows == 0 && reach < (1ll << 31) && page_bytes < (1ll << 32);
     e = elem == 2 ? sc::launch_attend_wide_bf16(p, uniform, s) : sc::launch_attend_wide_f32(p, uniform, s);
   }

@@ -499,6 +499,36 @@ def test_scale_strides_and_out():
     assert (wide[:, :2] == 5.0).all() and (wide[:, 6:] == 5.0).all() and (wide[23:] == 5.0).all()
 
 
+@pytest.mark.parametrize("dtype,group", [("bf16", 4), ("bf16", 40), ("f32", 4), ("f32", 40)])
+def test_strides_of_dimensions_of_one_place(dtype, group):
+    """One token, one key head, one page, or pages of one slot: the stride there may be any number, as a slice of a projection leaves it."""
+    rng = _rng(55)
+
+    def any_stride(x):
+        """The tensor with each stride of a dimension of one place no multiple of 16 bytes."""
+        return x.as_strided(x.shape, [s if n > 1 else 1001 + i for i, (n, s) in enumerate(zip(x.shape, x.stride()))])
+    for lens, page in (([(1, 40)], 64), ([(1, 9)], 1), ([(1, 40)], 16)):
+        cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, group, 1, 64, page, dtype)
+        want = O.attend(q64, k64, v64, table, starts, length)
+        keep = cache.k_pages[table[0, 0]:][:1], cache.v_pages[table[0, 0]:][:1]
+        if page == 64:  # a cache of one page
+            cache, table = A.PagedCache(*(any_stride(x.contiguous()) for x in keep)), np.zeros_like(table)
+        else:
+            cache = A.PagedCache(any_stride(cache.k_pages), any_stride(cache.v_pages))
+        batch, out = _device(table, starts, length), torch.empty_like(q)
+        for src in (any_stride(q), any_stride(q.repeat(2, 1, 1)[:1])):
+            got, lse = cache.attend(src, batch, out=any_stride(out), return_lse=True)
+            _compare(got, lse, want, dtype, 64)
+        # appending the token again, and the rotation: as with packed strides
+        rotary, pos = A.Rotary(A.axis_frequencies((16, 16)), 64), torch.ones(1, 2, dtype=torch.int32, device="cuda")
+        k, v = q[:, :1], q[:, 1:2]
+        turned = rotary.rotate(q, pos)
+        assert torch.equal(rotary.rotate(any_stride(q), pos, out=any_stride(out)), turned)
+        assert torch.equal(cache.append(any_stride(k), any_stride(v), batch, rotary=rotary, pos=pos, q=any_stride(q)), turned)
+        at = int(length[0]) - 1
+        assert torch.equal(cache.k_pages[table[0, at // page], 0, at % page], turned[0, 0]) and torch.equal(cache.v_pages[table[0, at // page], 0, at % page], v[0, 0])
+
+
 @pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 40), ("f32", 1), ("f32", 40)])
 def test_offsets_past_32_bits(dtype, new):
     """Pages whose element offsets pass 2^32."""
