@@ -74,7 +74,8 @@ int check_cache(const skipconv_cache* c, bool pointers) {
                     stride_of(c->pages, c->v_page), stride_of(c->kv_heads, c->v_head), stride_of(c->page_size, c->v_slot)})
     if (s < 0 || !whole16(s, e)) return invalid("cache: strides must be >= 0 and multiples of 16 bytes");
   if (!pointers) return SKIPCONV_OK;
-  if (!c->k_pages || !c->v_pages || !c->page_table || !c->row_start || !c->kv_len) return invalid("cache: NULL pointer");
+  if (!c->k_pages || !c->v_pages) return invalid("cache: NULL pointer");
+  if (c->batch > 0 && (!c->page_table || !c->row_start || !c->kv_len)) return invalid("cache: NULL pointer");  // arrays of no element have none
   if (!on16(c->k_pages) || !on16(c->v_pages)) return invalid("cache: the pages must be 16-byte aligned");
   return SKIPCONV_OK;
 }

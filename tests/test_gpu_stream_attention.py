@@ -128,6 +128,18 @@ def _small_call():
     return cache, _device(table, starts, length), A.Rotary(A.axis_frequencies((16, 16)), 64), torch.ones(2, 2, dtype=torch.int32, device="cuda"), q
 
 
+def test_a_batch_of_no_sequence():
+    cache, _, rotary, pos, q = _small_call()
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = A.CacheBatch(ints(0, 4), ints(1), ints(0))
+    for tokens in (0, 2):  # rows of no sequence are not written
+        x, at, out = q[:tokens], pos[:tokens], torch.full_like(q[:tokens], 3.0)
+        pages = cache.k_pages.clone(), cache.v_pages.clone()
+        cache.append(x[:, :2], x[:, 2:], none, rotary=rotary, pos=at, q=x, q_out=out)
+        assert cache.attend(x, none, out=out) is out and (out == 3.0).all()
+        assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(pages, (cache.k_pages, cache.v_pages)))
+
+
 def test_no_gradient_is_lost():
     """Calls without a graph refuse tensors that require a gradient, unless none are recorded."""
     cache, batch, rotary, pos, q = _small_call()

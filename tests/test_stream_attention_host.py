@@ -159,6 +159,14 @@ def test_nothing_to_do():
         assert lib.skipconv_attend_workspace(ctypes.byref(c), ctypes.byref(_attend()), ctypes.byref(n)) == S.SKIPCONV_OK and n.value == 0
 
 
+def test_a_batch_of_no_sequence_has_no_arrays():
+    lib = S.lib()
+    for tokens in (0, 8):
+        c = _cache(batch=0, tokens=tokens, page_table=None, row_start=None, kv_len=None)
+        assert lib.skipconv_cache_append(ctypes.byref(c), ctypes.byref(_append()), None) == S.SKIPCONV_OK
+        assert lib.skipconv_cache_attend(ctypes.byref(c), ctypes.byref(_attend()), None, 0, None) == S.SKIPCONV_OK
+
+
 CACHE = [
     (dict(dtype=2), INVALID), (dict(tokens=-1), INVALID), (dict(batch=-1), INVALID), (dict(kv_heads=0), INVALID), (dict(pages=0), INVALID),
     (dict(page_size=0), INVALID), (dict(table_width=0), INVALID), (dict(head_dim=60), UNSUPPORTED), (dict(head_dim=264), UNSUPPORTED),
