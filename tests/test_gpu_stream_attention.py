@@ -498,6 +498,121 @@ def test_keys_shared_by_workgroups(case):
             _compare(out, lse, want, dtype, dim)
 
 
+def _dense(q64, k64, v64, table, starts, length, causal, window):
+    """The oracle's attend() as dense products in 64 bits, sequence by sequence and head by head, for calls of many rows. The fourth result
+    says which outputs see a value that is not finite (they count as zero in the others)."""
+    tokens, heads, dim = q64.shape
+    kv_heads, page = k64.shape[1], k64.shape[2]
+    group = heads // kv_heads
+    f64 = lambda *shape: torch.zeros(shape, dtype=torch.float64, device="cuda")  # noqa: E731
+    out, weight, odd = f64(tokens, heads, dim), f64(tokens, heads, dim), f64(tokens, heads, dim)
+    lse, size, most, count = f64(tokens, heads) - math.inf, f64(tokens, heads), f64(tokens, heads), f64(tokens, heads)
+    for b, kv in enumerate(int(x) for x in length):
+        t0, n = int(starts[b]), int(starts[b + 1] - starts[b])
+        if n == 0 or kv == 0:
+            continue
+        held = table[b, :-(-kv // page)]
+        at, col = kv - n + torch.arange(n, device="cuda")[:, None], torch.arange(kv, device="cuda")
+        sees = col <= at if causal else (col >= 0).expand(n, kv)
+        if window >= 0:
+            sees = sees & (col >= (at if causal else kv - n) - window)
+        for g in range(kv_heads):
+            keys, values = (torch.from_numpy(x[held, g].reshape(-1, dim)[:kv]).cuda() for x in (k64, v64))
+            fine = torch.isfinite(values)
+            values = torch.where(fine, values, torch.zeros_like(values))
+            for h in range(g * group, (g + 1) * group):
+                q, rows = torch.from_numpy(q64[t0:t0 + n, h]).cuda(), slice(t0, t0 + n)
+                score = dim ** -0.5 * (q @ keys.T)
+                hidden = score.masked_fill(~sees, -math.inf)
+                top = hidden.amax(1, keepdim=True).nan_to_num(neginf=0.0)
+                e = (hidden - top).exp()
+                total = e.sum(1, keepdim=True)
+                scale = 1 / total.clamp(min=1e-300)
+                out[rows, h], weight[rows, h] = e @ values * scale, e @ values.abs() * scale
+                odd[rows, h] = sees.double() @ (~fine).double()
+                lse[rows, h] = (top + total.log())[:, 0]
+                size[rows, h] = (dim ** -0.5 * (q.abs() @ keys.abs().T)).masked_fill(~sees, 0.0).amax(1)
+                most[rows, h] = score.abs().masked_fill(~sees, 0.0).amax(1)
+                count[rows, h] = sees.sum(1).double()
+    np_of = lambda x: x.cpu().numpy()  # noqa: E731
+    return np_of(out), np_of(lse), {"weight": np_of(weight), "size": np_of(size), "most": np_of(most), "count": np_of(count)}, np_of(odd) > 0
+
+
+@pytest.mark.parametrize("mask", MASKS, ids=[f"{'causal' if c else 'frame'}{w}" for c, w in MASKS])
+def test_the_dense_oracle(mask):
+    rng = _rng(56)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(9, 5), (17, 60), (0, 8), (30, 30)], 6, 3, 24, 7, "f32")
+    want, got = O.attend(q64, k64, v64, table, starts, length, *mask), _dense(q64, k64, v64, table, starts, length, *mask)
+    for a, b in zip((want[0], want[1], *want[2].values()), (got[0], got[1], *got[2].values())):
+        assert np.allclose(a, b, rtol=1e-11, atol=1e-11)
+    assert not got[3].any()
+
+
+# Calls of which a workgroup takes 256 rows of a key head: bf16 heads of up to 64, and as many such units as half of what fits the GPU.
+# lens, heads, kv heads, dim, page, order, the form that the lengths give
+DOUBLE = [
+    ([(530, 700), (530, 640)], 64, 8, 64, 16, "heads", "short"),
+    ([(530, 690), (530, 531)], 64, 8, 40, 7, "slots", "short"),
+    ([(1040, 600), (3, 80)], 64, 8, 64, 16, "heads", "short"),
+    ([(1100, 1500), (1, 900)], 64, 8, 64, 16, "slots", "shared"),
+    ([(1024, 1537)], 64, 8, 32, 16, "heads", "shared"),
+    ([(600, 1201), (0, 40), (530, 531)], 64, 8, 40, 7, "heads", "shared"),
+    ([(1060, 2000)], 64, 8, 64, 9, "heads", "shared"),
+    ([(2100, 2111)], 64, 8, 64, 16, "heads", "many"),
+    ([(1050, 1900), (1060, 1063)], 64, 8, 32, 5, "slots", "many"),
+]
+
+
+def _double_case(rng, case, spoil=None):
+    """The case's tensors; checked that it is what it says."""
+    lens, heads, kv_heads, dim, page, order, form = case
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, kv_heads, dim, page, "bf16", order, spoil=spoil)
+    rows = q.shape[0] * heads // kv_heads
+    assert (rows >> 8) * kv_heads >= 256 and dim <= 64
+    batch = _device(table, starts, length)
+    a = S.skipconv_attend(None, None, None, *(heads * dim, dim) * 2, heads, 1, -1, 0.1, 0)
+    room = {"short": table.shape[1] * page <= 768, "shared": table.shape[1] * page > 768, "many": True}
+    few_units = ((rows >> 8) + min(len(lens), q.shape[0])) * kv_heads < 512
+    assert room[form] and few_units == (form != "many")
+    c = cache.desc(batch, q.shape[0])
+    assert (A.skipconv_attend_workspace(c, a) > 0) == (form == "shared")
+    if form != "many":  # the parts that a longer table takes show the rows of a unit
+        c.table_width = 1 << 20
+        assert A.skipconv_attend_workspace(c, a) == 2 * 512 * 256 * (dim + 2) * 4
+    return cache, k64, v64, q, q64, table, starts, length
+
+
+@pytest.mark.parametrize("mask", [(True, -1), (False, -1), (True, 200), (False, 333), (True, 0)], ids=lambda m: f"{'causal' if m[0] else 'frame'}{m[1]}")
+@pytest.mark.parametrize("case", DOUBLE, ids=[f"{i}-{c[-1]}" for i, c in enumerate(DOUBLE)])
+def test_two_row_blocks_a_wave(case, mask):
+    cache, k64, v64, q, q64, table, starts, length = _double_case(_rng(57 + case[3] + case[4]), case)
+    want = _dense(q64, k64, v64, table, starts, length, *mask)[:3]
+    for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+        say(f"[two blocks] {case} mask={mask} max_new={hint}")
+        _compare(out, lse, want, "bf16", case[3])
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("case", [DOUBLE[0], DOUBLE[1], DOUBLE[3], DOUBLE[7]], ids=lambda c: f"{c[-1]}-{c[3]}")
+def test_two_row_blocks_a_wave_and_values_that_are_not_finite(case, value):
+    """The newest tokens', which a causal mask hides from earlier rows, and ones that a window hides."""
+    lens, dim = case[0], case[3]
+
+    def spoil(kp, vp, table):
+        kv, page = lens[0][1], case[4]
+        for at in (kv - 1, kv - 2, kv - 300, 40, 0):
+            vp[table[0, at // page], :, at % page, 3:9] = value
+    cache, k64, v64, q, q64, table, starts, length = _double_case(_rng(58 + dim), case, spoil)
+    for mask in ((True, -1), (True, 150), (False, 100)):
+        o, l, b, odd = _dense(q64, k64, v64, table, starts, length, *mask)  # noqa: E741
+        assert odd.any() and not odd.all() and not odd[..., 9:].any()
+        for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+            say(f"[two blocks, {value}] {case} mask={mask} max_new={hint}")
+            got = torch.from_numpy(odd).cuda()
+            assert not torch.isfinite(out[got]).any()
+            _compare(out.masked_fill(got, 0.0), lse, (np.where(odd, 0.0, o), l, b), "bf16", dim)
+
+
 def test_scale_strides_and_out():
     rng = _rng(45)
     cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(20, 90), (3, 64)], 4, 2, 64, 16, "bf16")
