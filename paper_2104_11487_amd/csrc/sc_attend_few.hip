@@ -161,7 +161,7 @@ void launch_join(const AttendParams& p, hipStream_t stream) {
   const int rows = p.c.tokens * p.q_heads;
   int width = 8;
   while (width * 4 < p.dim) width *= 2;  // lanes of a row: 8..64
-  // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 128 parts); then lane groups, of
+  // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 241 parts); then lane groups, of
   // which many rows of few parts need no exchange.
   if (rows < 512) {
     attend_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kRowWaves), 0, stream>>>(p, width);

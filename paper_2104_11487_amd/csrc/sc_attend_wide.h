@@ -6,9 +6,13 @@
 // wave fit the registers of two waves a SIMD: bf16 heads of up to 64), and walks the keys in tiles that all waves share, the next
 // tile's copies into LDS in flight during this one's products. Where a launch has fewer items (128 rows and a key head) than workgroups
 // fit the GPU, they share its key tiles (sc_attend_device.h), and a second launch joins the parts.
-// With many rows the matrix and vector units bound it (8192 tokens over 24576, heads of 128: 1.58 ms, 1.04 PFLOP/s, matrix units busy
-// half of the time, the exponentials' vector work beside them as long); with a row of each of many sequences the
+// With many rows the matrix and vector units bound it (8192 tokens over 24576, heads of 128: 1.55 to 1.69 ms by card, 0.95 to 1.04 PFLOP/s, matrix
+// units busy half of the time, the exponentials' vector work beside them as long); with a row of each of many sequences the
 // cache's bytes do (64 sequences of up to 16384, heads of 128: 220 us, 5.2 TB/s).
+// Heads above 128 (fp32: above 96) leave one wave a SIMD (bf16 heads of 256, 4096 tokens of 4 streams over 12288: 2.1 ms, 64 % of the product's rate). Builds that
+// do not hold everything in registers: fp32 above 192, 114 to 147 in scratch memory (256 tokens of 4 sequences over
+// 1500, 4 heads of 256: 210 us, of 192: 82); fp32 96 (7 to 23, not where nothing is shared and pages are whole), bf16 64 with two row blocks where keys are
+// shared (12 to 23), bf16 96 and 128 where they are (1), bf16 256 (3 in one build).
 // Products are formed transposed: scores S' = K Q' have a row's scores in two lanes (l and l + 32), so softmax needs one
 // lane exchange a block of 32 keys, and O' = V' P' takes the exponentials from the registers that the scores left them in: the key
 // that a k index of the product stands for is free, as long as V's fragment follows, so no lane exchange and no LDS is needed for P.

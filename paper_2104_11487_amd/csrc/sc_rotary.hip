@@ -3,12 +3,14 @@
 //   angle(t, j) = sum_a pos[t][a] * freq[a][j]
 //   (u, w) -> (u cos - w sin, w cos + u sin)   for the pairs j < pairs of a head; the other elements stay
 //
-// One kernel for both: a workgroup takes a few tokens' heads (queries, keys, values), loads them into registers, forms each
+// One kernel for both: a workgroup takes a few tokens' heads (queries, keys, values), loads them, forms each
 // angle's cosine and sine once for all heads in LDS while those loads are in flight, and stores the turned heads to their
 // tensor or to the cache's slot. Nothing of a head is stored before all of it is loaded, so a tensor may be turned in place.
 // Bound by memory: every element is read once and written once, 16 bytes a lane (32768 tokens of 16 bf16 heads of 128 out of a packed
-// projection: 49 us, 5.5 TB/s; keys and values of 16384 tokens, 4 heads of 64, and 8 of queries: 15 us, 4.5 TB/s); a few tokens are one
-// launch's latency (3.7 us on the GPU).
+// projection: 50 us, 5.4 TB/s; keys and values of 16384 tokens, 4 heads of 64, and 8 of queries: 15 us, 4.5 TB/s); a few tokens are one
+// launch's latency (3.8 us on the GPU). That is modes 0 and 1 (below), whose operands stay in registers. Modes 2 and 3 load the partners one by one and
+// their builds keep the operands in scratch memory (296 bytes a thread), several times slower: the same 32768 tokens with 60 of 64 pairs 428 us (mode 2,
+// fp32 with 62: 795), with rows that begin anywhere 1600 us (mode 3).
 // Angles are summed and reduced to a turn in 64 bits (an fp32 product would be off by |angle| * 2^-24), the turn of an
 // element in 32 bits, rounded once to the tensor's type.
 #include "sc_attend_device.h"

@@ -210,8 +210,8 @@ class CacheBatch:
 
     page_table: sequences x width page numbers; row_start: sequences + 1, the first row of each sequence in the new
     tokens' tensors; kv_len: tokens of each sequence in the cache, the new ones included. max_new: the most new tokens that
-    a sequence has, where the program knows it (it selects the kernel; the results do not depend on it). The tensors' values may change
-    between calls, the tensors may not: others take another batch.
+    a sequence has, where the program knows it (it selects the kernel; the results are right whatever it is, though kernels differ in
+    rounding). The tensors' values may change between calls, the tensors may not: others take another batch.
     """
     page_table, row_start, kv_len, sequences, device = map(_fixed, ("_page_table", "_row_start", "_kv_len", "_sequences", "_device"))
 
