@@ -301,6 +301,8 @@ class PagedCache:
                 _, _, a.q_out_token, a.q_out_head = _heads_of(q_out, "q_out", tokens, heads, dim, dtype, index)
                 _written((q_out,))
             a.q, a.q_out, a.q_heads = q.data_ptr(), q_out.data_ptr(), heads
+        elif q_out is not None:
+            raise ValueError("q_out without q")
         self.desc(batch, tokens)
         _written(self._both)
         _enqueue(self._append, index, self._ref, ctypes.byref(a))

@@ -759,6 +759,14 @@ def test_what_a_description_holds_is_not_replaced():
     _compare(out, lse, O.attend(q64, k64, v64, table, starts, np.array([17], np.int32)), "bf16", 64)
 
 
+def test_an_output_without_queries_is_refused():
+    """Nothing would be written to it, and it would be returned as if."""
+    cache, batch, rotary, pos, q = _small_call()
+    for turn in ({}, dict(rotary=rotary, pos=pos)):
+        with pytest.raises(ValueError, match="q_out"):
+            cache.append(q[:, :2], q[:, 2:], batch, q_out=torch.empty_like(q), **turn)
+
+
 def test_a_rotation_on_another_device_is_refused():
     """Its table would be read from a device that the cache is not on. (One device stands for two: the rotation is told another index.)"""
     k = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16, device="cuda")
