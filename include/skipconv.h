@@ -505,6 +505,90 @@ int skipconv_attend_workspace(const skipconv_cache* c, const skipconv_attend* a,
 int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, void* workspace,
                           size_t workspace_bytes, void* stream);
 
+/* ---- the cache in 4 bits, and keeping a cache short ----
+ *
+ * The cache above held in codes of 4 bits: a third of the bf16 cache's bytes
+ * (5 bits an element). A head's elements lie in groups of 32, the last of which
+ * may be shorter (ceil(head_dim / 32) groups). Of a skipconv_cache for it,
+ * k_pages and v_pages hold the codes: a row (token and key head) is 16 bytes a
+ * group, element e in bits 0..3 (e even) or 4..7 of byte e / 2, and the strides
+ * count BYTES; `dtype` is that of the new tokens and queries. Beside them, for
+ * each row, a pair (scale, minimum) of fp16 a group. A code c stands for
+ *   fl16(minimum + c * scale),
+ * one rounding to fp16; every call below reads that value. */
+typedef struct skipconv_packing {
+  void* k_scales;                     /* device, 4-byte aligned: pages x kv_heads x page_size x groups x 2, fp16 */
+  void* v_scales;
+  int64_t ks_page, ks_head, ks_slot;  /* in fp16 elements, even */
+  int64_t vs_page, vs_head, vs_slot;
+} skipconv_packing;
+
+/* skipconv_cache_append into such a cache. Per group, on its elements in fp32
+ * (keys turned in 64 bits and rounded once to fp32):
+ *   y = clamp(x, +-32768), minimum = fl16(min y),
+ *   scale = fl16(max(0, (max y - minimum) / 15)),
+ *   code = clamp(rint((y - minimum) / scale), 0, 15), 0 where scale is 0;
+ * an element that is not finite makes its group NaN. */
+int skipconv_packed_append(const skipconv_cache* c, const skipconv_packing* s, const skipconv_append* a, void* stream);
+
+/* skipconv_cache_attend over such a cache: the same masks, batches, outputs
+ * and lse. Values are taken exactly, queries exactly (fp32: to 22 bits of the
+ * row's largest element); scores, sums and outputs are formed in 32 bits, and for bf16 the
+ * exponentials are rounded to fp16 for the product with v. Scales that make values
+ * infinite (append writes none): a row that sees one may get NaN in its place. */
+int skipconv_packed_attend_workspace(const skipconv_cache* c, const skipconv_attend* a, size_t* bytes);
+int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, const skipconv_attend* a, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* The values of pages list[0 .. count) (device, int32), exactly, as fp16: k and v
+ * count x kv_heads x page_size x head_dim, contiguous, 16-byte aligned. Zeros for a
+ * number outside the cache. Of c only the pages are looked at. */
+int skipconv_packed_unpack(const skipconv_cache* c, const skipconv_packing* s, const int32_t* list, int64_t count,
+                           void* k, void* v, void* stream);
+
+/* Accumulated attention weight. weights[page][key head][slot] of each token l of
+ * a sequence that has new tokens becomes
+ *   decay * weights + sum over its rows (new token i, query head h of the key
+ *   head) that see l of exp(scale q . k_l - lse[i][h]),
+ * for the new tokens themselves the sum alone (so their slots need no clearing). Masks
+ * as in skipconv_cache_attend, whose lse this takes (rows with lse = -inf
+ * give nothing). s: NULL for a float cache. Sums are formed in 32 bits in a fixed
+ * order: equal calls give equal bits. Tokens whose page number is outside the cache are
+ * left out. max_new: as in skipconv_attend. */
+typedef struct skipconv_weigh {
+  const void* q;         /* tokens x q_heads x head_dim, 16-byte aligned with strides of whole 16 bytes */
+  const float* lse;      /* tokens x q_heads */
+  float* weights;        /* pages x kv_heads x page_size */
+  int64_t q_token, q_head;
+  int32_t q_heads;       /* a multiple of kv_heads */
+  int32_t causal;        /* 0 or 1 */
+  int32_t window;
+  float scale;           /* > 0, finite */
+  float decay;           /* finite */
+  int32_t max_new;
+} skipconv_weigh;
+int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, const skipconv_weigh* w, void* stream);
+
+/* Eviction. Of each sequence and key head, min(kv_len, keep) tokens stay: the last
+ * `recent` ones, and of the others those of the largest weights (of equal
+ * weights the earlier ones; a NaN is larger than all). In their order they become
+ * tokens 0, 1, ... of the sequence in the pages of `into` (batch x
+ * into_width), keys, values and weights; key heads keep tokens of their own. kept (batch x
+ * kv_heads x keep) receives their positions, ascending, then -1, and lengths (batch)
+ * how many they are. s: NULL for a float cache. Tokens that have no page in the
+ * cache count less than any weight, and what has none on either side is not moved. The
+ * pages of `into` must hold no token of the batch and be different ones: rows
+ * move in any order. Of c's batch, row_start is not looked at (it may be NULL). */
+typedef struct skipconv_evict {
+  float* weights;        /* pages x kv_heads x page_size */
+  const int32_t* into;   /* device, batch x into_width */
+  int32_t* lengths;
+  int32_t* kept;
+  int32_t into_width;    /* >= 1, with room for the kept tokens: min(keep, table_width * page_size) */
+  int32_t keep, recent;  /* >= 1; 0..keep */
+} skipconv_evict;
+int skipconv_cache_evict(const skipconv_cache* c, const skipconv_packing* s, const skipconv_evict* e, void* stream);
+
 /* ---- kernel timing (benchmarks) ----
  * Time kernel by kernel, with HIP events recorded on the step's stream, every
  * `every`-th step (every >= 1) of the following steps, for up to `frames`

@@ -1,0 +1,221 @@
+// Entry points of the cache in 4 bits, of accumulated attention weight and of eviction: checks of the descriptions, the choice of kernels.
+#include "sc_attend_checks.h"
+#include "sc_packed.h"
+
+using namespace sc;
+
+namespace {
+
+constexpr int64_t kMostGroups = (1 << 22) - 1;  // workgroups of a launch: 1024 threads each stay under 2^32
+
+int check_packing(const skipconv_cache* c, const skipconv_packing* s, bool pointers) {
+  for (int64_t x : {stride_of(c->pages, s->ks_page), stride_of(c->kv_heads, s->ks_head), stride_of(c->page_size, s->ks_slot),
+                    stride_of(c->pages, s->vs_page), stride_of(c->kv_heads, s->vs_head), stride_of(c->page_size, s->vs_slot)})
+    if (x < 0 || x % 2 != 0) return invalid("packing: strides must be >= 0 and even");
+  if (!pointers) return SKIPCONV_OK;
+  if (!s->k_scales || !s->v_scales) return invalid("packing: NULL pointer");
+  if (((uintptr_t)s->k_scales | (uintptr_t)s->v_scales) % 4 != 0) return invalid("packing: the scales must be 4-byte aligned");
+  return SKIPCONV_OK;
+}
+
+void fill_packing(ScaleView* v, const skipconv_cache* c, const skipconv_packing* s) {
+  v->k = static_cast<char*>(s->k_scales);
+  v->v = static_cast<char*>(s->v_scales);
+  v->k_page = 2 * stride_of(c->pages, s->ks_page), v->k_head = 2 * stride_of(c->kv_heads, s->ks_head), v->k_slot = 2 * stride_of(c->page_size, s->ks_slot);
+  v->v_page = 2 * stride_of(c->pages, s->vs_page), v->v_head = 2 * stride_of(c->kv_heads, s->vs_head), v->v_slot = 2 * stride_of(c->page_size, s->vs_slot);
+}
+
+// The kernel and the cut of a launch, from the shapes alone (the lengths are on the device).
+struct PackedPlan {
+  bool few;
+  int log_rows, target, min_chunk, slack, units, slots;
+  size_t part_o, part_ml;
+};
+
+int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p) {
+  const int group = a->q_heads / c->kv_heads;
+  const int64_t rows = c->tokens * group;  // of one key head
+  const int64_t most = a->max_new > 0 ? std::min<int64_t>(a->max_new, c->tokens) : c->tokens;
+  const int64_t room = (int64_t)c->table_width * c->page_size;
+  const int64_t reach = std::min(room, a->window < 0 ? room : (int64_t)a->window + most);  // keys that an item may have
+  const auto items = [&](int log_rows) { return ((rows >> log_rows) + std::min<int64_t>(c->batch, c->tokens)) * c->kv_heads; };
+  p->few = most * group <= 32;
+  p->log_rows = p->few ? 4 : 6 + packed_many_blocks_log(elem_of(c), c->head_dim);
+  int64_t units = items(p->log_rows);
+  // Workgroups that share keys: `want`, or as many as all items' keys are least shares.
+  const auto shares = [&](int want) {
+    const int64_t tiles = (reach + 2 * kPackedKeys - 2) / kPackedKeys;
+    return (int)std::min<int64_t>(want, units * ((tiles + p->min_chunk - 1) / p->min_chunk));
+  };
+  if (p->few) {
+    p->min_chunk = 2 * kPackedFewWaves;
+    p->target = reach <= 4 * kPackedKeys * kPackedFewWaves ? 0 : shares(256);
+    p->slack = 0;
+  } else {
+    p->min_chunk = 256 / kPackedKeys;
+    p->target = units < 512 && reach > 3 * 256 ? shares(512) : 0;
+    p->slack = p->target ? 256 / kPackedKeys : 0;
+  }
+  p->slots = 2 * p->target;
+  if (p->target) units = p->target;
+  if (units > kMostGroups) return fail(SKIPCONV_E_UNSUPPORTED, "attend: too many rows");
+  p->units = (int)units;
+  const size_t parts = (size_t)p->slots << p->log_rows;
+  p->part_o = parts * c->head_dim * 4;
+  p->part_ml = parts * 2 * 4;
+  return SKIPCONV_OK;
+}
+
+// Every lane's row of a 16-key block lies in the block's page, at an offset of 31 bits.
+bool whole_pages(const CacheView& c, const ScaleView& s) {
+  const int64_t slot = std::max(std::max(c.k_slot, c.v_slot), std::max(s.k_slot, s.v_slot));
+  return c.page_size % 16 == 0 && 15 * slot < (1ll << 31);
+}
+
+int check_weigh(const skipconv_cache* c, const skipconv_weigh* w) {
+  if (w->q_heads < 1 || w->q_heads % c->kv_heads != 0) return invalid("weigh: q_heads must be a multiple of kv_heads");
+  if (c->tokens > kMostRows / w->q_heads) return fail(SKIPCONV_E_UNSUPPORTED, "weigh: too many rows");
+  if (w->causal != 0 && w->causal != 1) return invalid("weigh: causal must be 0 or 1");
+  if (!(w->scale > 0.0f) || !std::isfinite(w->scale)) return invalid("weigh: scale must be positive and finite");
+  if (!std::isfinite(w->decay)) return invalid("weigh: decay must be finite");
+  if (w->max_new < 0) return invalid("weigh: max_new must be >= 0");
+  return SKIPCONV_OK;
+}
+
+int check_any_cache(const skipconv_cache* c, const skipconv_packing* s) {
+  if (int e = check_cache(c, true, s ? 1 : elem_of(c))) return e;
+  return s ? check_packing(c, s, true) : SKIPCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int skipconv_packed_append(const skipconv_cache* c, const skipconv_packing* s, const skipconv_append* a, void* stream) {
+  if (!c || !s || !a) return invalid("append: NULL description");
+  if (int e = check_any_cache(c, s)) return e;
+  PackParams p = {};
+  bool wide;
+  if (int e = take_append(c, a, &p.r, &wide)) return e;
+  if (p.r.tokens == 0) return SKIPCONV_OK;
+  if (c->tokens > 4 * kMostGroups) return fail(SKIPCONV_E_UNSUPPORTED, "append: too many rows");
+  fill_packing(&p.s, c, s);
+  return hip_result(launch_pack(p, c->dtype, wide, static_cast<hipStream_t>(stream)), "append launch");
+}
+
+int skipconv_packed_attend_workspace(const skipconv_cache* c, const skipconv_attend* a, size_t* bytes) {
+  if (!c || !a || !bytes) return invalid("attend: NULL argument");
+  if (int e = check_cache(c, false, 1)) return e;
+  if (int e = check_attend(c, a)) return e;
+  PackedPlan p;
+  if (int e = plan_packed(c, a, &p)) return e;
+  *bytes = c->tokens == 0 || c->batch == 0 ? 0 : p.part_o + p.part_ml;
+  return SKIPCONV_OK;
+}
+
+int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, const skipconv_attend* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || !s || !a) return invalid("attend: NULL description");
+  if (int e = check_any_cache(c, s)) return e;
+  if (int e = check_attend(c, a)) return e;
+  if (c->tokens == 0 || c->batch == 0) return SKIPCONV_OK;
+  PackedAttendParams p = {};
+  if (int e = take_attend(c, a, &p.a)) return e;
+  PackedPlan plan;
+  if (int e = plan_packed(c, a, &plan)) return e;
+  if (plan.part_o + plan.part_ml > workspace_bytes)
+    return fail(SKIPCONV_E_SMALL_BUFFER, "attend: workspace smaller than skipconv_packed_attend_workspace");
+  if (plan.part_o && (!workspace || !on16(workspace))) return invalid("attend: workspace must be a 16-byte aligned pointer");
+  p.a.part_o = static_cast<float*>(workspace);
+  p.a.part_ml = plan.part_o ? p.a.part_o + plan.part_o / 4 : nullptr;
+  p.a.log_rows = plan.log_rows, p.a.keys = kPackedKeys, p.a.target = plan.target, p.a.min_chunk = plan.min_chunk, p.a.slack = plan.slack;
+  p.a.units = plan.units, p.a.slots = plan.slots;
+  fill_packing(&p.s, c, s);
+  p.groups = pack_groups(c->head_dim);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const int whole = whole_pages(p.a.c, p.s);
+  const bool half = c->dtype == SKIPCONV_BF16;
+  hipError_t e = plan.few ? (half ? launch_packed_few_bf16(p, whole, st) : launch_packed_few_f32(p, whole, st))
+                          : (half ? launch_packed_many_bf16(p, whole, st) : launch_packed_many_f32(p, whole, st));
+  if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), st);
+  return hip_result(e, "attend launch");
+}
+
+int skipconv_packed_unpack(const skipconv_cache* c, const skipconv_packing* s, const int32_t* list, int64_t count, void* k, void* v, void* stream) {
+  if (!c || !s) return invalid("unpack: NULL description");
+  skipconv_cache pages_only = *c;  // the batch is not looked at
+  pages_only.tokens = 0, pages_only.batch = 0, pages_only.table_width = 1;
+  if (int e = check_any_cache(&pages_only, s)) return e;
+  if (count < 0) return invalid("unpack: count must be >= 0");
+  if (count > (1ll << 40) / ((int64_t)c->kv_heads * c->page_size)) return fail(SKIPCONV_E_UNSUPPORTED, "unpack: too many rows");
+  if (count == 0) return SKIPCONV_OK;
+  if (!list || !k || !v) return invalid("unpack: NULL pointer");
+  if ((uintptr_t)list % 4 != 0 || !on16(k) || !on16(v)) return invalid("unpack: list must be 4-byte, k and v 16-byte aligned");
+  UnpackParams p = {};
+  fill_cache(&p.c, &pages_only);
+  fill_packing(&p.s, c, s);
+  p.list = list, p.count = count, p.kv_heads = c->kv_heads, p.dim = c->head_dim;
+  p.out[0] = static_cast<char*>(k), p.out[1] = static_cast<char*>(v);
+  return hip_result(launch_unpack(p, static_cast<hipStream_t>(stream)), "unpack launch");
+}
+
+int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, const skipconv_weigh* w, void* stream) {
+  if (!c || !w) return invalid("weigh: NULL description");
+  if (int e = check_any_cache(c, s)) return e;
+  if (int e = check_weigh(c, w)) return e;
+  if (c->tokens == 0 || c->batch == 0) return SKIPCONV_OK;
+  if (!w->q || !w->lse || !w->weights) return invalid("weigh: NULL pointer");
+  const int elem = elem_of(c);
+  WeighParams p = {};
+  p.q_token = stride_of(c->tokens, w->q_token), p.q_head = stride_of(w->q_heads, w->q_head);
+  if (!on16(w->q) || !whole16(p.q_token, elem) || !whole16(p.q_head, elem)) return invalid("weigh: q must be 16-byte aligned with strides of whole 16 bytes");
+  if (((uintptr_t)w->lse | (uintptr_t)w->weights) % 4 != 0) return invalid("weigh: lse or weights is not aligned to its elements");
+  fill_cache(&p.c, c);
+  if (s) {
+    fill_packing(&p.s, c, s);
+  } else {
+    p.c.k_page *= elem, p.c.k_head *= elem, p.c.k_slot *= elem;
+  }
+  p.q = static_cast<const char*>(w->q), p.lse = w->lse, p.weights = w->weights;
+  p.q_heads = w->q_heads, p.kv_heads = c->kv_heads, p.group = w->q_heads / c->kv_heads, p.dim = c->head_dim, p.groups = pack_groups(c->head_dim);
+  p.causal = w->causal, p.window = w->window < 0 ? -1 : w->window, p.packed = s != nullptr;
+  p.scale_log2 = (float)((double)w->scale * 1.4426950408889634), p.decay = w->decay;
+  p.tiles = ((int64_t)c->table_width * c->page_size + 31) / 32;
+  const int64_t most = w->max_new > 0 ? std::min<int64_t>(w->max_new, c->tokens) : c->tokens;
+  return hip_result(launch_weigh(p, c->dtype, most * p.group > 64, static_cast<hipStream_t>(stream)), "weigh launch");
+}
+
+int skipconv_cache_evict(const skipconv_cache* c, const skipconv_packing* s, const skipconv_evict* e, void* stream) {
+  if (!c || !e) return invalid("evict: NULL description");
+  skipconv_cache no_rows = *c;  // the new tokens are not looked at
+  no_rows.tokens = 0;
+  if (!no_rows.row_start) no_rows.row_start = c->kv_len;
+  if (int x = check_any_cache(&no_rows, s)) return x;
+  if (e->keep < 1) return invalid("evict: keep must be >= 1");
+  if (e->recent < 0 || e->recent > e->keep) return invalid("evict: recent must be 0..keep");
+  if (e->into_width < 1) return invalid("evict: into_width must be >= 1");
+  const int64_t room = (int64_t)c->table_width * c->page_size;
+  if ((int64_t)e->into_width * c->page_size < std::min<int64_t>(e->keep, room)) return invalid("evict: into has no room for the kept tokens");
+  if (c->batch == 0) return SKIPCONV_OK;
+  if (!e->weights || !e->into || !e->lengths || !e->kept) return invalid("evict: NULL pointer");
+  if (((uintptr_t)e->weights | (uintptr_t)e->into | (uintptr_t)e->lengths | (uintptr_t)e->kept) % 4 != 0) return invalid("evict: a tensor is not aligned to its elements");
+  if ((int64_t)c->batch * c->kv_heads > kMostGroups / (std::min<int64_t>(e->keep, room) / 64 + 1)) return fail(SKIPCONV_E_UNSUPPORTED, "evict: too many rows");
+  EvictParams p = {};
+  fill_cache(&p.c, &no_rows);
+  const int64_t unit = s ? 1 : elem_of(c);
+  const int row = s ? pack_groups(c->head_dim) * 16 : c->head_dim * elem_of(c);
+  p.part[0] = {p.c.k, p.c.k_page * unit, p.c.k_head * unit, p.c.k_slot * unit, row / 16, 16};
+  p.part[1] = {p.c.v, p.c.v_page * unit, p.c.v_head * unit, p.c.v_slot * unit, row / 16, 16};
+  p.parts = 2;
+  if (s) {
+    ScaleView v;
+    fill_packing(&v, c, s);
+    p.part[2] = {v.k, v.k_page, v.k_head, v.k_slot, pack_groups(c->head_dim), 4};
+    p.part[3] = {v.v, v.v_page, v.v_head, v.v_slot, pack_groups(c->head_dim), 4};
+    p.parts = 4;
+  }
+  p.weights = e->weights, p.into = e->into, p.lengths = e->lengths, p.kept = e->kept;
+  p.kv_heads = c->kv_heads, p.into_width = e->into_width, p.keep = e->keep, p.recent = e->recent;
+  return hip_result(launch_evict(p, static_cast<hipStream_t>(stream)), "evict launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,49 @@
+// Device-side helpers of the kernels on the cache in 4 bits (gfx950 only): codes to fp16 values, masks on those.
+#pragma once
+
+#include "sc_attend_device.h"
+#include "sc_packed.h"
+
+#pragma clang fp contract(off)
+
+namespace sc {
+
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ uint32_t bits_of(half2 v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ half2 half2_of(uint32_t v) { return __builtin_bit_cast(half2, v); }
+
+// fp16 round-to-nearest-even of two floats, packed.
+__device__ __forceinline__ uint32_t pack2h(float a, float b) { return bits_of(__builtin_convertvector(floatx2{a, b}, half2)); }
+
+// Of a word whose 16-bit halves hold a code each in bits 0..3 (4..7): the codes as fp16. An fp16 number with the code in its mantissa's last
+// bits is 1024 + code (in bits 4..7 and exponent 6: 64 + code), exactly, so one logical operation and one packed addition make two.
+__device__ __forceinline__ half2 codes_low(uint32_t w) { return half2_of((w & 0x000f000fu) | 0x64006400u) + half2{-1024.0f16, -1024.0f16}; }
+__device__ __forceinline__ half2 codes_high(uint32_t w) { return half2_of((w & 0x00f000f0u) | 0x54005400u) + half2{-64.0f16, -64.0f16}; }
+
+// The values of two codes: one rounding, as the format has it.
+__device__ __forceinline__ uint32_t values2(half2 codes, half2 scale, half2 low) { return bits_of(__builtin_elementwise_fma(codes, scale, low)); }
+
+// (a's, b's) scale, and minimum, of two (scale, minimum) words.
+__device__ __forceinline__ half2 scales2(uint32_t a, uint32_t b) { return half2_of(__builtin_amdgcn_perm(b, a, 0x05040100u)); }
+__device__ __forceinline__ half2 lows2(uint32_t a, uint32_t b) { return half2_of(__builtin_amdgcn_perm(b, a, 0x07060302u)); }
+
+// The eight values of a word of codes, in the order 0 4 1 5 2 6 3 7 (what one mask leaves side by side). pair: its (scale, minimum).
+__device__ __forceinline__ half8 values8(uint32_t w, uint32_t pair) {
+  const half2 s = scales2(pair, pair), m = lows2(pair, pair);
+  const uint4 v{values2(codes_low(w), s, m), values2(codes_high(w), s, m), values2(codes_low(w >> 8), s, m), values2(codes_high(w >> 8), s, m)};
+  return __builtin_bit_cast(half8, v);
+}
+
+// Of two packed fp16 values those outside the mask become zero, and so do those that are infinite or NaN, which set *odd.
+__device__ __forceinline__ uint32_t finite2h(uint32_t v, uint32_t mask, int* odd) {
+  v &= mask;
+  uint32_t f = v;
+  if ((v & 0x7c00u) == 0x7c00u) f &= 0xffff0000u;
+  if ((v & 0x7c000000u) == 0x7c000000u) f &= 0x0000ffffu;
+  if (f != v) *odd = 1;
+  return f;
+}
+
+}  // namespace sc

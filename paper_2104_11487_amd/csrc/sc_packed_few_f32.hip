@@ -1,0 +1,8 @@
+// Attention over a paged cache in 4 bits, few rows, fp32 (sc_packed_attend.h).
+#include "sc_packed_attend.h"
+
+namespace sc {
+
+hipError_t launch_packed_few_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream) { return launch_packed_dim<1, 1, 2, false>(p, whole_pages, stream); }
+
+}  // namespace sc

@@ -69,6 +69,22 @@ class skipconv_attend(ctypes.Structure):
                    ("max_new", ctypes.c_int32)])
 
 
+class skipconv_packing(ctypes.Structure):
+    _fields_ = ([("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+                + [(f"{t}s_{d}", ctypes.c_int64) for t in "kv" for d in ("page", "head", "slot")])
+
+
+class skipconv_weigh(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "lse", "weights")] + [("q_token", ctypes.c_int64), ("q_head", ctypes.c_int64)]
+                + [("q_heads", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float),
+                   ("decay", ctypes.c_float), ("max_new", ctypes.c_int32)])
+
+
+class skipconv_evict(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("weights", "into", "lengths", "kept")]
+                + [("into_width", ctypes.c_int32), ("keep", ctypes.c_int32), ("recent", ctypes.c_int32)])
+
+
 class SkipConvError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"skipconv error {code}: {msg}")
@@ -117,6 +133,18 @@ _SIGS = {
                                                  ctypes.POINTER(ctypes.c_size_t)]),
     "skipconv_cache_attend": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_attend), _P,
                                              ctypes.c_size_t, _P]),
+    "skipconv_packed_append": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_packing),
+                                              ctypes.POINTER(skipconv_append), _P]),
+    "skipconv_packed_attend_workspace": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_attend),
+                                                        ctypes.POINTER(ctypes.c_size_t)]),
+    "skipconv_packed_attend": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_packing),
+                                              ctypes.POINTER(skipconv_attend), _P, ctypes.c_size_t, _P]),
+    "skipconv_packed_unpack": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_packing), _P, ctypes.c_int64,
+                                              _P, _P, _P]),
+    "skipconv_cache_weigh": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_packing),
+                                            ctypes.POINTER(skipconv_weigh), _P]),
+    "skipconv_cache_evict": (ctypes.c_int, [ctypes.POINTER(skipconv_cache), ctypes.POINTER(skipconv_packing),
+                                            ctypes.POINTER(skipconv_evict), _P]),
     "skipconv_timing_begin": (ctypes.c_int, [_P, ctypes.c_int, ctypes.c_int]),
     "skipconv_timing_read": (ctypes.c_int, [_P, _P, ctypes.POINTER(ctypes.c_double),
                                             ctypes.POINTER(ctypes.c_int), _P, ctypes.c_int]),

@@ -1,5 +1,6 @@
-"""Attention of a stream's new tokens over its earlier ones: rotary positions with several axes, a paged
-cache of keys and values, and attention over it (include/skipconv.h, the C names; here also torch-facing classes).
+"""Attention of a stream's new tokens over its earlier ones: rotary positions with several axes, a paged cache of keys and values (in the
+tokens' type or in 4 bits), attention over it, and eviction by the attention that tokens received (include/skipconv.h, the C names; here
+also torch-facing classes).
 
 A 1 x 1 ``SkipConv`` layer's activation output, N x H x W x (heads * head_dim), viewed as
 N*H*W x heads x head_dim, is a tensor of tokens that these calls take as it lies. Work is enqueued on the current torch
@@ -11,6 +12,14 @@ autograd; the other calls record no graph and refuse tensors that require a grad
     batch = CacheBatch(page_table, row_start, kv_len, max_new=64 * 64)
     q = cache.append(k, v, batch, rotary=rotary, pos=pos, q=q)
     out = cache.attend(q, batch, causal=False)
+
+A long stream's cache is a PackedCache, in 4 bits, and is kept short by eviction:
+
+    cache = PackedCache.empty(pages=256, page_size=64, kv_heads=2, head_dim=64)
+    out, lse = cache.attend(q, batch, causal=False, return_lse=True)
+    cache.weigh(q, lse, batch, weights, causal=False)                      # weights: float32, pages x kv_heads x page_size
+    lengths, kept = cache.evict(weights, batch, other_pages, keep=4096, recent=256)
+    batch = CacheBatch(other_pages, row_start, lengths, max_new=64 * 64)
 """
 from __future__ import annotations
 
@@ -28,6 +37,7 @@ _MOST = 0x7fffffff  # of a description's 32-bit fields, which keep the low bits 
 
 skipconv_rotary, skipconv_cache = _S.skipconv_rotary, _S.skipconv_cache
 skipconv_append, skipconv_attend = _S.skipconv_append, _S.skipconv_attend
+skipconv_packing, skipconv_weigh, skipconv_evict = _S.skipconv_packing, _S.skipconv_weigh, _S.skipconv_evict
 
 
 # ------------------------------------------------------------------ C names --
@@ -50,6 +60,33 @@ def skipconv_attend_workspace(c: skipconv_cache, a: skipconv_attend) -> int:
 
 def skipconv_cache_attend(c: skipconv_cache, a: skipconv_attend, workspace_ptr: Optional[int], workspace_bytes: int, stream: int) -> None:
     _S._check(_S.lib().skipconv_cache_attend(ctypes.byref(c), ctypes.byref(a), workspace_ptr, workspace_bytes, stream))
+
+
+def skipconv_packed_append(c: skipconv_cache, s: skipconv_packing, a: skipconv_append, stream: int) -> None:
+    _S._check(_S.lib().skipconv_packed_append(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), stream))
+
+
+def skipconv_packed_attend_workspace(c: skipconv_cache, a: skipconv_attend) -> int:
+    n = ctypes.c_size_t()
+    _S._check(_S.lib().skipconv_packed_attend_workspace(ctypes.byref(c), ctypes.byref(a), ctypes.byref(n)))
+    return n.value
+
+
+def skipconv_packed_attend(c: skipconv_cache, s: skipconv_packing, a: skipconv_attend, workspace_ptr: Optional[int], workspace_bytes: int,
+                           stream: int) -> None:
+    _S._check(_S.lib().skipconv_packed_attend(ctypes.byref(c), ctypes.byref(s), ctypes.byref(a), workspace_ptr, workspace_bytes, stream))
+
+
+def skipconv_packed_unpack(c: skipconv_cache, s: skipconv_packing, list_ptr: int, count: int, k_ptr: int, v_ptr: int, stream: int) -> None:
+    _S._check(_S.lib().skipconv_packed_unpack(ctypes.byref(c), ctypes.byref(s), list_ptr, count, k_ptr, v_ptr, stream))
+
+
+def skipconv_cache_weigh(c: skipconv_cache, s: Optional[skipconv_packing], w: skipconv_weigh, stream: int) -> None:
+    _S._check(_S.lib().skipconv_cache_weigh(ctypes.byref(c), None if s is None else ctypes.byref(s), ctypes.byref(w), stream))
+
+
+def skipconv_cache_evict(c: skipconv_cache, s: Optional[skipconv_packing], e: skipconv_evict, stream: int) -> None:
+    _S._check(_S.lib().skipconv_cache_evict(ctypes.byref(c), None if s is None else ctypes.byref(s), ctypes.byref(e), stream))
 
 
 # ------------------------------------------------------------ torch classes --
@@ -229,38 +266,25 @@ class CacheBatch:
         self._width = page_table.shape[1]
 
 
-class PagedCache:
-    """Keys and values of earlier tokens in pages.
+class _Cache:
+    """What the caches share: descriptions, and the calls on them. A subclass sets the pages' tensors and the library's functions."""
+    pages, kv_heads, page_size, head_dim = map(_fixed, ("_pages", "_kv_heads", "_page_size", "_head_dim"))
+    dtype, device = map(_fixed, ("_dtype", "_device"))
 
-    k_pages, v_pages: GPU tensors, pages x kv_heads x page_size x head_dim (views of another order are taken as they lie), float32 or
-    bfloat16, 16-byte aligned rows; the caller owns them and the page numbers. Other pages take another cache.
-    """
-    k_pages, v_pages, pages, kv_heads = map(_fixed, ("_k_pages", "_v_pages", "_pages", "_kv_heads"))
-    page_size, head_dim, dtype, device = map(_fixed, ("_page_size", "_head_dim", "_dtype", "_device"))
-
-    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
-        _need(k_pages.dim() == 4 and k_pages.is_cuda and k_pages.dtype in _DTYPE, "k_pages must be a 4-d float32 or bfloat16 GPU tensor")
-        _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device,
-              "v_pages must match k_pages in shape, dtype and device")
-        _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "the pages' last dimension must be packed")
-        self._k_pages, self._v_pages = self._both = k_pages, v_pages
-        self._pages, self._kv_heads, self._page_size, self._head_dim = k_pages.shape
-        self._dtype, self._device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
+    def _describe(self, k: torch.Tensor, v: torch.Tensor, tensors, packing, append, attend, workspace):
+        """k, v: what the C description's pages are; tensors: all that a call may write; packing: a reference to the C packing, or None."""
+        self._tensors = tensors
         c = skipconv_cache()
-        c.k_pages, c.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
-        c.k_page, c.k_head, c.k_slot = k_pages.stride()[:3]
-        c.v_page, c.v_head, c.v_slot = v_pages.stride()[:3]
+        c.k_pages, c.v_pages = k.data_ptr(), v.data_ptr()
+        c.k_page, c.k_head, c.k_slot = k.stride()[:3]
+        c.v_page, c.v_head, c.v_slot = v.stride()[:3]
         c.pages, c.page_size, c.kv_heads, c.head_dim, c.dtype = self._pages, self._page_size, self._kv_heads, self._head_dim, _DTYPE[self._dtype]
-        self._c, self._ref = c, ctypes.byref(c)
+        self._c, self._ref, self._packing = c, ctypes.byref(c), packing
+        self._refs = (self._ref,) if packing is None else (self._ref, packing)
         lib = _S.lib()
-        self._append, self._attend = lib.skipconv_cache_append, lib.skipconv_cache_attend
+        self._append, self._attend, self._weigh, self._evict = append, attend, lib.skipconv_cache_weigh, lib.skipconv_cache_evict
+        self._workspace = workspace
         self._need = {}  # workspace bytes of attend(), by the shapes that decide them
-
-    @classmethod
-    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
-        """A cache of its own pages (not cleared: no token is read before it is appended)."""
-        shape = (pages, kv_heads, page_size, head_dim)
-        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
 
     def desc(self, batch: CacheBatch, tokens: int) -> skipconv_cache:
         """The C description for a batch (the object's own, valid until the next call of it)."""
@@ -271,6 +295,18 @@ class PagedCache:
         c.tokens, c.batch, c.table_width = tokens, batch._sequences, batch._width
         return c
 
+    def _graph(self, *tensors) -> bool:
+        """Whether gradients are recorded and one of these tensors, or of the pages, requires one."""
+        if not _recording():
+            return False
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                return True
+        for t in self._tensors:
+            if t.requires_grad:
+                return True
+        return False
+
     def append(self, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, rotary: Optional[Rotary] = None,
                pos: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None):
         """Write the new tokens' keys and values (tokens x kv_heads x head_dim) into the cache, the keys turned by `rotary` at
@@ -278,9 +314,7 @@ class PagedCache:
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, _, kt, kh = _heads_of(k, "k", None, self._kv_heads, dim, dtype, index)
         _, _, vt, vh = _heads_of(v, "v", tokens, self._kv_heads, dim, dtype, index)
-        if _recording() and (k.requires_grad or v.requires_grad or self._k_pages.requires_grad or self._v_pages.requires_grad
-                             or (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad)
-                             or (rotary is not None and rotary._freq.requires_grad)):
+        if self._graph(k, v, q, q_out, None if rotary is None else rotary._freq):
             _refuse_graph()
         a = skipconv_append(k.data_ptr(), v.data_ptr(), None, None, kt, kh, vt, vh)
         if rotary is not None:
@@ -304,8 +338,8 @@ class PagedCache:
         elif q_out is not None:
             raise ValueError("q_out without q")
         self.desc(batch, tokens)
-        _written(self._both)
-        _enqueue(self._append, index, self._ref, ctypes.byref(a))
+        _written(self._tensors)
+        _enqueue(self._append, index, *self._refs, ctypes.byref(a))
         return q_out
 
     def attend(self, q: torch.Tensor, batch: CacheBatch, causal: bool = True, window: int = -1, scale: Optional[float] = None,
@@ -319,8 +353,7 @@ class PagedCache:
         """
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
-        if _recording() and (q.requires_grad or self._k_pages.requires_grad or self._v_pages.requires_grad
-                             or (out is not None and out.requires_grad)):
+        if self._graph(q, out):
             _refuse_graph()
         if out is None:
             out = _like(q)
@@ -336,9 +369,136 @@ class PagedCache:
         shapes = (tokens, heads, batch._sequences, batch._width, window, batch.max_new)
         need = self._need.get(shapes)
         if need is None:
-            need = skipconv_attend_workspace(c, a)
+            need = self._workspace(c, a)
             if len(self._need) < 4096:
                 self._need[shapes] = need
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        _enqueue(self._attend, index, self._ref, ctypes.byref(a), ws.data_ptr() if need else None, need)
+        _enqueue(self._attend, index, *self._refs, ctypes.byref(a), ws.data_ptr() if need else None, need)
         return (out, lse) if return_lse else out
+
+    def _weights(self, weights: torch.Tensor) -> None:
+        shape = (self._pages, self._kv_heads, self._page_size)
+        if weights.dtype is not torch.float32 or weights.get_device() != self._index or weights.shape != shape or not weights.is_contiguous():
+            raise ValueError(f"weights must be a contiguous float32 tensor {list(shape)} on {self._device}")
+
+    def weigh(self, q: torch.Tensor, lse: torch.Tensor, batch: CacheBatch, weights: torch.Tensor, causal: bool = True, window: int = -1,
+              scale: Optional[float] = None, decay: float = 1.0) -> torch.Tensor:
+        """Adds the attention weight that each cached token received from the new tokens' queries to `weights` (float32, pages x kv_heads x
+        page_size), and returns it: decay times what it held, plus the sum over the query heads and the new tokens that see it of exp(score - lse);
+        a new token's own is set, so its slot needs no clearing. q, lse: what attend() took, and returned with return_lse; the mask and the
+        scale as there. Tokens of sequences without new ones stay as they are.
+        """
+        dim, dtype, index = self._head_dim, self._dtype, self._index
+        tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
+        if lse.dtype is not torch.float32 or lse.get_device() != index or lse.shape != (tokens, heads) or not lse.is_contiguous():
+            raise ValueError(f"lse must be a contiguous float32 tensor {[tokens, heads]} on {self._device}")
+        self._weights(weights)
+        if self._graph(q, lse, weights):
+            _refuse_graph()
+        w = skipconv_weigh(q.data_ptr(), lse.data_ptr(), weights.data_ptr(), qt, qh, heads, 1 if causal else 0,
+                           -1 if window < 0 else min(window, _MOST), dim ** -0.5 if scale is None else scale, decay, batch.max_new)
+        self.desc(batch, tokens)
+        _written((weights,))
+        _enqueue(self._weigh, index, self._ref, self._packing, ctypes.byref(w))
+        return weights
+
+    def evict(self, weights: torch.Tensor, batch: CacheBatch, into: torch.Tensor, keep: int, recent: int = 0):
+        """Keeps min(kv_len, keep) tokens of each sequence, for each key head its own: the last `recent` ones, and of the others those of
+        the largest weights (of equal ones the earlier). In their order they become the tokens of the sequence in the pages of `into`
+        (int32, sequences x width): keys, values and weights. These pages must be different ones, and hold no token of the batch.
+        Returns (lengths, kept): int32, the tokens of each sequence now, and their earlier positions, sequences x kv_heads x keep, -1 past
+        the last. What comes next is CacheBatch(into, row_start, lengths).
+        """
+        index = self._index
+        self._weights(weights)
+        _need(1 <= keep <= _MOST and 0 <= recent <= keep, "keep must be >= 1, and recent 0..keep")
+        n = batch._sequences
+        if into.dtype is not torch.int32 or into.get_device() != index or into.dim() != 2 or into.shape[0] != n or not into.is_contiguous():
+            raise ValueError(f"into must be a contiguous int32 tensor [{n}, width] on {self._device}")
+        if self._graph(weights):
+            _refuse_graph()
+        lengths = torch.empty(n, dtype=torch.int32, device=into.device)
+        kept = torch.empty((n, self._kv_heads, keep), dtype=torch.int32, device=into.device)
+        e = skipconv_evict(weights.data_ptr(), into.data_ptr(), lengths.data_ptr(), kept.data_ptr(), into.shape[1], keep, recent)
+        self.desc(batch, 0)
+        _written((*self._tensors, weights))
+        _enqueue(self._evict, index, self._ref, self._packing, ctypes.byref(e))
+        return lengths, kept
+
+
+class PagedCache(_Cache):
+    """Keys and values of earlier tokens in pages.
+
+    k_pages, v_pages: GPU tensors, pages x kv_heads x page_size x head_dim (views of another order are taken as they lie), float32 or
+    bfloat16, 16-byte aligned rows; the caller owns them and the page numbers. Other pages take another cache.
+    """
+    k_pages, v_pages = map(_fixed, ("_k_pages", "_v_pages"))
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
+        _need(k_pages.dim() == 4 and k_pages.is_cuda and k_pages.dtype in _DTYPE, "k_pages must be a 4-d float32 or bfloat16 GPU tensor")
+        _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == k_pages.device,
+              "v_pages must match k_pages in shape, dtype and device")
+        _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, "the pages' last dimension must be packed")
+        self._k_pages, self._v_pages = k_pages, v_pages
+        self._pages, self._kv_heads, self._page_size, self._head_dim = k_pages.shape
+        self._dtype, self._device, self._index = k_pages.dtype, k_pages.device, k_pages.get_device()
+        lib = _S.lib()
+        self._describe(k_pages, v_pages, (k_pages, v_pages), None, lib.skipconv_cache_append, lib.skipconv_cache_attend, skipconv_attend_workspace)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "PagedCache":
+        """A cache of its own pages (not cleared: no token is read before it is appended)."""
+        shape = (pages, kv_heads, page_size, head_dim)
+        return cls(torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device))
+
+
+class PackedCache(_Cache):
+    """A PagedCache in 4 bits: a third of the bytes, the same calls.
+
+    k_codes, v_codes: uint8 GPU tensors, pages x kv_heads x page_size x 16 * groups, where groups = ceil(head_dim / 32); k_scales, v_scales:
+    float16, pages x kv_heads x page_size x groups x 2 (views of another order are taken as they lie). Element e of a row is in the lower
+    (e even) or upper half of byte e // 2; with (scale, minimum) of its group of 32 elements, a code stands for minimum + code * scale,
+    rounded to float16. dtype: of the new tokens and queries. Elements are held between -32768 and 32768; one that is
+    not finite makes its group NaN.
+    """
+    k_codes, v_codes, k_scales, v_scales = map(_fixed, ("_k_codes", "_v_codes", "_k_scales", "_v_scales"))
+
+    def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, head_dim: int,
+                 dtype=torch.bfloat16):
+        _need(dtype in _DTYPE, "dtype must be float32 or bfloat16")
+        _need(head_dim >= 1, "head_dim must be >= 1")
+        groups = -(-head_dim // 32)
+        for x, name in ((k_codes, "k_codes"), (v_codes, "v_codes")):
+            _need(x.dim() == 4 and x.is_cuda and x.dtype == torch.uint8 and x.shape[3] == 16 * groups and x.stride(3) == 1,
+                  f"{name} must be a uint8 GPU tensor, pages x kv_heads x page_size x {16 * groups}, with a packed last dimension")
+        _need(v_codes.shape == k_codes.shape and v_codes.device == k_codes.device, "v_codes must match k_codes in shape and device")
+        for x, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+            _need(x.dtype == torch.float16 and x.device == k_codes.device and tuple(x.shape) == (*k_codes.shape[:3], groups, 2)
+                  and x.stride(4) == 1 and (groups == 1 or x.stride(3) == 2),
+                  f"{name} must be a float16 tensor {[*k_codes.shape[:3], groups, 2]} on the codes' device, its last two dimensions packed")
+        self._k_codes, self._v_codes, self._k_scales, self._v_scales = k_codes, v_codes, k_scales, v_scales
+        self._pages, self._kv_heads, self._page_size = k_codes.shape[:3]
+        self._head_dim, self._dtype = head_dim, dtype
+        self._device, self._index = k_codes.device, k_codes.get_device()
+        self._scales = skipconv_packing(k_scales.data_ptr(), v_scales.data_ptr(), *k_scales.stride()[:3], *v_scales.stride()[:3])
+        lib = _S.lib()
+        self._describe(k_codes, v_codes, (k_codes, v_codes, k_scales, v_scales), ctypes.byref(self._scales), lib.skipconv_packed_append,
+                       lib.skipconv_packed_attend, skipconv_packed_attend_workspace)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda") -> "PackedCache":
+        """A cache of its own pages (not cleared: no token is read before it is appended)."""
+        shape, groups = (pages, kv_heads, page_size), -(-head_dim // 32)
+        codes = [torch.empty((*shape, 16 * groups), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.empty((*shape, groups, 2), dtype=torch.float16, device=device) for _ in range(2)]
+        return cls(*codes, *scales, head_dim, dtype)
+
+    def unpack(self, pages: torch.Tensor):
+        """The values of the pages whose numbers an int32 GPU tensor of any shape holds (a page table, say), exactly: (k, v), float16, the
+        shape x kv_heads x page_size x head_dim. Zeros for a number outside the cache."""
+        index = self._index
+        if pages.dtype is not torch.int32 or pages.get_device() != index or not pages.is_contiguous():
+            raise ValueError(f"pages must be a contiguous int32 tensor on {self._device}")
+        k, v = (torch.empty((*pages.shape, self._kv_heads, self._page_size, self._head_dim), dtype=torch.float16, device=pages.device) for _ in range(2))
+        _enqueue(_S.lib().skipconv_packed_unpack, index, *self._refs, pages.data_ptr(), pages.numel(), k.data_ptr(), v.data_ptr())
+        return k, v

@@ -1,0 +1,915 @@
+"""The cache in 4 bits, attention over it, accumulated attention weight and eviction on the GPU, against the oracle in 64 bits.
+
+What a cache in 4 bits holds is compared bit for bit: codes, scales and the values they stand for. Bounds of attention, per element (u = 2^-24;
+A the weighted mean of |v|, V the largest |v|, Q the largest sum of |q k| * scale, S the largest |score|, n keys):
+  scores    fp32 queries are two parts, off by 4 u of each element: (2 dim + 6) u Q;
+  exponents 4 u (S + 1); sums n u, once in the numerator and once in the denominator;
+  exponentials for the product: fp32 two parts, 4 u each; bf16 one, 2^-11; those under 2^-21 of the largest up to 2^-32 V more each;
+  the output's rounding: bf16 2^-8 of it, a quarter more for products of these terms.
+Accumulated weight: a term is off by its exponent's error, (2 dim + 2) u Q + 4 u (S + |lse| + 1), sums by the number of rows times u.
+Slots of the cache that hold no token are garbage (codes 255, scales NaN and infinite), entries of the page table that hold no page are wild.
+"""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from oracle import packed_cache_oracle as P  # noqa: E402
+from oracle import stream_attention_oracle as O  # noqa: E402
+from paper_2104_11487_amd import skipconv as S  # noqa: E402
+from paper_2104_11487_amd import stream_attention as A  # noqa: E402
+from parity_util import say  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _rng(seed):
+    return np.random.Generator(np.random.PCG64(seed))
+
+
+def _gpu(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def _stored(x, dtype):
+    """A GPU tensor of x in the dtype, and its values in 64 bits."""
+    t = torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(DT[dtype])
+    return t.cuda(), t.double().numpy()
+
+
+def _laid(x, layout):
+    """The GPU tensor tokens x heads x dim in another memory layout."""
+    t, h, d = x.shape
+    if layout == "view":  # the middle of a wider projection
+        w = torch.full((t, h + 3, d), float("nan"), dtype=x.dtype, device="cuda")
+        w[:, 1:1 + h] = x
+        return w[:, 1:1 + h]
+    if layout == "heads":  # heads outermost
+        return x.transpose(0, 1).contiguous().transpose(0, 1)
+    if layout == "odd":  # rows that begin anywhere
+        w = torch.full((t * (h * d + 1) + 1,), float("nan"), dtype=x.dtype, device="cuda")
+        v = w[1:].as_strided((t, h, d), (h * d + 1, d, 1))
+        v.copy_(x)
+        return v
+    return x.contiguous()
+
+
+def _batch(rng, lens, page, spare=3, pages_first=0, width=None):
+    """Page table (wild where it holds no page), starts and lengths of sequences with (new, kv) tokens."""
+    held = [-(-kv // page) for _, kv in lens]
+    width = width or max(held + [1]) + 2
+    order = pages_first + rng.permutation(sum(held) + spare)
+    table = rng.choice(np.array([-1, -12345, 1 << 30, 2 ** 31 - 1]), (len(lens), width)).astype(np.int32)
+    at = 0
+    for b, n in enumerate(held):
+        table[b, :n] = order[at:at + n]
+        at += n
+    starts = np.concatenate([[0], np.cumsum([n for n, _ in lens])]).astype(np.int32)
+    return table, starts, np.array([kv for _, kv in lens], np.int32), pages_first + sum(held) + spare
+
+
+def _device(table, starts, lens, max_new=0):
+    return A.CacheBatch(_gpu(table), _gpu(starts), _gpu(lens), max_new=max_new)
+
+
+def _order(x, order):
+    """Pages as they lie in another memory order."""
+    return x.transpose(1, 2).contiguous().transpose(1, 2) if order == "slots" else x
+
+
+def _packed(codes, scales, dim, dtype, order="heads"):
+    """A cache of (k, v) codes and scales."""
+    return A.PackedCache(*(_order(_gpu(x), order) for x in (*codes, *scales)), dim, dtype=DT[dtype])
+
+
+def _held(cache):
+    """A cache's codes and scales: (k codes, v codes), (k scales' bits, v scales' bits)."""
+    codes = [x.cpu().numpy() for x in (cache.k_codes, cache.v_codes)]
+    return codes, [x.cpu().numpy() for x in (cache.k_scales, cache.v_scales)]
+
+
+def _same(a, b):
+    return np.array_equal(np.ascontiguousarray(a).view(np.uint8), np.ascontiguousarray(b).view(np.uint8))
+
+
+def _garbage(shape, groups):
+    """Codes and scales of pages that hold nothing: no finite value among them."""
+    codes, scales = np.full((*shape, 16 * groups), 255, np.uint8), np.full((*shape, groups, 2), np.nan, np.float16)
+    scales[..., ::2, :, :] = np.inf
+    return codes, scales
+
+
+# ------------------------------------------------------------------ append --
+
+# lens, q heads, kv heads, dim, pairs, adjacent, page, dtype, layout, order
+APPENDS = [
+    ([(1, 1)], 4, 2, 64, 32, False, 16, "bf16", "packed", "heads"),
+    ([(1, 40), (1, 17), (1, 16), (1, 1)], 8, 2, 128, 64, False, 16, "bf16", "packed", "heads"),
+    ([(5, 5), (0, 9), (17, 40), (0, 0), (1, 300)], 2, 1, 64, 31, False, 7, "bf16", "view", "slots"),
+    ([(196, 500), (3, 3)], 3, 3, 80, 32, True, 196, "f32", "packed", "heads"),
+    ([(30, 30), (2, 64)], 4, 4, 96, 48, True, 1, "bf16", "heads", "slots"),
+    ([(9, 33)], 6, 2, 40, 20, False, 5, "bf16", "odd", "heads"),
+    ([(1, 2)] * 130, 2, 1, 32, 16, False, 4, "f32", "packed", "heads"),
+    ([(700, 900), (400, 400)], 4, 2, 64, 32, False, 64, "bf16", "view", "heads"),
+    ([(4, 8)], 70, 20, 256, 100, False, 32, "bf16", "packed", "heads"),
+    ([(4, 8), (6, 6)], 2, 1, 8, 3, True, 3, "f32", "odd", "heads"),
+    ([(2000, 2100)], 3, 1, 168, 84, False, 32, "bf16", "packed", "heads"),
+]
+
+
+def _certain(x64):
+    """Whether 64-bit values surely round to the same fp32 number here and there. Angles stay under 3 * 5000 < 2^14: three products, two sums and the
+    reduction to a turn are off by 2^-53 * 2^14 each, under 2^-36 together, and a turned element by that much of its pair's size."""
+    d = 2.0 ** -36 * np.maximum(np.abs(x64).max(-1, keepdims=True), 1.0)
+    return (x64 - d).astype(np.float32) == (x64 + d).astype(np.float32)
+
+
+@pytest.mark.parametrize("mode", ["queries", "keys", "copy"])
+@pytest.mark.parametrize("case", APPENDS, ids=[f"{i}" for i in range(len(APPENDS))])
+def test_append(case, mode):
+    lens, heads, kv_heads, dim, pairs, adjacent, page, dtype, layout, order = case
+    say(f"[packed append] {case[1:]} {mode}")
+    rng = _rng(121 + dim + page)
+    table, starts, length, pages = _batch(rng, lens, page)
+    extra, groups = 3, -(-dim // 32)  # rows of no sequence
+    tokens = int(starts[-1]) + extra
+    k, k64 = _stored(rng.standard_normal((tokens, kv_heads, dim)) + 0.3, dtype)
+    v, v64 = _stored(rng.standard_normal((tokens, kv_heads, dim)) * 10.0 ** rng.integers(-4, 4, (tokens, 1, 1)), dtype)
+    q, q64 = _stored(rng.standard_normal((tokens, heads, dim)), dtype)
+    pos = rng.integers(0, 5000, (tokens, 3)).astype(np.int32)
+    freq = rng.random((3, pairs)).astype(np.float32)
+    rotary, at = A.Rotary(_gpu(freq), dim, "adjacent" if adjacent else "halves"), _gpu(pos)
+    old = [_garbage((pages, kv_heads, page), groups) for _ in range(2)]
+    cache = _packed([c for c, _ in old], [s for _, s in old], dim, dtype, order)
+    batch = _device(table, starts, length)
+    turn = dict(rotary=rotary, pos=at) if mode != "copy" else {}
+    q_out = torch.full((tokens, heads, dim), 7.0, dtype=DT[dtype], device="cuda")
+    got_q = cache.append(_laid(k, layout), _laid(v, layout), batch, **turn, **(dict(q=_laid(q, layout), q_out=q_out) if mode == "queries" else {}))
+    turned = O.rotate(k64, pos, freq.astype(np.float64), adjacent) if mode != "copy" else k64
+    sure = _certain(turned) if mode != "copy" else np.ones(turned.shape, bool)
+    sure[..., 2 * pairs:] = True
+    codes, scales = _held(cache)
+    for which, x, certain in ((0, turned, sure), (1, v64, np.ones(v64.shape, bool))):
+        new_codes, new_scales = P.pack(x.astype(np.float32))
+        want_c, want_s = old[which][0].copy(), old[which][1].copy()
+        skip = np.zeros(want_c.shape, bool)
+        for row, p, slot in O.places(table, starts, length, page, pages):
+            want_c[p, :, slot], want_s[p, :, slot] = new_codes[row], new_scales[row]
+            for g in range(groups):
+                doubt = ~certain[row, :, 32 * g:32 * g + 32].all(-1)
+                skip[p, doubt, slot, 16 * g:16 * g + 16] = True
+        assert skip.mean() < 0.25  # an element of size x is in doubt once in 2^11 x times, and one of 32 elements of size 0.1 makes a group so
+        assert np.array_equal(np.where(skip, 0, codes[which]), np.where(skip, 0, want_c))
+        ok = ~skip.reshape(*skip.shape[:-1], groups, 16).any(-1)
+        assert _same(scales[which][ok], want_s[ok])
+    if mode == "queries":
+        assert got_q is q_out
+        want = O.rotate(q64, pos, freq.astype(np.float64), adjacent)
+        first, second = O.partners(pairs, adjacent)
+        bound = np.zeros_like(want)
+        bound[..., first] = bound[..., second] = 8 * U * (np.abs(q64[..., first]) + np.abs(q64[..., second]))
+        if dtype == "bf16":
+            bound[..., :2 * pairs] += (2.0 ** -8 * np.abs(want) + 2.0 ** -8 * bound)[..., :2 * pairs]
+        assert (np.abs(q_out.double().cpu().numpy() - want) <= bound)[:-extra].all() and (q_out[-extra:] == 7.0).all()
+        inplace = q.clone()
+        assert cache.append(k, v, batch, **turn, q=inplace, q_out=inplace) is inplace
+        assert torch.equal(inplace[:-extra], q_out[:-extra]) and torch.equal(inplace[-extra:], q[-extra:])
+        again = _held(cache)
+        assert all(_same(a, b) for x, y in zip(again, (codes, scales)) for a, b in zip(x, y))
+    else:
+        assert got_q is None
+
+
+def test_append_leaves_out_what_has_no_place():
+    rng = _rng(122)
+    table = np.array([[1, 5, 0, 2]], np.int32)  # page 5 of 4 does not exist
+    (k, k64), (v, v64) = (_stored(rng.standard_normal((10, 2, 64)), "bf16") for _ in range(2))
+    for new, kv in ((10, 12), (10, 7), (10, 40)):  # over the missing page; from before the begin; past the table
+        starts, length = np.array([0, new], np.int32), np.array([kv], np.int32)
+        old = [_garbage((4, 2, 4), 2) for _ in range(2)]
+        cache = _packed([c for c, _ in old], [s for _, s in old], 64, "bf16")
+        cache.append(k, v, _device(table, starts, length))
+        codes, scales = _held(cache)
+        for which, x in ((0, k64), (1, v64)):
+            new_codes, new_scales = P.pack(x)
+            for row, p, slot in O.places(table, starts, length, 4, 4):
+                old[which][0][p, :, slot], old[which][1][p, :, slot] = new_codes[row], new_scales[row]
+            assert _same(codes[which], old[which][0]) and _same(scales[which], old[which][1])
+
+
+SPECIAL = {
+    "constant": np.full(64, 3.14159), "zeros": np.zeros(64), "minus zero": np.full(64, -0.0), "one spike": np.eye(1, 64, 5)[0] * 1000, "tiny": np.linspace(-1e-6, 1e-6, 64),
+    "subnormal": np.linspace(-1e-40, 1e-40, 64), "large": np.linspace(-30000, 32768, 64), "too large": np.linspace(-1e6, 1e6, 64), "all too large": np.full(64, 1e30),
+    "narrow": 1000 + np.linspace(0, 0.01, 64), "low rounds up": np.full(64, 1.0 + 2.0 ** -11 + 2.0 ** -14), "infinite": np.where(np.arange(64) == 40, np.inf, 1.0),
+    "minus infinite": np.where(np.arange(64) == 3, -np.inf, 1.0), "nan": np.where(np.arange(64) == 63, np.nan, np.arange(64)), "ties": np.arange(64) % 31 / 2.0,
+}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_what_is_held_of_special_rows(dtype):
+    rows = np.stack(list(SPECIAL.values()))[:, None]
+    x, x64 = _stored(rows, dtype)
+    n = len(rows)
+    cache = A.PackedCache.empty(1, 32, 1, 64, dtype=DT[dtype])
+    batch = _device(np.zeros((1, 1), np.int32), np.array([0, n], np.int32), np.array([n], np.int32))
+    cache.append(x, x, batch)
+    codes, scales = _held(cache)
+    want_c, want_s = P.pack(x64.astype(np.float32))
+    for i, name in enumerate(SPECIAL):
+        assert _same(codes[0][0, 0, i], want_c[i, 0]) and np.array_equal(np.isnan(scales[0][0, 0, i]), np.isnan(want_s[i, 0])), name
+        fine = ~np.isnan(want_s[i, 0])
+        assert _same(scales[0][0, 0, i][fine], want_s[i, 0][fine]) and _same(codes[1][0, 0, i], codes[0][0, 0, i]), name
+    k, _ = cache.unpack(torch.zeros(1, dtype=torch.int32, device="cuda"))
+    got, want = k[0, 0, :n].double().cpu().numpy(), P.values(want_c, want_s, 64)[:, 0]
+    assert np.array_equal(got, want, equal_nan=True)
+    # how far a value is from the element: half a step, and the roundings of minimum, scale and value to fp16
+    held = np.clip(x64[:, 0], -32768, 32768)
+    for i, name in enumerate(SPECIAL):
+        for g in (0, 1):
+            part, back = held[i, 32 * g:32 * g + 32], got[i, 32 * g:32 * g + 32]
+            if not np.isfinite(x64[i, 0, 32 * g:32 * g + 32]).all():
+                assert np.isnan(back).all(), name
+                continue
+            step = max((part.max() - part.min()) / 15, 0)
+            bound = 0.5 * step + 2.0 ** -11 * (2 * np.abs(part).max() + 16 * step) + 17 * 2.0 ** -25
+            assert (np.abs(back - part) <= bound).all(), name
+
+
+@pytest.mark.parametrize("dim", [8, 32, 40, 64, 80, 96, 128, 160, 256])
+def test_unpack(dim):
+    rng = _rng(123 + dim)
+    groups, shape = -(-dim // 32), (5, 3, 7)
+    codes = [rng.integers(0, 256, (*shape, 16 * groups)).astype(np.uint8) for _ in range(2)]
+    scales = [rng.integers(0, 1 << 16, (*shape, groups, 2)).astype(np.uint16).view(np.float16) for _ in range(2)]  # any bits at all
+    for order in ("heads", "slots"):
+        cache = _packed(codes, scales, dim, "bf16", order)
+        listed = np.array([[4, 0, 9], [-1, 2, 2]], np.int32)
+        got = cache.unpack(_gpu(listed))
+        for which in (0, 1):
+            want = P.values(codes[which], scales[which], dim)
+            there = (listed >= 0) & (listed < 5)
+            out = got[which].double().cpu().numpy()
+            assert out.shape == (2, 3, 3, 7, dim) and not out[~there].any()
+            assert np.array_equal(out[there], want[listed[there]], equal_nan=True)
+    assert cache.unpack(torch.empty(0, dtype=torch.int32, device="cuda"))[0].shape == (0, 3, 7, dim)
+
+
+# --------------------------------------------------------------- attention --
+
+def _filled(rng, lens, heads, kv_heads, dim, page, dtype, order="heads", gain=1.0, spoil=None, width=None):
+    """A cache whose sequences' slots are packed features, and what it holds in 64 bits."""
+    table, starts, length, pages = _batch(rng, lens, page, width=width)
+    groups = -(-dim // 32)
+    codes, scales = zip(*(_garbage((pages, kv_heads, page), groups) for _ in range(2)))
+    for b, (_, kv) in enumerate(lens):
+        for i in range(0, kv, page):
+            n = min(page, kv - i)
+            for which in (0, 1):
+                c, s = P.pack((0.5 * which + rng.standard_normal((kv_heads, n, dim))).astype(np.float32))
+                codes[which][table[b, i // page], :, :n], scales[which][table[b, i // page], :, :n] = c, s
+    if spoil:
+        spoil(codes, scales, table)
+    k64, v64 = (P.values(c, s, dim) for c, s in zip(codes, scales))
+    q, q64 = _stored(gain * rng.standard_normal((int(starts[-1]), heads, dim)), dtype)
+    return _packed(codes, scales, dim, dtype, order), k64, v64, q, q64, table, starts, length
+
+
+def _compare(out, lse, want, dtype, dim, largest):
+    o, l, b = want  # noqa: E741
+    got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    # an infinity (which append never writes) may come out as NaN, where its exponential, or a part of it, is zero
+    assert np.array_equal(np.isfinite(got), np.isfinite(o)) and np.isnan(got[np.isnan(o)]).all()
+    with np.errstate(invalid="ignore"):
+        q, s, n = (b[x][..., None] for x in ("size", "most", "count"))
+        bound = b["weight"] * (4 * (2 * dim + 6) * U * q + 16 * U * (s + 1) + 2 * n * U + 16 * U) + n * 2.0 ** -32 * largest
+        if dtype == "bf16":
+            bound = 1.25 * (bound + 2.0 ** -11 * b["weight"] + 2.0 ** -8 * np.abs(o))
+        fine = np.isfinite(o)
+        off = np.abs(got - o)
+        ok = off[fine] <= bound[fine]
+        assert ok.all(), f"{(~ok).sum()} of {ok.size} off, worst {np.max(off[fine] / np.maximum(bound[fine], 1e-30)):.3g} of the bound"
+    none = np.isneginf(l)
+    assert np.array_equal(np.isneginf(gl), none) and not got[none].any()
+    size = (2 * dim + 6) * U * b["size"] + (b["count"] + 16) * U + 8 * U * (b["most"] + np.abs(np.where(none, 0, l)))
+    sure = ~none & np.isfinite(l)
+    assert (np.abs(gl - l)[sure] <= size[sure]).all()
+
+
+def _largest(v64):
+    return np.abs(v64[np.isfinite(v64)]).max(initial=0.0)
+
+
+def _bits(x):
+    return x.view(torch.int16 if x.dtype == torch.bfloat16 else torch.int32)
+
+
+def _attend_both(cache, q, table, starts, length, **kw):
+    """The call with every hint about the new tokens; all must hold, and equal calls give equal bits."""
+    most = int(np.max(np.diff(starts), initial=0))
+    for hint in sorted({0, most, 1}):
+        batch = _device(table, starts, length, max_new=hint)
+        out, lse = cache.attend(q, batch, return_lse=True, **kw)
+        assert torch.equal(_bits(out), _bits(cache.attend(q, batch, **kw)))
+        yield hint, out, lse
+
+
+MASKS = [(True, -1), (False, -1), (True, 0), (True, 37), (False, 37), (True, 1000)]
+# lens, heads, kv heads, dim, page, dtype, order
+ATTENDS = [
+    ([(1, 1)], 1, 1, 8, 1, "bf16", "heads"),
+    ([(1, 77)], 4, 1, 64, 16, "bf16", "heads"),
+    ([(1, 64), (1, 65), (1, 1), (1, 200), (1, 31)], 8, 2, 128, 16, "bf16", "slots"),
+    ([(1, 3000)], 16, 2, 128, 64, "bf16", "heads"),
+    ([(5, 5), (0, 40), (17, 90), (0, 0), (40, 333)], 6, 3, 80, 7, "bf16", "heads"),
+    ([(3, 900), (2, 2)], 10, 2, 32, 3, "bf16", "slots"),
+    ([(130, 300)], 4, 1, 64, 64, "bf16", "heads"),
+    ([(70, 150), (33, 33)], 2, 2, 128, 16, "bf16", "slots"),
+    ([(20, 196), (5, 700)], 6, 2, 96, 196, "bf16", "heads"),
+    ([(25, 130)], 4, 2, 256, 32, "bf16", "heads"),
+    ([(40, 41)], 3, 1, 160, 5, "bf16", "heads"),
+    ([(1, 500), (2, 70)], 4, 2, 256, 16, "bf16", "heads"),
+    ([(1, 300), (1, 20)], 4, 2, 192, 16, "bf16", "heads"),
+    ([(1, 90), (30, 64)], 2, 2, 8, 16, "bf16", "heads"),
+    ([(6, 90), (50, 64)], 2, 1, 16, 48, "bf16", "slots"),
+    ([(1, 1), (1, 50)], 1, 1, 8, 1, "f32", "heads"),
+    ([(1, 900), (2, 64), (3, 17)], 8, 2, 80, 196, "f32", "slots"),
+    ([(100, 240), (0, 3), (9, 9)], 6, 3, 64, 16, "f32", "heads"),
+    ([(60, 90)], 2, 1, 128, 9, "f32", "heads"),
+    ([(30, 70), (1, 300)], 4, 2, 256, 32, "f32", "heads"),
+    ([(1, 333), (4, 4)], 8, 4, 256, 16, "f32", "heads"),
+    ([(33, 200)], 3, 3, 32, 64, "f32", "slots"),
+    ([(40, 100)], 2, 1, 192, 4, "f32", "heads"),
+    ([(5, 400)], 4, 1, 96, 8, "f32", "heads"),
+    ([(1, 9)] * 70 + [(3, 60)] * 70, 2, 1, 64, 16, "bf16", "heads"),
+]
+
+
+@pytest.mark.parametrize("mask", MASKS, ids=[f"{'causal' if c else 'frame'}{w}" for c, w in MASKS])
+@pytest.mark.parametrize("case", ATTENDS, ids=[f"{i}" for i in range(len(ATTENDS))])
+def test_attention(case, mask):
+    lens, heads, kv_heads, dim, page, dtype, order = case
+    rng = _rng(131 + dim + page + len(lens))
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, kv_heads, dim, page, dtype, order)
+    want = O.attend(q64, k64, v64, table, starts, length, *mask)
+    for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+        say(f"[packed attention] lens={lens[:5]} {case[1:]} mask={mask} max_new={hint}")
+        _compare(out, lse, want, dtype, dim, _largest(v64))
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 50), ("f32", 1), ("f32", 50)])
+def test_more_rows_than_tokens(dtype, new):
+    rng = _rng(132)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new + 3, 3), (2, 0), (new, 40 + new)], 4, 2, 64, 16, dtype)
+    for causal in (True, False):
+        want = O.attend(q64, k64, v64, table, starts, length, causal, -1)
+        for _, out, lse in _attend_both(cache, q, table, starts, length, causal=causal):
+            _compare(out, lse, want, dtype, 64, _largest(v64))
+
+
+@pytest.mark.parametrize("window", [(1 << 30) - 1, (1 << 31) - 4, (1 << 31) - 1, 1 << 40])
+@pytest.mark.parametrize("dtype,new,kv", [("bf16", 6, 4), ("bf16", 50, 30), ("bf16", 300, 200), ("f32", 50, 30)])
+def test_windows_past_every_length(dtype, new, kv, window):
+    rng = _rng(133)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, kv)], 2, 1, 64, 16, dtype)
+    for causal in (True, False):
+        out, lse = cache.attend(q, _device(table, starts, length), causal=causal, window=window, return_lse=True)
+        _compare(out, lse, O.attend(q64, k64, v64, table, starts, length, causal, window), dtype, 64, _largest(v64))
+
+
+@pytest.mark.parametrize("value", ["nan", "inf", "overflow"])
+@pytest.mark.parametrize("dtype,lens,heads,page", [("bf16", [(3, 100), (1, 70)], 4, 16), ("bf16", [(90, 150)], 4, 16), ("bf16", [(90, 150)], 4, 7),
+                                                   ("f32", [(3, 100), (1, 70)], 4, 16), ("f32", [(90, 150)], 4, 16)])
+def test_what_a_row_does_not_see_does_not_reach_it(dtype, lens, heads, page, value):
+    """Groups that are not finite: rows that see them have NaN or infinities, the others their own values."""
+    def spoil(codes, scales, table):
+        for b, (n, kv) in enumerate(lens):
+            for at in {kv - 1, kv - n // 2 - 1, max(kv - n - 20, 0)}:
+                pair = {"nan": (np.nan, np.nan), "inf": (0.0, np.inf), "overflow": (60000.0, 1.0)}[value]
+                scales[1][table[b, at // page], 0, at % page, 1] = pair
+    rng = _rng(134)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, 2, 64, page, dtype, spoil=spoil)
+    for mask in ((True, -1), (True, 5), (False, 10)):
+        with np.errstate(invalid="ignore"):
+            want = O.attend(q64, k64, v64, table, starts, length, *mask)
+        assert not np.isfinite(want[0]).all() or mask == (True, 5)
+        for _, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+            _compare(out, lse, want, dtype, 64, _largest(v64))
+
+
+@pytest.mark.parametrize("dtype,new,kv", [("bf16", 1, 40), ("bf16", 1, 6000), ("bf16", 9, 6000), ("bf16", 50, 300), ("bf16", 200, 900),
+                                          ("f32", 1, 6000), ("f32", 60, 300)])
+def test_scores_that_are_nan_stay_nan(dtype, new, kv):
+    """A key's group that is NaN makes every row that sees it NaN, whatever the cut of the keys; so does a query's element."""
+    def spoil(codes, scales, table):
+        at = kv - new - 1
+        scales[0][table[0, at // 16], 0, at % 16, 0] = np.nan
+    rng = _rng(135)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, kv)], 4, 2, 64, 16, dtype, spoil=spoil)
+    for hint, out, lse in _attend_both(cache, q, table, starts, length):
+        assert torch.isnan(out[:, :2]).all() and torch.isnan(lse[:, :2]).all()
+        assert torch.isfinite(out[:, 2:]).all() and torch.isfinite(lse[:, 2:]).all()
+    q[0, 3, 5] = float("nan")
+    for hint, out, lse in _attend_both(cache, q, table, starts, length):
+        assert torch.isnan(out[0, 3]).all() and torch.isfinite(out[0, 2]).all() and torch.isfinite(out[1:, 3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("gain", [1e-30, 1e-6, 30.0, 1e30])
+def test_queries_of_every_size(dtype, new, gain):
+    """Scores of great range, and queries beyond fp16's."""
+    rng = _rng(136)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, 700)], 4, 2, 64, 16, dtype, gain=gain)
+    scale = 0.125 if gain < 1e10 else 2.0 ** -100
+    want = O.attend(q64, k64, v64, table, starts, length, scale=scale)
+    for _, out, lse in _attend_both(cache, q, table, starts, length, scale=scale):
+        _compare(out, lse, want, dtype, 64, _largest(v64))
+
+
+def test_queries_of_one_row_of_many_sizes():
+    """Elements of 2^-20 of a row's largest, and fewer, keep their value."""
+    rng = _rng(137)
+    for dtype in ("bf16", "f32"):
+        cache, k64, v64, q, _, table, starts, length = _filled(rng, [(2, 300)], 4, 2, 64, 16, dtype)
+        q *= torch.from_numpy(2.0 ** rng.integers(-25, 1, q.shape)).to(q.dtype).cuda()
+        want = O.attend(q.double().cpu().numpy(), k64, v64, table, starts, length)
+        for _, out, lse in _attend_both(cache, q, table, starts, length):
+            _compare(out, lse, want, dtype, 64, _largest(v64))
+
+
+def _random_cache(seed, lens, heads, kv_heads, dim, page, dtype, gain=1.0):
+    """A larger cache, made on the GPU."""
+    rng = _rng(seed)
+    table, starts, length, pages = _batch(rng, lens, page)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    groups = -(-dim // 32)
+    codes = [torch.randint(0, 256, (pages, kv_heads, page, 16 * groups), dtype=torch.uint8, device="cuda", generator=g) for _ in range(2)]
+    scales = [torch.stack([0.2 + 0.1 * torch.rand((pages, kv_heads, page, groups), device="cuda", generator=g),
+                           -2 + torch.rand((pages, kv_heads, page, groups), device="cuda", generator=g)], -1).half() for _ in range(2)]
+    cache = A.PackedCache(*codes, *scales, dim, dtype=DT[dtype])
+    q = (gain * torch.randn((int(starts[-1]), heads, dim), device="cuda", generator=g)).to(DT[dtype])
+    return cache, q, table, starts, length
+
+
+def _dense(cache, q, table, starts, length, causal, window):
+    """The oracle's formula with all rows of a sequence and key head at once, in 64 bits on the CPU."""
+    tokens, heads, dim = q.shape
+    kv_heads, page = cache.kv_heads, cache.page_size
+    group = heads // kv_heads
+    out, weight = np.zeros((tokens, heads, dim)), np.zeros((tokens, heads, dim))
+    lse = np.full((tokens, heads), -np.inf)
+    size, most, count = np.zeros((tokens, heads)), np.zeros((tokens, heads)), np.zeros((tokens, heads))
+    q64, largest = q.double().cpu(), 0.0
+    for b, kv in enumerate(length):
+        n = int(starts[b + 1] - starts[b])
+        if n == 0 or kv == 0:
+            continue
+        held = _gpu(table[b, :-(-kv // page)])
+        k, v = (x.double().cpu().transpose(1, 2).flatten(0, 1)[:kv] for x in cache.unpack(held))
+        i, col = torch.arange(n)[:, None], torch.arange(int(kv))[None]
+        p = kv - n + i
+        ok = (col <= p) if causal else torch.ones((n, int(kv)), dtype=torch.bool)
+        if window >= 0:
+            ok = ok & (col >= (p if causal else kv - n) - window)
+        rows = slice(int(starts[b]), int(starts[b]) + n)
+        largest = max(largest, float(v.abs().max()))
+        for h in range(heads):
+            x = q64[rows, h]
+            s = (x @ k[:, h // group].T) * dim ** -0.5
+            s = s.masked_fill(~ok, -np.inf)
+            e = torch.softmax(s, 1).nan_to_num(0.0)
+            out[rows, h], weight[rows, h] = e @ v[:, h // group], e @ v[:, h // group].abs()
+            lse[rows, h] = torch.logsumexp(s, 1)
+            size[rows, h] = ((x.abs() @ k[:, h // group].abs().T) * dim ** -0.5).masked_fill(~ok, 0).amax(1)
+            most[rows, h] = s.abs().masked_fill(~ok, 0).amax(1)
+            count[rows, h] = ok.sum(1)
+    return (out, lse, {"weight": weight, "size": size, "most": most, "count": count}), largest
+
+
+LARGE = [
+    ([(1, 9001)], 4, 2, 64, 16, "bf16"), ([(3, 20000)], 4, 1, 128, 64, "bf16"), ([(100, 3333)], 4, 2, 64, 16, "bf16"), ([(1, 9001)], 4, 2, 64, 16, "f32"),
+    ([(33, 2500)], 2, 1, 128, 196, "f32"), ([(1, 70 + 31 * b) for b in range(90)], 4, 2, 128, 16, "bf16"), ([(9, 60 + 17 * b) for b in range(70)], 6, 3, 80, 7, "bf16"),
+    ([(2, 900 - 10 * b) for b in range(70)], 8, 2, 256, 16, "bf16"), ([(300, 300), (1, 4000), (700, 2100)], 4, 2, 128, 64, "bf16"), ([(513, 1025)], 2, 2, 256, 32, "bf16"),
+    ([(260, 900), (40, 5000)], 4, 2, 96, 48, "bf16"), ([(600, 1300)], 8, 2, 32, 16, "bf16"), ([(300, 700), (1, 2500)], 4, 2, 64, 16, "f32"), ([(130, 600)], 2, 1, 256, 16, "f32"),
+    ([(1500, 1500)], 2, 1, 64, 64, "bf16"), ([(257, 1000)] * 5, 4, 4, 40, 16, "bf16"),
+]
+
+
+@pytest.mark.parametrize("mask", [(True, -1), (False, -1), (True, 200), (False, 333)], ids=lambda m: f"{'causal' if m[0] else 'frame'}{m[1]}")
+@pytest.mark.parametrize("case", LARGE, ids=[f"{i}" for i in range(len(LARGE))])
+def test_attention_over_many_keys_and_rows(case, mask):
+    lens, heads, kv_heads, dim, page, dtype = case
+    cache, q, table, starts, length = _random_cache(141, lens, heads, kv_heads, dim, page, dtype)
+    want, largest = _dense(cache, q, table, starts, length, *mask)
+    for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+        say(f"[packed attention, many] lens={lens[:3]} {case[1:]} mask={mask} max_new={hint}")
+        _compare(out, lse, want, dtype, dim, largest)
+
+
+def test_scale_strides_and_out():
+    rng = _rng(138)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(3, 90), (30, 60)], 4, 2, 64, 16, "bf16", order="slots")
+    batch = _device(table, starts, length)
+    want = O.attend(q64, k64, v64, table, starts, length, scale=0.3)
+    wide = torch.full((q.shape[0] + 2, 6, 64), 5.0, dtype=q.dtype, device="cuda")  # rows behind the last sequence, heads beside
+    more = torch.cat([q, q[:2]])
+    got, lse = cache.attend(_laid(more, "view"), batch, scale=0.3, out=wide[:, 1:5], return_lse=True)
+    assert got.data_ptr() == wide[:, 1:5].data_ptr()
+    _compare(wide[:-2, 1:5], lse[:-2], want, "bf16", 64, _largest(v64))
+    assert (wide[-2:] == 5.0).all() and (wide[:, 0] == 5.0).all() and (wide[:, 5] == 5.0).all()
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 40), ("f32", 1)])
+def test_offsets_past_32_bits(dtype, new):
+    """Pages whose byte offsets pass 2^32: all calls."""
+    rng = _rng(146)
+    kv_heads, page, dim = 2, 16, 128
+    pages = (1 << 32) // (kv_heads * page * 64) + 64
+    cache = A.PackedCache.empty(pages, page, kv_heads, dim, dtype=DT[dtype])
+    table, starts, length, _ = _batch(rng, [(new, 100)], page, pages_first=pages - 16)
+    k, k64 = _stored(rng.standard_normal((100, kv_heads, dim)), dtype)
+    v, v64 = _stored(rng.standard_normal((100, kv_heads, dim)), dtype)
+    cache.append(k, v, _device(table, np.array([0, 100], np.int32), length))
+    held = [P.values(*P.pack(x), dim) for x in (k64, v64)]
+    q, q64 = _stored(rng.standard_normal((new, 4, dim)), dtype)
+    k_pages, v_pages = (np.full((16, kv_heads, page, dim), np.nan) for _ in range(2))
+    k_pages, v_pages = O.append(k_pages, v_pages, *held, table - (pages - 16), [0, 100], length)
+    got = cache.unpack(_gpu(table[:, :7]))[0].double().cpu().numpy()[0].swapaxes(1, 2).reshape(-1, kv_heads, dim)[:100]
+    assert np.array_equal(got, held[0])
+    want = O.attend(q64, k_pages, v_pages, table - (pages - 16), starts, length)
+    for _, out, lse in _attend_both(cache, q, table, starts, length):
+        _compare(out, lse, want, dtype, dim, _largest(v_pages))
+    weights = torch.zeros((pages, kv_heads, page), device="cuda")
+    cache.weigh(q, lse, _device(table, starts, length), weights)
+    w, size = P.weigh(np.zeros((16, kv_heads, page)), q64, lse.double().cpu().numpy(), k_pages, table - (pages - 16), starts, length)
+    _compare_weights(weights[pages - 16:].double().cpu().numpy(), w, size, dim, 1.0, 0.0, new * 4)
+    into = np.arange(pages - 16, pages)[~np.isin(np.arange(pages - 16, pages), table)][:3][None].astype(np.int32)
+    lengths, kept = cache.evict(weights, _device(table, starts, length), _gpu(into), keep=40, recent=3)
+    want_len, want_kept = P.evict(weights[pages - 16:].cpu().numpy(), table - (pages - 16), length, 40, 3)
+    assert lengths.tolist() == want_len.tolist() and np.array_equal(kept.cpu().numpy(), want_kept)
+    new_k = cache.unpack(_gpu(into))[0].double().cpu().numpy()[0].swapaxes(1, 2).reshape(-1, kv_heads, dim)[:40]
+    for h in range(kv_heads):
+        assert np.array_equal(new_k[:, h], held[0][want_kept[0, h], h])
+
+
+# ------------------------------------------------------------------ weight --
+
+def _compare_weights(got, want, size, dim, decay, before, rows):
+    bound = (2 * dim + 2) * U * size[..., 1] + 4 * U * (size[..., 2] + size[..., 0]) + (rows + 4) * U * size[..., 0] + 3 * U * (np.abs(decay * before) + np.abs(want))
+    off = np.abs(got - want)
+    assert (off <= bound).all(), f"{(off > bound).sum()} off, worst {np.max(off / np.maximum(bound, 1e-30)):.3g} of the bound"
+
+
+# lens, heads, kv heads, dim, page, dtype, packed
+WEIGHS = [
+    ([(1, 1)], 1, 1, 8, 1, "bf16", True), ([(1, 77), (1, 300)], 4, 1, 64, 16, "bf16", True), ([(1, 64), (0, 65), (1, 1), (1, 200), (1, 31)], 8, 2, 128, 16, "bf16", True),
+    ([(5, 5), (0, 40), (17, 90), (0, 0), (40, 333)], 6, 3, 80, 7, "bf16", True), ([(130, 300), (2, 9)], 4, 1, 96, 64, "bf16", True), ([(20, 196)], 3, 1, 256, 196, "bf16", True),
+    ([(1, 150), (30, 60)], 6, 2, 160, 16, "f32", True), ([(3, 100)], 4, 2, 32, 5, "f32", True), ([(70, 90)], 2, 1, 256, 16, "f32", True), ([(33, 70)], 4, 4, 64, 16, "f32", True),
+    ([(1, 77), (30, 200)], 4, 2, 64, 16, "bf16", False), ([(1, 40)] * 70, 2, 1, 128, 16, "bf16", False), ([(9, 90)], 2, 2, 40, 3, "bf16", False), ([(90, 100)], 2, 1, 256, 16, "bf16", False),
+    ([(1, 77), (30, 200)], 4, 2, 80, 16, "f32", False), ([(100, 120)], 2, 1, 256, 32, "f32", False), ([(4, 50)], 1, 1, 8, 16, "f32", False),
+]
+
+
+def _weigh_case(case, seed):
+    lens, heads, kv_heads, dim, page, dtype, packed = case
+    rng = _rng(seed + dim + page)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, kv_heads, dim, page, dtype)
+    if not packed:
+        kp, k64 = _stored(k64, dtype)  # unseen slots: not finite
+        vp, v64 = _stored(v64, dtype)
+        cache = A.PagedCache(kp, vp)
+    return rng, cache, k64, q, q64, table, starts, length
+
+
+@pytest.mark.parametrize("mask", MASKS, ids=[f"{'causal' if c else 'frame'}{w}" for c, w in MASKS])
+@pytest.mark.parametrize("case", WEIGHS, ids=[f"{i}" for i in range(len(WEIGHS))])
+def test_weight(case, mask):
+    lens, heads, kv_heads, dim, page, dtype, packed = case
+    rng, cache, k64, q, q64, table, starts, length = _weigh_case(case, 151)
+    say(f"[weigh] {lens[:4]} {case[1:]} mask={mask}")
+    with np.errstate(invalid="ignore"):
+        _, lse, _ = O.attend(q64, k64, np.zeros_like(k64), table, starts, length, *mask)
+    lse = _gpu(lse.astype(np.float32))
+    before = rng.random(k64.shape[:3]).astype(np.float32)
+    for b, (n, kv) in enumerate(lens):  # the new tokens' slots are not cleared
+        for at in range(max(kv - n, 0), kv):
+            before[table[b, at // page], :, at % page] = np.nan
+    most = int(np.max(np.diff(starts)))
+    for hint in sorted({0, most, 1}):
+        for decay in (1.0, 0.0, 0.75):
+            weights = _gpu(before)
+            batch = _device(table, starts, length, max_new=hint)
+            assert cache.weigh(q, lse, batch, weights, causal=mask[0], window=mask[1], decay=decay) is weights
+            want, size = P.weigh(before, q64, lse.double().cpu().numpy(), k64, table, starts, length, *mask, decay=decay)
+            untouched = ~np.isfinite(want)
+            assert np.array_equal(np.isnan(weights.cpu().numpy()), np.isnan(want))
+            keep = np.where(untouched, 0.0, want)
+            _compare_weights(np.where(untouched, 0.0, weights.double().cpu().numpy()), keep, size, dim, decay, np.nan_to_num(before), most * heads // kv_heads)
+            again = cache.weigh(q, lse, batch, _gpu(before), causal=mask[0], window=mask[1], decay=decay)
+            assert torch.equal(again.view(torch.int32), weights.view(torch.int32))
+
+
+def test_weight_adds_up_to_the_rows():
+    """Over a whole cache the weights of a step sum to the number of rows, and steps add up."""
+    rng = _rng(152)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(4, 300), (1, 50)], 8, 2, 64, 16, "bf16")
+    batch = _device(table, starts, length)
+    weights = torch.zeros(k64.shape[:3], device="cuda")
+    _, lse = cache.attend(q, batch, return_lse=True)
+    cache.weigh(q, lse, batch, weights)
+    rows = 5 * 4
+    assert np.abs(weights.double().sum((0, 2)).cpu().numpy() - rows).max() <= 1e-4 * rows  # lse, terms and sums, each within 1e-5
+    first = weights.clone()
+    cache.weigh(q, lse, batch, weights)
+    old = torch.ones_like(weights, dtype=torch.bool)
+    for b, (n, kv) in enumerate([(4, 300), (1, 50)]):
+        for at in range(kv - n, kv):
+            old[table[b, at // 16], :, at % 16] = False
+    assert torch.equal(weights[~old], first[~old]) and torch.allclose(weights[old], 2 * first[old], rtol=1e-6, atol=0)
+
+
+def test_rows_that_see_nothing_give_no_weight():
+    rng = _rng(153)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(9, 4), (70, 30)], 4, 2, 64, 16, "bf16")
+    _, lse = cache.attend(q, _device(table, starts, length), return_lse=True)
+    assert torch.isneginf(lse).any()
+    weights = cache.weigh(q, lse, _device(table, starts, length), torch.zeros(k64.shape[:3], device="cuda"))
+    want, size = P.weigh(np.zeros(k64.shape[:3]), q64, lse.double().cpu().numpy(), k64, table, starts, length)
+    _compare_weights(weights.double().cpu().numpy(), want, size, 64, 1.0, 0.0, 140)
+
+
+# ---------------------------------------------------------------- eviction --
+
+def _eviction(rng, lens, keep, page, kv_heads, values, wild=False):
+    """Table, lengths, weights and the pages that the kept tokens go to; `values`: what the weights are drawn from."""
+    table, starts, length, first = _batch(rng, [(0, n) for n in lens], page)
+    width = max(1, -(-min(keep, max(max(lens), 1)) // page))
+    if width * page < min(keep, table.shape[1] * page):
+        width = -(-min(keep, table.shape[1] * page) // page)
+    pages = first + len(lens) * width
+    into = (first + rng.permutation(len(lens) * width)).reshape(len(lens), width).astype(np.int32)
+    if wild:  # a page of a sequence and one to go to that do not exist
+        table[0, 0], into[-1, 0] = pages + 5, -7
+    weights = values(rng, (pages, kv_heads, page)).astype(np.float32)
+    return table, starts, length, weights, into, pages
+
+
+DRAWS = {
+    "spread": lambda r, s: np.exp(2 * r.standard_normal(s)), "few": lambda r, s: r.integers(0, 3, s), "zero": lambda r, s: np.zeros(s),
+    "signed": lambda r, s: r.choice([0.0, -0.0, -1.5, 1.5, np.inf, -np.inf, np.nan, 1e-42, -1e-42], s), "close": lambda r, s: 1 + 2.0 ** -23 * r.integers(0, 50, s),
+}
+# lens, keep, recent, page, kv heads
+EVICTS = [
+    ([1], 1, 0, 1, 1), ([5, 0, 17], 4, 1, 4, 2), ([300, 64, 65, 1], 64, 16, 16, 3), ([2500], 1000, 0, 16, 2), ([5000, 1024, 1025], 1024, 1024, 64, 1),
+    ([3000, 700], 2999, 100, 7, 2), ([400] * 70, 33, 3, 196, 1), ([90, 30], 500, 20, 16, 2), ([70000], 3000, 64, 256, 1),
+]
+
+
+@pytest.mark.parametrize("draw", list(DRAWS))
+@pytest.mark.parametrize("case", EVICTS, ids=[f"{i}" for i in range(len(EVICTS))])
+def test_eviction_picks_and_moves(case, draw):
+    lens, keep, recent, page, kv_heads = case
+    say(f"[evict] {case} {draw}")
+    rng = _rng(161 + keep)
+    table, starts, length, weights, into, pages = _eviction(rng, lens, keep, page, kv_heads, DRAWS[draw], wild=len(lens) > 1)
+    dim = 40
+    codes = [rng.integers(0, 256, (pages, kv_heads, page, 32)).astype(np.uint8) for _ in range(2)]
+    scales = [rng.integers(0, 1 << 16, (pages, kv_heads, page, 2, 2)).astype(np.uint16).view(np.float16) for _ in range(2)]
+    batch = _device(table, starts, length)
+    want_len, want = P.evict(weights, table, length, keep, recent)
+    caches = [_packed(codes, scales, dim, "bf16", "slots"), _packed(codes, scales, dim, "f32")]
+    for dtype in ("bf16", "f32"):
+        bits = rng.integers(0, 1 << 16, (2, pages, kv_heads, page, 8 * (2 if dtype == "f32" else 1))).astype(np.uint16)
+        caches.append(A.PagedCache(*(_order(_gpu(x.view(np.int16)).view(DT[dtype]), "slots" if dtype == "f32" else "heads") for x in bits)))
+    for cache in caches:
+        w = _gpu(weights)
+        old = [x.cpu().contiguous().view(torch.uint8).numpy() for x in cache._tensors]
+        lengths, kept = cache.evict(w, batch, _gpu(into), keep=keep, recent=recent)
+        assert np.array_equal(lengths.cpu().numpy(), want_len) and np.array_equal(kept.cpu().numpy(), want)
+        assert _same(w.cpu().numpy(), P.move(weights, table, into, want, page, pages))
+        for x, before in zip(cache._tensors, old):
+            assert np.array_equal(x.cpu().contiguous().view(torch.uint8).numpy(), P.move(before, table, into, want, page, pages))
+
+
+def test_append_attend_weigh_evict():
+    """A stream as it would be used: frames go in, are attended to, weighed, and the cache is brought down to a budget again and again."""
+    rng = _rng(171)
+    n, kv_heads, heads, dim, page, frame, keep, recent = 2, 2, 4, 64, 16, 20, 64, 24
+    width = -(-(keep + 3 * frame) // page)
+    pages = 2 * n * width
+    for kind in ("packed", "bf16"):
+        cache = (A.PackedCache if kind == "packed" else A.PagedCache).empty(pages, page, kv_heads, dim)
+        tables = torch.arange(pages, dtype=torch.int32, device="cuda").view(2, n, width).contiguous()
+        starts = torch.arange(n + 1, dtype=torch.int32, device="cuda") * frame
+        length = torch.zeros(n, dtype=torch.int32, device="cuda")
+        weights = torch.full((pages, kv_heads, page), float("nan"), device="cuda")
+        rotary = A.Rotary(A.axis_frequencies((11, 11, 10)), dim)
+        now = 0
+        # what each sequence and key head holds, in 64 bits: keys, values, weights
+        held = [[(np.zeros((0, dim)), np.zeros((0, dim)), np.zeros(0)) for _ in range(kv_heads)] for _ in range(n)]
+        for t in range(7):
+            length += frame
+            batch = A.CacheBatch(tables[now], starts, length, max_new=frame)
+            (k, k64), (v, v64), (q, q64) = (_stored(rng.standard_normal((n * frame, h, dim)), "bf16") for h in (kv_heads, kv_heads, heads))
+            pos = torch.tensor([[t, i // 5, i % 5] for i in range(frame)] * n, dtype=torch.int32, device="cuda")
+            turned = cache.append(k, v, batch, rotary=rotary, pos=pos, q=q)
+            out, lse = cache.attend(turned, batch, causal=False, return_lse=True)
+            cache.weigh(turned, lse, batch, weights, causal=False, decay=0.9)
+            tq, at = turned.double().cpu().numpy(), tables[now].long()
+            pages_of = cache.unpack(tables[now]) if kind == "packed" else (cache.k_pages[at], cache.v_pages[at])
+            kk, vv = (x.double().cpu().numpy().swapaxes(2, 3).reshape(n, -1, kv_heads, dim) for x in pages_of)
+            for b in range(n):
+                L = int(length[b])
+                for h in range(kv_heads):
+                    old_k, old_v, old_w = held[b][h]
+                    assert np.array_equal(kk[b, :L - frame, h], old_k) and np.array_equal(vv[b, :L - frame, h], old_v)
+                    rows = slice(b * frame, (b + 1) * frame)
+                    s = np.einsum("igd,ld->igl", tq[rows, 2 * h:2 * h + 2], kk[b, :L, h]) * dim ** -0.5
+                    e = np.exp(s - s.max(-1, keepdims=True))
+                    e /= e.sum(-1, keepdims=True)
+                    want = np.einsum("igl,ld->igd", e, vv[b, :L, h])
+                    got = out.double().cpu().numpy()[rows, 2 * h:2 * h + 2]
+                    spread = np.einsum("igl,ld->igd", e, np.abs(vv[b, :L, h]))
+                    # bf16's output, and exponentials for the product: fp16 or bf16; scores are exact to 2^-16
+                    assert (np.abs(got - want) <= 1.25 * (2.0 ** -8 * np.abs(want) + 2.0 ** -8 * spread) + 1e-4 * spread).all()
+                    w = np.concatenate([0.9 * old_w, np.zeros(frame)]) + e.sum((0, 1))
+                    mine = weights[at[b]].transpose(0, 1).reshape(kv_heads, -1)[h, :L].double().cpu().numpy()
+                    assert np.abs(mine - w).max() <= 1e-4 * w.max()
+                    held[b][h] = (kk[b, :L, h], vv[b, :L, h], mine)
+            if int(length[0]) > keep + frame:
+                length2, kept = cache.evict(weights, batch, tables[1 - now], keep=keep, recent=recent)
+                assert length2.tolist() == [keep] * n
+                for b in range(n):
+                    for h in range(kv_heads):
+                        w = held[b][h][2]
+                        late = int(length[b]) - recent
+                        order = sorted(range(late), key=lambda j: (-w[j], j))[:keep - recent]
+                        chosen = np.array(sorted(order) + list(range(late, int(length[b]))))
+                        assert np.array_equal(kept[b, h].cpu().numpy(), chosen)
+                        held[b][h] = tuple(x[chosen] for x in held[b][h])
+                now, length = 1 - now, length2
+
+
+def test_another_stream_and_graph_replays():
+    """A step (append, attend, weigh, evict, unpack) on a stream of its own, then captured twice and replayed in turn with new inputs in between."""
+    rng = _rng(172)
+    lens = [(1, 1400), (1, 33)]
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, 8, 2, 64, 16, "bf16")
+    extra = A.PackedCache.empty(cache.pages + 8, 16, 2, 64)
+    for a, b in zip(extra._tensors, cache._tensors):
+        a.view(torch.uint8)[:cache.pages] = b.contiguous().view(torch.uint8)
+    batch = _device(table, starts, length, max_new=1)
+    into = torch.arange(cache.pages, cache.pages + 8, dtype=torch.int32, device="cuda").view(2, 4)
+    pos = torch.tensor([[3, 2, 1], [1, 1, 9]], dtype=torch.int32, device="cuda")
+    rotary = A.Rotary(A.axis_frequencies((11, 11, 10)), 64)
+    k, v = (torch.randn(2, 2, 64, device="cuda").bfloat16() for _ in range(2))
+    start = torch.rand((extra.pages, 2, 16), device="cuda")
+    weights = start.clone()
+
+    def step():
+        weights.copy_(start)
+        turned = extra.append(k, v, batch, rotary=rotary, pos=pos, q=q)
+        out, lse = extra.attend(turned, batch, return_lse=True)
+        extra.weigh(turned, lse, batch, weights, decay=0.5)
+        lengths, kept = extra.evict(weights, batch, into, keep=60, recent=7)
+        return (out, lse, lengths, kept, weights.clone(), *extra.unpack(into[:1]))
+    eager = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        other = step()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(eager, other))
+    graphs = []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            graphs.append((graph, step()))
+    for i in range(6):
+        for t in (q, k, v):
+            t.copy_(torch.randn(t.shape, device="cuda"))
+        graph, held = graphs[i % 2]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in held]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {i}"
+
+
+# ---------------------------------------------------------------- the rest --
+
+def _small():
+    rng = _rng(181)
+    cache, _, _, q, _, table, starts, length = _filled(rng, [(2, 40)], 4, 2, 64, 16, "bf16")
+    return cache, _device(table, starts, length), q, torch.zeros((cache.pages, 2, 16), device="cuda")
+
+
+def test_nothing_to_do():
+    cache, _, q, weights = _small()
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    none = A.CacheBatch(ints(0, 4), ints(1), ints(0))
+    before = [x.clone() for x in cache._tensors]
+    for tokens in (0, 2):  # rows of no sequence are not written
+        x, out = q[:tokens], torch.full_like(q[:tokens], 3.0)
+        cache.append(x[:, :2], x[:, 2:], none)
+        assert cache.attend(x, none, out=out) is out and (out == 3.0).all()
+        assert not cache.weigh(x, torch.zeros(tokens, 4, device="cuda"), none, weights).any()
+    lengths, kept = cache.evict(weights, none, ints(0, 1), keep=16)
+    assert lengths.shape == (0,) and kept.shape == (0, 2, 16)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, cache._tensors))
+
+
+def test_no_gradient_is_lost():
+    cache, batch, q, weights = _small()
+    lse = torch.zeros(2, 4, device="cuda")
+    into = torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+    grad = q.clone().requires_grad_(True)
+    for call in (lambda: cache.append(grad[:, :2], q[:, 2:], batch), lambda: cache.attend(grad, batch), lambda: cache.weigh(grad, lse, batch, weights),
+                 lambda: cache.weigh(q, lse.clone().requires_grad_(True), batch, weights), lambda: cache.weigh(q, lse, batch, weights.clone().requires_grad_(True)),
+                 lambda: cache.evict(weights.clone().requires_grad_(True), batch, into, keep=8)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    with torch.no_grad():
+        cache.attend(grad, batch)
+
+
+def test_what_a_call_writes_is_known_to_autograd():
+    cache, batch, q, weights = _small()
+    spare = torch.tensor([[3, 3]], dtype=torch.int32, device="cuda")
+    count = lambda: [x._version for x in (*cache._tensors, weights)]  # noqa: E731
+    a = count()
+    cache.append(q[:, :2], q[:, 2:], batch)
+    b = count()
+    assert [y - x for x, y in zip(a, b)] == [1, 1, 1, 1, 0]
+    _, lse = cache.attend(q, batch, return_lse=True)
+    cache.unpack(spare)
+    assert count() == b
+    cache.weigh(q, lse, batch, weights)
+    assert count() == [*b[:4], b[4] + 1]
+
+
+def test_the_tensors_device_is_current_in_every_call(monkeypatch):
+    cache, batch, q, weights = _small()
+    lse, spare = torch.zeros(2, 4, device="cuda"), torch.full((1, 1), 4, dtype=torch.int32, device="cuda")
+    entered = []
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            entered.append(self.index)
+
+        def __exit__(self, *_):
+            entered.append("left")
+    calls = (lambda: cache.append(q[:, :2], q[:, 2:], batch), lambda: cache.attend(q, batch), lambda: cache.unpack(spare),
+             lambda: cache.weigh(q, lse, batch, weights), lambda: cache.evict(weights, batch, spare, keep=16))
+    for call in calls:
+        call()
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(A, "_current", lambda: 1, raising=False)
+    for call in calls:
+        call()
+        assert entered == [0, "left"]
+        entered.clear()
+
+
+def test_refusals():
+    cache, batch, q, weights = _small()
+    codes, scales = cache.k_codes, cache.k_scales
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lse, kv, into = torch.zeros(2, 4, device="cuda"), q[:, :2], ints(0, 1, 2, 3)[None]
+    make = lambda *a, **k: A.PackedCache(*a, **k)  # noqa: E731
+    for bad in (lambda: make(codes, codes, scales, scales, 96), lambda: make(codes, codes, scales, scales, 0), lambda: make(codes.int(), codes, scales, scales, 64),
+                lambda: make(codes, codes[:2], scales, scales, 64), lambda: make(codes, codes, scales.float(), scales, 64), lambda: make(codes, codes, scales, scales[..., :1], 64),
+                lambda: make(codes, codes, scales, scales.flip(0)[:2], 64), lambda: make(codes.cpu(), codes.cpu(), scales.cpu(), scales.cpu(), 64),
+                lambda: make(codes, codes, scales, scales, 64, dtype=torch.float16), lambda: make(codes, codes, scales.transpose(3, 4), scales, 64),
+                lambda: make(codes.transpose(2, 3), codes.transpose(2, 3), scales, scales, 64),
+                lambda: cache.append(kv, kv[:, :1], batch), lambda: cache.append(kv.float(), kv.float(), batch), lambda: cache.append(kv, kv, batch, q=q),
+                lambda: cache.append(kv, kv, batch, q_out=q), lambda: cache.attend(q.float(), batch), lambda: cache.attend(q[..., :32], batch),
+                lambda: cache.attend(q, batch, out=q.float()), lambda: cache.unpack(into.long()), lambda: cache.unpack(into.cpu()), lambda: cache.unpack(into[:, ::2]),
+                lambda: cache.weigh(q, lse[:1], batch, weights), lambda: cache.weigh(q, lse.double(), batch, weights), lambda: cache.weigh(q, lse.t().contiguous().t(), batch, weights),
+                lambda: cache.weigh(q, lse, batch, weights[:2]), lambda: cache.weigh(q, lse, batch, weights.half()), lambda: cache.weigh(q.float(), lse, batch, weights),
+                lambda: cache.evict(weights, batch, into, keep=0), lambda: cache.evict(weights, batch, into, keep=8, recent=9), lambda: cache.evict(weights, batch, into, keep=8, recent=-1),
+                lambda: cache.evict(weights, batch, into[0], keep=8), lambda: cache.evict(weights, batch, into.long(), keep=8), lambda: cache.evict(weights[:2], batch, into, keep=8),
+                lambda: cache.evict(weights, batch, into.repeat(2, 1), keep=8), lambda: cache.evict(weights, batch, into, keep=1 << 31)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: cache.attend(q[:, :3], batch), lambda: cache.attend(q, batch, scale=0.0), lambda: cache.weigh(q[:, :3], lse[:, :3].contiguous(), batch, weights),
+                lambda: cache.weigh(q, lse, batch, weights, decay=float("nan")), lambda: cache.weigh(q, lse, batch, weights, scale=-1.0),
+                lambda: cache.evict(weights, batch, into[:, :1].contiguous(), keep=40)):
+        with pytest.raises(S.SkipConvError) as e:
+            bad()
+        assert e.value.code == S.SKIPCONV_E_INVALID_ARG
+    held = A.PackedCache(codes[..., :16].contiguous(), codes[..., :16].contiguous(), scales[..., :1, :].contiguous(), scales[..., :1, :].contiguous(), 20)
+    with pytest.raises(S.SkipConvError) as e:
+        held.attend(q[..., :20], batch)
+    assert e.value.code == S.SKIPCONV_E_UNSUPPORTED
+    for name in ("k_codes", "v_codes", "k_scales", "v_scales", "pages", "kv_heads", "page_size", "head_dim", "dtype"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
