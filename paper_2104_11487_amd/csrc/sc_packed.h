@@ -55,7 +55,7 @@ hipError_t launch_packed_few_f32(const PackedAttendParams& p, int whole_pages, h
 hipError_t launch_packed_many_bf16(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
 hipError_t launch_packed_many_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
 // log2 of the row blocks (of 16 rows) that a wave of the kernel for many rows takes.
-inline int packed_many_blocks_log(int elem_bytes, int dim) { return dim > 128 || elem_bytes == 4 ? 1 : 2; }
+inline int packed_many_blocks_log(int elem_bytes, int dim) { return dim > 128 || elem_bytes == 4 ? 0 : 1; }
 
 // Accumulated attention weight. The cache's keys are codes where `packed`, else of the dtype.
 struct WeighParams {

@@ -26,14 +26,8 @@ namespace sc {
 constexpr float kPackedSlack = 8.0f;  // powers of two that an exponential may exceed the reference's by
 constexpr float kPackedLift = 7.0f;   // powers of two that exponentials are formed too large by: 2^15 at most
 
-// One key tile's codes and (scale, minimum) pairs, as a lane holds them.
-template <int NG>
-struct PackedTile {
-  static constexpr int kPieces = NG == 8 ? 2 : 1;
-  uint32_t kc[2][NG], kp[2][kPieces], vc[8][kPieces], vp[8];
-};
-
-// Where a tile's keys lie: whole pages of 16-key blocks: alike in all lanes, per block; otherwise of the lane's key (lane & 31).
+// Where a tile's keys lie, looked up ahead: with whole pages of 16-key blocks a block's page and first slot, alike in all lanes; otherwise the
+// lane's key's (lane & 31).
 template <bool WHOLE>
 struct PackedPlace {
   int entry[WHOLE ? 2 : 1], slot[WHOLE ? 2 : 1];
@@ -44,7 +38,7 @@ struct PackedPlace {
 template <int NG, int NB, int PARTS, bool MANY, bool WHOLE>
 __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWaves), MANY ? 2 : 1) attend_packed_kernel(PackedAttendParams pp) {
   constexpr int NW = MANY ? kPackedManyWaves : kPackedFewWaves, WROWS = 16 * NB, ROWS = MANY ? NW * WROWS : WROWS;
-  constexpr int KEYS = kPackedKeys, DP = 32 * NG, NJ = 2 * NG, PIECES = PackedTile<NG>::kPieces;
+  constexpr int KEYS = kPackedKeys, DP = 32 * NG, NJ = 2 * NG, PIECES = NG == 8 ? 2 : 1;
   constexpr int JP = DP + 4;  // joining: a row's stride in LDS, in floats
   __shared__ alignas(16) float lds[MANY ? 4 : NW * ROWS * (JP + 2)];
   const AttendParams& p = pp.a;
@@ -59,19 +53,21 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
   const int col = lane & 15, quad = lane >> 4, last_group = pp.groups - 1;
 
   // Byte offsets in a row: the lane's pieces of a key, of a value; of their pairs. Groups past the head's are led to the last one (the queries
-  // are zero there, and the outputs are not stored).
-  uint32_t k_at[NG <= 4 ? 1 : 2], kp_at[PIECES];
+  // are zero there, and the outputs are not stored). With whole pages the lane's row of a block is in them.
+  uint32_t k_at[PIECES], kp_at[PIECES], v_at[WHOLE ? 4 : 1], vp_at[WHOLE ? 4 : 1];
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    if constexpr (NG >= 4) {
-      const int g = min(quad * (NG / 4) + i, last_group);
-      k_at[i] = 16 * g, kp_at[i] = 4 * g;
-    } else {
-      k_at[i] = 4 * NG * quad, kp_at[i] = 4 * (NG * quad / 4);
-    }
+    const int g = NG >= 4 ? min(quad * (NG / 4) + i, last_group) : NG * quad / 4;
+    k_at[i] = (NG >= 4 ? 16 * g : 4 * NG * quad) + (WHOLE ? (uint32_t)(col * (int)p.c.k_slot) : 0u);
+    kp_at[i] = 4 * g + (WHOLE ? (uint32_t)(col * (int)pp.s.k_slot) : 0u);
   }
   const int v_group = min(NG * col / 16, last_group);
-  const uint32_t v_at = NG >= 4 ? 16 * v_group + (NG * col) % 16 : (NG * col) & ~3, vp_at = 4 * v_group;
+  const uint32_t v_byte = NG >= 4 ? 16 * v_group + (NG * col) % 16 : (NG * col) & ~3;
+#pragma unroll
+  for (int r = 0; r < (WHOLE ? 4 : 1); ++r) {
+    v_at[r] = v_byte + (WHOLE ? (uint32_t)((4 * quad + r) * (int)p.c.v_slot) : 0u);
+    vp_at[r] = 4 * v_group + (WHOLE ? (uint32_t)((4 * quad + r) * (int)pp.s.v_slot) : 0u);
+  }
   const uint32_t v_sel = NG >= 4 ? 0x0c040c00u : 0x0c040c00u + ((NG * col) & 3) * 0x00010001u;  // picks a byte of two words into 16-bit halves
 
   for (int64_t at = first_unit;;) {
@@ -151,16 +147,20 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     const char* const ksb = pp.s.k + (int64_t)u.head * pp.s.k_head;
     const char* const vsb = pp.s.v + (int64_t)u.head * pp.s.v_head;
 
-    auto find = [&](int key0, PackedPlace<WHOLE>& to) {
+    // A tile in the lane's registers: codes and pairs of keys and of values.
+    uint32_t kc[2][NG], kp[2][PIECES], vc[8][PIECES], vp[8];
+    PackedPlace<WHOLE> place;
+    const char* v_rows[2];  // whole pages: a block's first value, its pairs
+    const char* v_pairs[2];
+    int v_page = 0, v_slot = 0;  // otherwise: the lane's key's
+
+    auto find = [&](int key0) {
       if constexpr (WHOLE) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) to.entry[j] = entry_at(p.c, u.b, key0 + 16 * j, 16, &to.slot[j]);
+        for (int j = 0; j < 2; ++j) place.entry[j] = entry_at(p.c, u.b, key0 + 16 * j, 16, &place.slot[j]);
       } else {
-        to.entry[0] = entry_at(p.c, u.b, key0 + (lane & 31), 1, &to.slot[0]);
+        place.entry[0] = entry_at(p.c, u.b, key0 + (lane & 31), 1, &place.slot[0]);
       }
-    };
-    auto row_of = [&](const PackedPlace<WHOLE>& from, int key, int* page, int* slot) {  // of a tile's key, from the lane that looked it up
-      *page = page_of_entry(p.c, __shfl(from.entry[0], key)), *slot = __shfl(from.slot[0], key);
     };
     auto load_key = [&](const char* row, const char* pairs, uint32_t* codes, uint32_t* pair) {
       if constexpr (NG == 1) {
@@ -178,44 +178,50 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) pair[i] = *reinterpret_cast<const uint32_t*>(pairs + kp_at[i]);
     };
-    auto load_value = [&](const char* row, const char* pairs, uint32_t* codes, uint32_t* pair) {
+    auto load_value = [&](const char* row, const char* pairs, int r, uint32_t* codes, uint32_t* pair) {
       if constexpr (PIECES == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + v_at);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(row + v_at[r]);
         codes[0] = w[0], codes[1] = w[1];
       } else {
-        codes[0] = *reinterpret_cast<const uint32_t*>(row + v_at);
+        codes[0] = *reinterpret_cast<const uint32_t*>(row + v_at[r]);
       }
-      *pair = *reinterpret_cast<const uint32_t*>(pairs + vp_at);
+      *pair = *reinterpret_cast<const uint32_t*>(pairs + vp_at[r]);
     };
-    auto fetch = [&](const PackedPlace<WHOLE>& from, PackedTile<NG>& to) {
+    auto fetch_keys = [&]() {  // of the tile at `place`, which then is free
+      if constexpr (WHOLE) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < 2; ++j) {
+          const uint64_t page = (uint32_t)page_of_entry(p.c, uniform(place.entry[j])), slot = (uint32_t)uniform(place.slot[j]);
+          load_key(kb + (page * (uint32_t)p.c.k_page + slot * (uint32_t)p.c.k_slot), ksb + (page * (uint32_t)pp.s.k_page + slot * (uint32_t)pp.s.k_slot), kc[j], kp[j]);
+          v_rows[j] = vb + (page * (uint32_t)p.c.v_page + slot * (uint32_t)p.c.v_slot);
+          v_pairs[j] = vsb + (page * (uint32_t)pp.s.v_page + slot * (uint32_t)pp.s.v_slot);
+        }
+      } else {
+        v_page = page_of_entry(p.c, place.entry[0]), v_slot = place.slot[0];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int64_t page = __shfl(v_page, 16 * j + col), slot = __shfl(v_slot, 16 * j + col);
+          load_key(kb + page * p.c.k_page + slot * p.c.k_slot, ksb + page * pp.s.k_page + slot * pp.s.k_slot, kc[j], kp[j]);
+        }
+      }
+    };
+    auto fetch_values = [&]() {  // of the tile whose keys were fetched last
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
         if constexpr (WHOLE) {
-          const int64_t page = page_of_entry(p.c, uniform(from.entry[j])), slot = uniform(from.slot[j]);
-          const char* const k0 = kb + page * p.c.k_page + slot * p.c.k_slot;
-          const char* const v0 = vb + page * p.c.v_page + slot * p.c.v_slot;
-          const char* const ks0 = ksb + page * pp.s.k_page + slot * pp.s.k_slot;
-          const char* const vs0 = vsb + page * pp.s.v_page + slot * pp.s.v_slot;
-          load_key(k0 + (uint32_t)(col * (int)p.c.k_slot), ks0 + (uint32_t)(col * (int)pp.s.k_slot), to.kc[j], to.kp[j]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            load_value(v0 + (uint32_t)((4 * quad + r) * (int)p.c.v_slot), vs0 + (uint32_t)((4 * quad + r) * (int)pp.s.v_slot), to.vc[4 * j + r], &to.vp[4 * j + r]);
+          load_value(v_rows[e / 4], v_pairs[e / 4], e % 4, vc[e], &vp[e]);
         } else {
-          int page, slot;
-          row_of(from, 16 * j + col, &page, &slot);
-          load_key(kb + page * p.c.k_page + slot * p.c.k_slot, ksb + page * pp.s.k_page + slot * pp.s.k_slot, to.kc[j], to.kp[j]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            row_of(from, 16 * j + 4 * quad + r, &page, &slot);
-            load_value(vb + page * p.c.v_page + slot * p.c.v_slot, vsb + page * pp.s.v_page + slot * pp.s.v_slot, to.vc[4 * j + r], &to.vp[4 * j + r]);
-          }
+          const int64_t page = __shfl(v_page, 16 * (e / 4) + 4 * quad + e % 4), slot = __shfl(v_slot, 16 * (e / 4) + 4 * quad + e % 4);
+          load_value(vb + page * p.c.v_page + slot * p.c.v_slot, vsb + page * pp.s.v_page + slot * pp.s.v_slot, 0, vc[e], &vp[e]);
         }
       }
     };
 
-    // One tile's work. edge: some row does not see some of its keys.
-    auto tile = [&](auto edge_, int key0, const PackedTile<NG>& f) {
+    // One tile's work, and the loads of the next one, whose keys take the place of this one's as soon as these are in the product, and values
+    // likewise. edge: some row does not see some of its keys.
+    auto tile = [&](auto edge_, int it) {
       constexpr bool edge = edge_;
+      const int key0 = begin + it * kStep;
       floatx4 s[NB][2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -223,13 +229,17 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
         for (int n = 0; n < NB; ++n) s[n][j] = floatx4{};
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const half8 kf = values8(f.kc[j][i], f.kp[j][NG == 8 ? i / 4 : 0]);
+          const half8 kf = values8(kc[j][i], kp[j][NG == 8 ? i / 4 : 0]);
 #pragma unroll
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int part = 0; part < PARTS; ++part) s[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][part][i], s[n][j], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + 1 < count) fetch_keys();
+      if (it + 2 < count) find(key0 + 2 * kStep);
+      __builtin_amdgcn_sched_barrier(0);
       half8 pf[NB][PARTS];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -278,12 +288,13 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
       // Values. Where some row does not see some key, a masked key's exponential is zero, but zero times an infinity or a
       // NaN is not: values of keys that no row sees are cleared, and those that are not finite leave the product and
       // are added to the rows that see their key.
+      __builtin_amdgcn_sched_barrier(0);
       int odd = 0;
       half2 scale[4], low[4];
       uint32_t mask[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {  // pairs of keys
-        scale[e] = scales2(f.vp[2 * e], f.vp[2 * e + 1]), low[e] = lows2(f.vp[2 * e], f.vp[2 * e + 1]);
+        scale[e] = scales2(vp[2 * e], vp[2 * e + 1]), low[e] = lows2(vp[2 * e], vp[2 * e + 1]);
         if constexpr (edge) {
           const int key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
           mask[e] = (key >= any_lo && key <= any_hi ? 0xffffu : 0u) | (key + 1 >= any_lo && key + 1 <= any_hi ? 0xffff0000u : 0u);
@@ -294,7 +305,7 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
         uint32_t even[4], odds[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const uint32_t w = __builtin_amdgcn_perm(f.vc[2 * e + 1][b / 4], f.vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
+          const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
           even[e] = values2(codes_low(w), scale[e], low[e]);
           odds[e] = values2(codes_high(w), scale[e], low[e]);
           if constexpr (edge) even[e] = finite2h(even[e], mask[e], &odd), odds[e] = finite2h(odds[e], mask[e], &odd);
@@ -310,54 +321,51 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
           }
       }
       if (edge && __any(odd)) {
+        // A key at a time: its values alone in the left operand, ones in the other, give every row its values; those that are not finite
+        // are added where the row sees the key.
+        const uint32_t one2 = bits_of(half2{1.0f16, 1.0f16});
+        const half8 ones = __builtin_bit_cast(half8, uint4{one2, one2, one2, one2});
         const int from = max(key0, any_lo), to = min(key0 + KEYS - 1, any_hi);
 #pragma unroll 1
         for (int key = from; key <= to; ++key) {
-          int slot;
-          const int64_t page = page_of_entry(p.c, entry_at(p.c, u.b, key, 1, &slot));
-          const char* const row = vb + page * p.c.v_page + slot * p.c.v_slot;
-          const char* const pairs = vsb + page * pp.s.v_page + slot * pp.s.v_slot;
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+          for (int b = 0; b < NG; ++b) {
+            uint32_t x[2][4];
 #pragma unroll
-            for (int b = 0; b < NG; ++b) {
-              const int byte = NG * (4 * quad + r) + b;
-              if (byte >= 16 * pp.groups) continue;
-              const uint32_t w = *reinterpret_cast<const uint8_t*>(row + byte), pair = *reinterpret_cast<const uint32_t*>(pairs + byte / 16 * 4);
-              const half2 v = half2_of(values2(codes_low(w | w >> 4 << 16), scales2(pair, pair), lows2(pair, pair)));
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float x = (float)v[k];
-                if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) {
-#pragma unroll
-                  for (int n = 0; n < NB; ++n)
-                    if (key >= seen[n].lo && key <= seen[n].hi) o[n][2 * b + k][r] += x;
-                }
-              }
+            for (int e = 0; e < 4; ++e) {
+              const int first_key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
+              const uint32_t only = first_key == key ? 0xffffu : first_key + 1 == key ? 0xffff0000u : 0u;
+              const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
+              x[0][e] = values2(codes_low(w), scale[e], low[e]) & only;
+              x[1][e] = values2(codes_high(w), scale[e], low[e]) & only;
             }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const floatx4 got = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{x[k][0], x[k][1], x[k][2], x[k][3]}), ones, floatx4{}, 0, 0, 0);
+#pragma unroll
+              for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  if ((__float_as_uint(got[r]) & 0x7f800000u) == 0x7f800000u && key >= seen[n].lo && key <= seen[n].hi) o[n][2 * b + k][r] += got[r];
+            }
+          }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      if (it + 1 < count) fetch_values();
     };
 
-    // Page numbers are looked up two tiles ahead, codes loaded one tile ahead.
-    PackedTile<NG> even, odds;
-    PackedPlace<WHOLE> place;
     if (count > 0) {
-      find(begin, place);
-      fetch(place, even);
-      if (count > 1) find(begin + kStep, place);
+      find(begin);
+      fetch_keys();
+      fetch_values();
+      if (count > 1) find(begin + kStep);
     }
-    auto step = [&](int it, PackedTile<NG>& now, PackedTile<NG>& next) {
+#pragma unroll 1
+    for (int it = 0; it < count; ++it) {
       const int key0 = begin + it * kStep;
-      if (it + 1 < count) fetch(place, next);
-      if (it + 2 < count) find(key0 + 2 * kStep, place);
-      __builtin_amdgcn_sched_barrier(0);
-      if (key0 >= all_lo && key0 + KEYS - 1 <= all_hi) tile(std::false_type{}, key0, now);
-      else tile(std::true_type{}, key0, now);
-    };
-    for (int it = 0; it < count; it += 2) {
-      step(it, even, odds);
-      if (it + 1 < count) step(it + 1, odds, even);
+      if (key0 >= all_lo && key0 + KEYS - 1 <= all_hi) tile(std::false_type{}, it);
+      else tile(std::true_type{}, it);
     }
 
     // A row's statistics: the reference that its exponentials and their sum are relative to.
