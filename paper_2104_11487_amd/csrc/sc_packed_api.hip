@@ -27,8 +27,8 @@ void fill_packing(ScaleView* v, const skipconv_cache* c, const skipconv_packing*
 
 // The kernel and the cut of a launch, from the shapes alone (the lengths are on the device).
 struct PackedPlan {
-  bool few;
-  int log_rows, target, min_chunk, slack, units, slots;
+  bool few, wide;
+  int log_rows, keys, target, min_chunk, slack, units, slots;
   size_t part_o, part_ml;
 };
 
@@ -40,11 +40,14 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
   const int64_t reach = std::min(room, a->window < 0 ? room : (int64_t)a->window + most);  // keys that an item may have
   const auto items = [&](int log_rows) { return ((rows >> log_rows) + std::min<int64_t>(c->batch, c->tokens)) * c->kv_heads; };
   p->few = most * group <= 32;
-  p->log_rows = p->few ? 4 : 6 + packed_many_blocks_log(elem_of(c), c->head_dim);
+  p->wide = !p->few && c->dtype == SKIPCONV_BF16;
+  const bool twice = p->wide && c->head_dim <= kWideDoubleDim && most * group > 256 && (rows >> 9) * c->kv_heads >= 128;
+  p->log_rows = p->few ? 4 : p->wide ? log_packed_wide_rows(c->head_dim) + twice : 6 + packed_many_blocks_log(elem_of(c), c->head_dim);
+  p->keys = p->wide ? packed_wide_keys(c->head_dim) : kPackedKeys;
   int64_t units = items(p->log_rows);
   // Workgroups that share keys: `want`, or as many as all items' keys are least shares.
   const auto shares = [&](int want) {
-    const int64_t tiles = (reach + 2 * kPackedKeys - 2) / kPackedKeys;
+    const int64_t tiles = (reach + 2 * p->keys - 2) / p->keys;
     return (int)std::min<int64_t>(want, units * ((tiles + p->min_chunk - 1) / p->min_chunk));
   };
   if (p->few) {
@@ -52,9 +55,10 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
     p->target = reach <= 4 * kPackedKeys * kPackedFewWaves ? 0 : shares(256);
     p->slack = 0;
   } else {
-    p->min_chunk = 256 / kPackedKeys;
-    p->target = units < 512 && reach > 3 * 256 ? shares(512) : 0;
-    p->slack = p->target ? 256 / kPackedKeys : 0;
+    const int want = p->wide ? 256 : 512;  // workgroups that the GPU holds
+    p->min_chunk = 256 / p->keys;
+    p->target = units < want && reach > 3 * 256 ? shares(want) : 0;
+    p->slack = p->target ? 256 / p->keys : 0;
   }
   p->slots = 2 * p->target;
   if (p->target) units = p->target;
@@ -128,15 +132,15 @@ int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, c
   if (plan.part_o && (!workspace || !on16(workspace))) return invalid("attend: workspace must be a 16-byte aligned pointer");
   p.a.part_o = static_cast<float*>(workspace);
   p.a.part_ml = plan.part_o ? p.a.part_o + plan.part_o / 4 : nullptr;
-  p.a.log_rows = plan.log_rows, p.a.keys = kPackedKeys, p.a.target = plan.target, p.a.min_chunk = plan.min_chunk, p.a.slack = plan.slack;
+  p.a.log_rows = plan.log_rows, p.a.keys = plan.keys, p.a.target = plan.target, p.a.min_chunk = plan.min_chunk, p.a.slack = plan.slack;
   p.a.units = plan.units, p.a.slots = plan.slots;
   fill_packing(&p.s, c, s);
   p.groups = pack_groups(c->head_dim);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int whole = whole_pages(p.a.c, p.s);
   const bool half = c->dtype == SKIPCONV_BF16;
-  hipError_t e = plan.few ? (half ? launch_packed_few_bf16(p, whole, st) : launch_packed_few_f32(p, whole, st))
-                          : (half ? launch_packed_many_bf16(p, whole, st) : launch_packed_many_f32(p, whole, st));
+  hipError_t e = plan.few    ? (half ? launch_packed_few_bf16(p, whole, st) : launch_packed_few_f32(p, whole, st))
+                 : plan.wide ? launch_packed_wide_bf16(p, st) : launch_packed_many_f32(p, whole, st);
   if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), st);
   return hip_result(e, "attend launch");
 }
