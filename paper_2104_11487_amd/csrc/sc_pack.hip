@@ -203,6 +203,7 @@ hipError_t launch_pack_type(PackParams p, bool wide, hipStream_t stream) {
 // A thread makes eight values of a row: out[which][entry][head][slot][8 word ..].
 __global__ void __launch_bounds__(kThreads) unpack_kernel(UnpackParams p, int words, int64_t items) {
   const int64_t rows = (int64_t)p.kv_heads * p.c.page_size;
+  const CodeBits bits = code_bits();
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < items; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / words, entry = row / rows;
     const int word = (int)(i - row * words), rest = (int)(row - entry * rows), h = rest / p.c.page_size, slot = rest - h * p.c.page_size;
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(UnpackParams p, int wo
       if (there) {
         const char* codes = which ? p.c.v + page * p.c.v_page + h * p.c.v_head + slot * p.c.v_slot : p.c.k + page * p.c.k_page + h * p.c.k_head + slot * p.c.k_slot;
         const char* pairs = which ? p.s.v + page * p.s.v_page + h * p.s.v_head + slot * p.s.v_slot : p.s.k + page * p.s.k_page + h * p.s.k_head + slot * p.s.k_slot;
-        const uint4 v = __builtin_bit_cast(uint4, values8(reinterpret_cast<const uint32_t*>(codes)[word], reinterpret_cast<const uint32_t*>(pairs)[word >> 2]));
+        const uint4 v = __builtin_bit_cast(uint4, values8(reinterpret_cast<const uint32_t*>(codes)[word], reinterpret_cast<const uint32_t*>(pairs)[word >> 2], bits));
         out = uint4{__builtin_amdgcn_perm(v.y, v.x, 0x05040100u), __builtin_amdgcn_perm(v.w, v.z, 0x05040100u),
                     __builtin_amdgcn_perm(v.y, v.x, 0x07060302u), __builtin_amdgcn_perm(v.w, v.z, 0x07060302u)};
       }

@@ -68,6 +68,10 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     v_at[r] = v_byte + (WHOLE ? (uint32_t)((4 * quad + r) * (int)p.c.v_slot) : 0u);
     vp_at[r] = 4 * v_group + (WHOLE ? (uint32_t)((4 * quad + r) * (int)pp.s.v_slot) : 0u);
   }
+  const CodeBits bits = code_bits();
+  // page and slot strides of the keys' codes and pairs, the values' codes and pairs
+  const uint32_t k_page = alone(p.c.k_page), k_slot = alone(p.c.k_slot), ks_page = alone(pp.s.k_page), ks_slot = alone(pp.s.k_slot);
+  const uint32_t v_page = alone(p.c.v_page), v_slot = alone(p.c.v_slot), vs_page = alone(pp.s.v_page), vs_slot = alone(pp.s.v_slot);
   const uint32_t v_sel = NG >= 4 ? 0x0c040c00u : 0x0c040c00u + ((NG * col) & 3) * 0x00010001u;  // picks a byte of two words into 16-bit halves
 
   for (int64_t at = first_unit;;) {
@@ -125,10 +129,10 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     const int all_lo = last.lo, all_hi = first.hi, any_lo = first.lo, any_hi = last.hi;
 
     floatx4 o[NB][NJ];
-    float ref[NB], sum[NB];
+    float ref[NB], sum[NB], raised[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-      ref[n] = kNegInf, sum[n] = 0.0f;
+      ref[n] = raised[n] = kNegInf, sum[n] = 0.0f;
 #pragma unroll
       for (int j = 0; j < NJ; ++j) o[n][j] = floatx4{};
     }
@@ -152,7 +156,7 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     PackedPlace<WHOLE> place;
     const char* v_rows[2];  // whole pages: a block's first value, its pairs
     const char* v_pairs[2];
-    int v_page = 0, v_slot = 0;  // otherwise: the lane's key's
+    int page_l = 0, slot_l = 0;  // otherwise: the lane's key's
 
     auto find = [&](int key0) {
       if constexpr (WHOLE) {
@@ -164,43 +168,43 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     };
     auto load_key = [&](const char* row, const char* pairs, uint32_t* codes, uint32_t* pair) {
       if constexpr (NG == 1) {
-        codes[0] = *reinterpret_cast<const uint32_t*>(row + k_at[0]);
+        codes[0] = *reinterpret_cast<const uint32_t*>(row + here(k_at[0]));
       } else if constexpr (NG == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + k_at[0]);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(row + here(k_at[0]));
         codes[0] = w[0], codes[1] = w[1];
       } else {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-          const uint4 w = *reinterpret_cast<const uint4*>(row + k_at[i]);
+          const uint4 w = *reinterpret_cast<const uint4*>(row + here(k_at[i]));
           codes[4 * i] = w.x, codes[4 * i + 1] = w.y, codes[4 * i + 2] = w.z, codes[4 * i + 3] = w.w;
         }
       }
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) pair[i] = *reinterpret_cast<const uint32_t*>(pairs + kp_at[i]);
+      for (int i = 0; i < PIECES; ++i) pair[i] = *reinterpret_cast<const uint32_t*>(pairs + here(kp_at[i]));
     };
     auto load_value = [&](const char* row, const char* pairs, int r, uint32_t* codes, uint32_t* pair) {
       if constexpr (PIECES == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + v_at[r]);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(row + here(v_at[r]));
         codes[0] = w[0], codes[1] = w[1];
       } else {
-        codes[0] = *reinterpret_cast<const uint32_t*>(row + v_at[r]);
+        codes[0] = *reinterpret_cast<const uint32_t*>(row + here(v_at[r]));
       }
-      *pair = *reinterpret_cast<const uint32_t*>(pairs + vp_at[r]);
+      *pair = *reinterpret_cast<const uint32_t*>(pairs + here(vp_at[r]));
     };
     auto fetch_keys = [&]() {  // of the tile at `place`, which then is free
       if constexpr (WHOLE) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const uint64_t page = (uint32_t)page_of_entry(p.c, uniform(place.entry[j])), slot = (uint32_t)uniform(place.slot[j]);
-          load_key(kb + (page * (uint32_t)p.c.k_page + slot * (uint32_t)p.c.k_slot), ksb + (page * (uint32_t)pp.s.k_page + slot * (uint32_t)pp.s.k_slot), kc[j], kp[j]);
-          v_rows[j] = vb + (page * (uint32_t)p.c.v_page + slot * (uint32_t)p.c.v_slot);
-          v_pairs[j] = vsb + (page * (uint32_t)pp.s.v_page + slot * (uint32_t)pp.s.v_slot);
+          load_key(kb + (page * k_page + slot * k_slot), ksb + (page * ks_page + slot * ks_slot), kc[j], kp[j]);
+          v_rows[j] = vb + (page * v_page + slot * v_slot);
+          v_pairs[j] = vsb + (page * vs_page + slot * vs_slot);
         }
       } else {
-        v_page = page_of_entry(p.c, place.entry[0]), v_slot = place.slot[0];
+        page_l = page_of_entry(p.c, place.entry[0]), slot_l = place.slot[0];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int64_t page = __shfl(v_page, 16 * j + col), slot = __shfl(v_slot, 16 * j + col);
+          const int64_t page = __shfl(page_l, 16 * j + col), slot = __shfl(slot_l, 16 * j + col);
           load_key(kb + page * p.c.k_page + slot * p.c.k_slot, ksb + page * pp.s.k_page + slot * pp.s.k_slot, kc[j], kp[j]);
         }
       }
@@ -211,14 +215,15 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
         if constexpr (WHOLE) {
           load_value(v_rows[e / 4], v_pairs[e / 4], e % 4, vc[e], &vp[e]);
         } else {
-          const int64_t page = __shfl(v_page, 16 * (e / 4) + 4 * quad + e % 4), slot = __shfl(v_slot, 16 * (e / 4) + 4 * quad + e % 4);
+          const int64_t page = __shfl(page_l, 16 * (e / 4) + 4 * quad + e % 4), slot = __shfl(slot_l, 16 * (e / 4) + 4 * quad + e % 4);
           load_value(vb + page * p.c.v_page + slot * p.c.v_slot, vsb + page * pp.s.v_page + slot * pp.s.v_slot, 0, vc[e], &vp[e]);
         }
       }
     };
 
     // One tile's work, and the loads of the next one, whose keys take the place of this one's as soon as these are in the product, and values
-    // likewise. edge: some row does not see some of its keys.
+    // likewise. edge: some row does not see some of its keys. Where a score passes the reference by more than the slack nothing is done but to
+    // raise it, and the tile is to be gone through again: so the outputs' registers are touched by products alone in the loop, and keep their places.
     auto tile = [&](auto edge_, int it) {
       constexpr bool edge = edge_;
       const int key0 = begin + it * kStep;
@@ -229,18 +234,15 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
         for (int n = 0; n < NB; ++n) s[n][j] = floatx4{};
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const half8 kf = values8(kc[j][i], kp[j][NG == 8 ? i / 4 : 0]);
+          const half8 kf = values8(kc[j][i], kp[j][NG == 8 ? i / 4 : 0], bits);
 #pragma unroll
           for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int part = 0; part < PARTS; ++part) s[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][part][i], s[n][j], 0, 0, 0);
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (it + 1 < count) fetch_keys();
-      if (it + 2 < count) find(key0 + 2 * kStep);
-      __builtin_amdgcn_sched_barrier(0);
-      half8 pf[NB][PARTS];
+      bool past = false;
+      float top[NB];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         if constexpr (edge) {
@@ -252,22 +254,26 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
               s[n][j][r] = key >= seen[n].lo && key <= seen[n].hi ? s[n][j][r] : kNegInf;
             }
         }
-        float top = s[n][0][0];
+        top[n] = s[n][0][0];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][j][r]);
-        top = max_across32(max_across16(top)) * factor[n];
-        if (__any(top > ref[n] + kPackedSlack)) {
-          const float to = fmaxf(ref[n], top);
-          const float keep = to == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref[n] - to);
-          ref[n] = to;
-          sum[n] *= keep;
+          for (int r = 0; r < 4; ++r) top[n] = fmaxf(top[n], s[n][j][r]);
+        top[n] = max_across32(max_across16(top[n])) * factor[n];
+        past = past || top[n] > ref[n] + kPackedSlack;
+      }
+      if (__any(past)) {
 #pragma unroll
-          for (int j = 0; j < NJ; ++j)
+        for (int n = 0; n < NB; ++n) raised[n] = fmaxf(ref[n], top[n]);
+        return false;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      fetch_keys();
+      find(key0 + 2 * kStep);
+      __builtin_amdgcn_sched_barrier(0);
+      half8 pf[NB][PARTS];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[n][j][r] *= keep;
-        }
+      for (int n = 0; n < NB; ++n) {
         const float base = ref[n] == kNegInf ? 0.0f : ref[n] - kPackedLift;
         uint32_t w[PARTS][4];
 #pragma unroll
@@ -306,8 +312,8 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
-          even[e] = values2(codes_low(w), scale[e], low[e]);
-          odds[e] = values2(codes_high(w), scale[e], low[e]);
+          even[e] = values2(codes_low(w, bits), scale[e], low[e]);
+          odds[e] = values2(codes_high(w, bits), scale[e], low[e]);
           if constexpr (edge) even[e] = finite2h(even[e], mask[e], &odd), odds[e] = finite2h(odds[e], mask[e], &odd);
         }
         const half8 v0 = __builtin_bit_cast(half8, uint4{even[0], even[1], even[2], even[3]});
@@ -336,8 +342,8 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
               const int first_key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
               const uint32_t only = first_key == key ? 0xffffu : first_key + 1 == key ? 0xffff0000u : 0u;
               const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
-              x[0][e] = values2(codes_low(w), scale[e], low[e]) & only;
-              x[1][e] = values2(codes_high(w), scale[e], low[e]) & only;
+              x[0][e] = values2(codes_low(w, bits), scale[e], low[e]) & only;
+              x[1][e] = values2(codes_high(w, bits), scale[e], low[e]) & only;
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -352,20 +358,37 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (it + 1 < count) fetch_values();
+      fetch_values();
+      return true;
+    };
+    auto raise = [&]() {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        const float keep = raised[n] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref[n] - raised[n]);
+        ref[n] = raised[n];
+        sum[n] *= keep;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[n][j][r] *= keep;
+      }
     };
 
     if (count > 0) {
       find(begin);
       fetch_keys();
       fetch_values();
-      if (count > 1) find(begin + kStep);
+      find(begin + kStep);
     }
+    // Tiles that all rows see whole have a loop of their own. The last tile's loads are of tiles past it, which no product takes.
+    const int inside_lo = uniform(all_lo), inside_hi = uniform(all_hi) - KEYS + 1;
+    for (int it = 0; it < count;) {
 #pragma unroll 1
-    for (int it = 0; it < count; ++it) {
-      const int key0 = begin + it * kStep;
-      if (key0 >= all_lo && key0 + KEYS - 1 <= all_hi) tile(std::false_type{}, it);
-      else tile(std::true_type{}, it);
+      for (; it < count && begin + it * kStep >= inside_lo && begin + it * kStep <= inside_hi && tile(std::false_type{}, it); ++it) {}
+      if (it >= count) break;
+      if (begin + it * kStep >= inside_lo && begin + it * kStep <= inside_hi) raise();
+      else if (tile(std::true_type{}, it)) ++it;
+      else raise();
     }
 
     // A row's statistics: the reference that its exponentials and their sum are relative to.

@@ -36,6 +36,7 @@ struct PackedStager {
   uint4 codes[kItems];
   uint32_t pair[kItems];
   int entry[kItems], slot[kItems];  // of the tile to be loaded next
+  const CodeBits bits = code_bits();
 
   __device__ __forceinline__ PackedStager(const PackedAttendParams& q, const Unit& u, int thread, int g, uint32_t at, int first)
       : p(q), b(u.b), head(u.head), groups(g), first_key(first), hi(u.hi), lds0(at) {
@@ -73,7 +74,7 @@ struct PackedStager {
     const uint32_t at = lds0 + region + r * TL::kRowBytes, sw = TL::swizzle(r) & (TL::kChunks - 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const u32x4_lds v = clear ? u32x4_lds{0u, 0u, 0u, 0u} : __builtin_bit_cast(u32x4_lds, values8(w[i], s));
+      const u32x4_lds v = clear ? u32x4_lds{0u, 0u, 0u, 0u} : __builtin_bit_cast(u32x4_lds, values8(w[i], s, bits));
       *(__attribute__((address_space(3))) u32x4_lds*)(at + (((4 * g + i) ^ sw) << 4)) = v;
     }
   }

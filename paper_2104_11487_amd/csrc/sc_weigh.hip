@@ -40,6 +40,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) weigh_kernel(WeighParams p) {
   constexpr int kWords = kHalf ? 4 : 8;  // registers of eight elements
   using Q = std::conditional_t<kHalf, uint16_t, float>;
   __shared__ float shares[kWaves][kWaveKeys];
+  const CodeBits bits = code_bits();
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
   // Sequences by 64s, one a lane, and where their units end.
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) weigh_kernel(WeighParams p) {
           const bool there = i < p.groups;
           const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot * p.s.k_slot;
           const uint32_t w = there ? reinterpret_cast<const uint32_t*>(row)[4 * i + quad] : 0u, pair = there ? reinterpret_cast<const uint32_t*>(pairs)[i] : 0u;
-          const half8 v = values8(w, pair);
+          const half8 v = values8(w, pair, bits);
           const float x[8] = {(float)v[0], (float)v[2], (float)v[4], (float)v[6], (float)v[1], (float)v[3], (float)v[5], (float)v[7]};
           if constexpr (kHalf) {
 #pragma unroll
