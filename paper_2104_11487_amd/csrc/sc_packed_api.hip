@@ -103,7 +103,7 @@ int skipconv_packed_append(const skipconv_cache* c, const skipconv_packing* s, c
   bool wide;
   if (int e = take_append(c, a, &p.r, &wide)) return e;
   if (p.r.tokens == 0) return SKIPCONV_OK;
-  if (c->tokens > 4 * kMostGroups) return fail(SKIPCONV_E_UNSUPPORTED, "append: too many rows");
+  if (c->tokens > 4 * kMostGroups || p.r.heads[0] + 2ll * c->kv_heads > 1 << 16) return fail(SKIPCONV_E_UNSUPPORTED, "append: too many rows");
   fill_packing(&p.s, c, s);
   return hip_result(launch_pack(p, c->dtype, wide, static_cast<hipStream_t>(stream)), "append launch");
 }
@@ -203,20 +203,22 @@ int skipconv_cache_evict(const skipconv_cache* c, const skipconv_packing* s, con
   if (c->batch == 0) return SKIPCONV_OK;
   if (!e->weights || !e->into || !e->lengths || !e->kept) return invalid("evict: NULL pointer");
   if (((uintptr_t)e->weights | (uintptr_t)e->into | (uintptr_t)e->lengths | (uintptr_t)e->kept) % 4 != 0) return invalid("evict: a tensor is not aligned to its elements");
-  if ((int64_t)c->batch * c->kv_heads > kMostGroups / (std::min<int64_t>(e->keep, room) / 64 + 1)) return fail(SKIPCONV_E_UNSUPPORTED, "evict: too many rows");
+  if ((int64_t)c->batch * c->kv_heads > kMostGroups / (std::min<int64_t>(e->keep, room) / 8 + 1)) return fail(SKIPCONV_E_UNSUPPORTED, "evict: too many rows");
   EvictParams p = {};
   fill_cache(&p.c, &no_rows);
   const int64_t unit = s ? 1 : elem_of(c);
   const int row = s ? pack_groups(c->head_dim) * 16 : c->head_dim * elem_of(c);
-  p.part[0] = {p.c.k, p.c.k_page * unit, p.c.k_head * unit, p.c.k_slot * unit, row / 16, 16};
-  p.part[1] = {p.c.v, p.c.v_page * unit, p.c.v_head * unit, p.c.v_slot * unit, row / 16, 16};
-  p.parts = 2;
+  const auto add = [&](char* base, int64_t page, int64_t head, int64_t slot, int bytes) {
+    const bool wide = ((uintptr_t)base | (uint64_t)page | (uint64_t)head | (uint64_t)slot | (uint64_t)bytes) % 16 == 0;
+    p.part[p.parts++] = {base, page, head, slot, bytes / (wide ? 16 : 4), wide ? 16 : 4};
+  };
+  add(p.c.k, p.c.k_page * unit, p.c.k_head * unit, p.c.k_slot * unit, row);
+  add(p.c.v, p.c.v_page * unit, p.c.v_head * unit, p.c.v_slot * unit, row);
   if (s) {
     ScaleView v;
     fill_packing(&v, c, s);
-    p.part[2] = {v.k, v.k_page, v.k_head, v.k_slot, pack_groups(c->head_dim), 4};
-    p.part[3] = {v.v, v.v_page, v.v_head, v.v_slot, pack_groups(c->head_dim), 4};
-    p.parts = 4;
+    add(v.k, v.k_page, v.k_head, v.k_slot, 4 * pack_groups(c->head_dim));
+    add(v.v, v.v_page, v.v_head, v.v_slot, 4 * pack_groups(c->head_dim));
   }
   p.weights = e->weights, p.into = e->into, p.lengths = e->lengths, p.kept = e->kept;
   p.kv_heads = c->kv_heads, p.into_width = e->into_width, p.keep = e->keep, p.recent = e->recent;
