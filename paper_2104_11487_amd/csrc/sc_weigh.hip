@@ -2,10 +2,11 @@
 //   w_l <- decay w_l + sum over the rows (new token, query head of the key head) that see l of exp(scale q . k_l - lse)
 // (a new token's own: the sum alone). Scores as in the attention kernels, transposed: S' = K Q', keys held in registers, rows streamed.
 //
-// A unit of work is a tile of keys of one sequence and key head; workgroups take units in turn (lengths are on the device, so the launch does
-// not know how many there are). Where rows are few the four waves take 32 keys each; where they are many the waves take
-// the same 32 keys and every fourth block of 16 rows, and are added in LDS, in wave order: no atomics, equal calls give equal bits.
-// Keys in 4 bits are fp16 numbers, which two bf16 parts hold exactly (8 + 3 bits), so bf16 queries enter the product as they are.
+// A unit of work is a tile of keys of one sequence and key head; a workgroup takes an equal share of them in a row (lengths are on the device, so
+// the launch does not know how many there are). Where rows are few the four waves take 32 keys each, and keep the rows' operand while the share
+// stays with a key head; where they are many the waves take the same keys and every fourth block of 16 rows, and are added in LDS, in wave
+// order: no atomics, equal calls give equal bits. Keys in 4 bits are fp16 numbers: few rows of bf16 come into fp16, exactly, by a power of two
+// (as in sc_packed_attend.h); for many rows, that would cost more than it saves, and the keys become two bf16 parts (8 + 3 bits) instead.
 #include "sc_packed_device.h"
 
 #include <algorithm>
@@ -17,8 +18,23 @@ namespace sc {
 
 namespace {
 
-constexpr int kWaves = 4, kWaveKeys = 32;
+constexpr int kWaves = 4;
 constexpr float kLog2e = 1.4426950408889634f;
+
+// KIND of the keys: 0 fp32, 1 bf16, 2 packed with bf16 queries, 3 packed with fp32 queries. SPLIT: the waves share the rows.
+template <int KIND, int NG, bool SPLIT>
+struct Weigh {
+  static constexpr bool kHalf = KIND == 1 || KIND == 2, kPacked = KIND >= 2;
+  static constexpr bool kScaled = KIND == 2 && !SPLIT;  // products in fp16
+  static constexpr int kParts = KIND == 2 && SPLIT ? 2 : 1;
+  static constexpr int kWords = kHalf ? 4 : 8;          // registers of eight elements
+  static constexpr int kRegs = NG * kParts * kWords;    // of a block of 16 keys
+  static constexpr int kBlocks = SPLIT && kRegs <= 16 ? 4 : kRegs <= 32 ? 2 : 1;  // that a wave holds
+  static constexpr int kKeys = 16 * kBlocks * (SPLIT ? 1 : kWaves);  // of a unit
+  static constexpr int kOperands = kBlocks * kRegs + 2 * NG * kWords;
+  static constexpr int kWavesPerSimd = kOperands <= 48 ? (SPLIT ? 3 : 4) : kOperands <= 64 ? 3 : 2;
+  using Q = std::conditional_t<kHalf, uint16_t, float>;
+};
 
 // Inclusive sum over the wave's lanes.
 __device__ __forceinline__ int64_t scan64(int64_t v) {
@@ -32,149 +48,242 @@ __device__ __forceinline__ int64_t scan64(int64_t v) {
   return v;
 }
 
-// KIND of the keys: 0 fp32, 1 bf16, 2 packed with bf16 queries, 3 packed with fp32 queries. SPLIT: the waves share the rows.
 template <int KIND, int NG, bool SPLIT>
-__global__ void __launch_bounds__(64 * kWaves, 2) weigh_kernel(WeighParams p) {
-  constexpr bool kHalf = KIND == 1 || KIND == 2, kPacked = KIND >= 2;
-  constexpr int PARTS = KIND == 2 ? 2 : 1, KEYS = SPLIT ? kWaveKeys : kWaveKeys * kWaves;
-  constexpr int kWords = kHalf ? 4 : 8;  // registers of eight elements
-  using Q = std::conditional_t<kHalf, uint16_t, float>;
-  __shared__ float shares[kWaves][kWaveKeys];
+__global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPerSimd)) weigh_kernel(WeighParams p) {
+  using W = Weigh<KIND, NG, SPLIT>;
+  using Q = typename W::Q;
+  constexpr bool kHalf = W::kHalf;
+  constexpr int PARTS = W::kParts, KEYS = W::kKeys, BLOCKS = W::kBlocks, kWords = W::kWords;
+  __shared__ float shares[SPLIT ? kWaves : 1][16 * BLOCKS];
   const CodeBits bits = code_bits();
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
 
   // Sequences by 64s, one a lane, and where their units end.
   const auto units_of = [&](const Sequence& s) { return s.n > 0 ? (int64_t)((s.len + KEYS - 1) / KEYS) * p.kv_heads : 0; };
   const auto load = [&](int b) { return b < p.c.batch ? sequence_of(p.c, b) : Sequence{0, 0, 0}; };
-  int b0 = 0;
-  int64_t base = 0;
   Sequence mine = load(lane);
   int64_t upto = scan64(units_of(mine)), all = from_lane(upto, 63);
-  for (int64_t unit = blockIdx.x;; unit += gridDim.x) {
-    while (unit >= base + all) {
-      base += all;
-      b0 += 64;
-      if (b0 >= p.c.batch) return;
-      mine = load(b0 + lane);
-      upto = scan64(units_of(mine)), all = from_lane(upto, 63);
-    }
-    const int src = (int)__ffsll((unsigned long long)__ballot(base + upto > unit)) - 1, b = b0 + src;
-    const Sequence s = {__builtin_amdgcn_readlane(mine.start, src), __builtin_amdgcn_readlane(mine.n, src), __builtin_amdgcn_readlane(mine.len, src)};
-    const int tiles = (s.len + KEYS - 1) / KEYS;
-    const int64_t rel = unit - (base + from_lane(upto, src) - (int64_t)tiles * p.kv_heads);
-    const int head = (int)divide(rel, tiles), key0 = (int)(rel - (int64_t)head * tiles) * KEYS + (SPLIT ? 0 : wave * kWaveKeys);
+  int64_t total = all;
+  for (int b = 64; b < p.c.batch; b += 64) total += from_lane(scan64(units_of(load(b + lane))), 63);
+  const int64_t share = divide(total, gridDim.x), rest = total - share * gridDim.x;
+  int64_t unit = blockIdx.x * share + min((int64_t)blockIdx.x, rest);
+  const int64_t end = unit + share + ((int64_t)blockIdx.x < rest ? 1 : 0);
 
-    // the keys, in the left operand's layout: lane (key of the block, quarter) holds elements 32 i + 8 quad ..
-    uint32_t kf[2][PARTS][NG][kWords];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      int slot;
-      const int64_t page = page_of_entry(p.c, entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot));
-      const char* const row = p.c.k + page * p.c.k_page + (int64_t)head * p.c.k_head + slot * p.c.k_slot;
+  int b0 = 0, b = 0, head = 0, tile = 0, tiles = 0;
+  bool rows_held = false;  // few rows: they are in the operand
+  int64_t base = 0, sequence_end = 0;
+  Sequence s = {0, 0, 0};
+
+  // a block of rows, in the right operand's layout: lane (row of the block, quarter) holds elements 32 i + 8 quad ..
+  uint32_t qf[NG][kWords];
+  float less = 0.0f, factor = 0.0f;  // of the lane's row: lse in powers of two (infinite: it gives nothing); of a score, to powers of two
+  int seen_lo = 0, seen_hi = -1;
+
+  for (; unit < end; ++unit) {
+    if (unit >= sequence_end) {
+      while (unit >= base + all) {
+        base += all;
+        b0 += 64;
+        mine = load(b0 + lane);
+        upto = scan64(units_of(mine)), all = from_lane(upto, 63);
+      }
+      const int src = (int)__ffsll((unsigned long long)__ballot(base + upto > unit)) - 1;
+      b = b0 + src;
+      s = {__builtin_amdgcn_readlane(mine.start, src), __builtin_amdgcn_readlane(mine.n, src), __builtin_amdgcn_readlane(mine.len, src)};
+      tiles = (s.len + KEYS - 1) / KEYS;
+      sequence_end = base + from_lane(upto, src);
+      const int64_t rel = unit - (sequence_end - (int64_t)tiles * p.kv_heads);
+      head = (int)divide(rel, tiles), tile = (int)(rel - (int64_t)head * tiles);
+      rows_held = false;
+    } else if (++tile == tiles) {
+      tile = 0, ++head, rows_held = false;
+    }
+    const int key0 = tile * KEYS + (SPLIT ? 0 : wave * 16 * BLOCKS), p0 = s.len - s.n;
+
+    // new tokens that see any of the wave's keys: [i0, i1]; those that see all of them: [all0, all1]
+    const int key_end = min(key0 + 16 * BLOCKS, s.len) - 1;
+    int i0 = 0, i1 = s.n - 1, all0 = 0, all1 = s.n - 1;
+    if (p.causal) {
+      i0 = max(0, key0 - p0), all0 = max(0, key_end - p0);
+      if (p.window >= 0) i1 = (int)min((int64_t)i1, (int64_t)key_end - p0 + p.window), all1 = (int)min((int64_t)all1, (int64_t)key0 - p0 + p.window);
+    } else if (p.window >= 0) {
+      if ((int64_t)key_end < (int64_t)p0 - p.window) i1 = -1;
+      if ((int64_t)key0 < (int64_t)p0 - p.window) all1 = -1;
+    }
+    if (key0 >= s.len) i1 = -1;
+    const bool whole_keys = key0 + 16 * BLOCKS <= s.len;
+    const int rows_end = (i1 + 1) * p.group, row_begin = SPLIT ? i0 * p.group : 0;
+    // (few rows: all of them, so that the operand holds for every unit)
+    const int rows_all = SPLIT ? rows_end : s.n * p.group;
+
+    uint32_t raw[NG][kWords];
+    float raw_lse = 0.0f;
+    const auto fetch_rows = [&](int r0) {
+      const int row = min(r0 + col, rows_all - 1), t = row / p.group, h = head * p.group + (row - t * p.group);
+      const Q* const q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + t) * p.q_token + (int64_t)h * p.q_head;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int d = 32 * i + 8 * quad;
-        if constexpr (kPacked) {
-          const bool there = i < p.groups;
-          const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot * p.s.k_slot;
-          const uint32_t w = there ? reinterpret_cast<const uint32_t*>(row)[4 * i + quad] : 0u, pair = there ? reinterpret_cast<const uint32_t*>(pairs)[i] : 0u;
-          const half8 v = values8(w, pair, bits);
-          const float x[8] = {(float)v[0], (float)v[2], (float)v[4], (float)v[6], (float)v[1], (float)v[3], (float)v[5], (float)v[7]};
-          if constexpr (kHalf) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t hi = pack2(x[2 * e], x[2 * e + 1]);
-              kf[j][0][i][e] = hi;
-              kf[j][PARTS - 1][i][e] = pack2(x[2 * e] - __uint_as_float(hi << 16), x[2 * e + 1] - __uint_as_float(hi & 0xffff0000u));
+        for (int part = 0; part < kWords / 4; ++part) {
+          const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(q + d)[part] : uint4{0u, 0u, 0u, 0u};
+          raw[i][4 * part] = w.x, raw[i][4 * part + 1] = w.y, raw[i][4 * part + 2] = w.z, raw[i][4 * part + 3] = w.w;
+        }
+      }
+      raw_lse = p.lse[(int64_t)(s.start + t) * p.q_heads + h];
+    };
+    const auto take_rows = [&](int r0) {  // what was fetched
+      less = raw_lse == kNegInf ? -kNegInf : raw_lse * kLog2e;
+      if (r0 + col >= rows_all) less = -kNegInf;
+      factor = p.scale_log2;
+      if constexpr (W::kScaled) {  // the largest element comes into [2^14, 2^15)
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(raw[i][e] << 16)), fabsf(__uint_as_float(raw[i][e] & 0xffff0000u))));
+        most = max_across32(max_across16(most));
+        const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);
+        factor = ldexpf(p.scale_log2, -lift);
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[2 * e] = ldexpf(__uint_as_float(raw[i][e] << 16), lift), x[2 * e + 1] = ldexpf(__uint_as_float(raw[i][e] & 0xffff0000u), lift);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qf[i][e] = pack2h(x[e], x[e + 4]);  // in the order that the keys' codes come in
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+          for (int e = 0; e < kWords; ++e) qf[i][e] = raw[i][e];
+      }
+      const int at = p0 + min(r0 + col, rows_all - 1) / p.group, from = p.causal ? at : p0;  // the row's position
+      seen_hi = p.causal ? min(at, s.len - 1) : s.len - 1;
+      seen_lo = p.window >= 0 && from > p.window ? from - p.window : 0;
+    };
+
+    const int first_row = row_begin + (SPLIT ? 16 * wave : 0);
+    const int row_count = rows_end > 0 ? rows_all : 0;
+    if (first_row < row_count && !rows_held) fetch_rows(first_row);
+
+    // the keys, in the left operand's layout: lane (key of the block, quarter) holds elements 32 i + 8 quad ..
+    uint32_t kf[BLOCKS][PARTS][NG][kWords];
+    if (first_row < row_count) {
+#pragma unroll
+      for (int j = 0; j < BLOCKS; ++j) {
+        int slot;
+        const int64_t page = page_of_entry(p.c, entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot));
+        const char* const row = p.c.k + page * p.c.k_page + (int64_t)head * p.c.k_head + slot * p.c.k_slot;
+        const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot * p.s.k_slot;
+        uint32_t codes[NG], pair[NG];
+        if constexpr (W::kPacked) {
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const int g = min(i, p.groups - 1);  // groups past the head's: the queries are zero there
+            codes[i] = reinterpret_cast<const uint32_t*>(row)[4 * g + quad], pair[i] = reinterpret_cast<const uint32_t*>(pairs)[g];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int d = 32 * i + 8 * quad;
+          if constexpr (W::kScaled) {
+            const uint4 v = __builtin_bit_cast(uint4, values8(codes[i], pair[i], bits));
+            kf[j][0][i][0] = v.x, kf[j][0][i][1] = v.y, kf[j][0][i][2] = v.z, kf[j][0][i][3] = v.w;
+          } else if constexpr (W::kPacked) {
+            const half8 v = values8(codes[i], pair[i], bits);
+            const float x[8] = {(float)v[0], (float)v[2], (float)v[4], (float)v[6], (float)v[1], (float)v[3], (float)v[5], (float)v[7]};
+            if constexpr (kHalf) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t hi = pack2(x[2 * e], x[2 * e + 1]);
+                kf[j][0][i][e] = hi;
+                kf[j][PARTS - 1][i][e] = pack2(x[2 * e] - __uint_as_float(hi << 16), x[2 * e + 1] - __uint_as_float(hi & 0xffff0000u));
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) kf[j][0][i][e] = __float_as_uint(x[e]);
             }
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) kf[j][0][i][e] = __float_as_uint(x[e]);
-          }
-        } else {
-          const uint4 none{0u, 0u, 0u, 0u};
-#pragma unroll
-          for (int part = 0; part < kWords / 4; ++part) {
-            const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[part] : none;
-            kf[j][0][i][4 * part] = w.x, kf[j][0][i][4 * part + 1] = w.y, kf[j][0][i][4 * part + 2] = w.z, kf[j][0][i][4 * part + 3] = w.w;
+            for (int part = 0; part < kWords / 4; ++part) {
+              const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[part] : uint4{0u, 0u, 0u, 0u};
+              kf[j][0][i][4 * part] = w.x, kf[j][0][i][4 * part + 1] = w.y, kf[j][0][i][4 * part + 2] = w.z, kf[j][0][i][4 * part + 3] = w.w;
+            }
           }
         }
       }
     }
-
-    // new tokens that see any of the keys: [i0, i1]
-    const int p0 = s.len - s.n, key_end = min(key0 + kWaveKeys, s.len) - 1;
-    int i0 = 0, i1 = s.n - 1;
-    if (p.causal) {
-      i0 = max(0, key0 - p0);
-      if (p.window >= 0) i1 = (int)min((int64_t)i1, (int64_t)key_end - p0 + p.window);
-    } else if (p.window >= 0 && (int64_t)key_end < (int64_t)p0 - p.window) {
-      i1 = -1;
-    }
-    if (key0 >= s.len) i1 = -1;
-    floatx4 got[2] = {floatx4{}, floatx4{}};
-    const int rows_end = (i1 + 1) * p.group;
-    for (int r0 = i0 * p.group + (SPLIT ? 16 * wave : 0); r0 < rows_end; r0 += SPLIT ? 16 * kWaves : 16) {
-      const int row = min(r0 + col, rows_end - 1), t = row / p.group, h = head * p.group + (row - t * p.group);
-      const Q* const q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + t) * p.q_token + (int64_t)h * p.q_head;
-      const float l = p.lse[(int64_t)(s.start + t) * p.q_heads + h];
-      const float less = l == kNegInf ? -kNegInf : l * kLog2e;  // a row that sees nothing gives nothing
-      floatx4 score[2] = {floatx4{}, floatx4{}};
+    floatx4 got[BLOCKS];
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int d = 32 * i + 8 * quad;
-        uint4 w[kWords / 4];
+    for (int j = 0; j < BLOCKS; ++j) got[j] = floatx4{};
+    // The held rows' scores with the held keys, and what they give. inside: every row sees every key.
+    const auto add = [&](bool inside) {
 #pragma unroll
-        for (int part = 0; part < kWords / 4; ++part) w[part] = d < p.dim ? reinterpret_cast<const uint4*>(q + d)[part] : uint4{0u, 0u, 0u, 0u};
+      for (int j = 0; j < BLOCKS; ++j) {
+        floatx4 score = floatx4{};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < NG; ++i)
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) {
             const uint32_t* const k = kf[j][part][i];
-            if constexpr (kHalf) {
-              score[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(bf16x8, w[0]), score[j], 0, 0, 0);
+            if constexpr (W::kScaled) {
+              score = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(half8, uint4{qf[i][0], qf[i][1], qf[i][2], qf[i][3]}), score, 0, 0, 0);
+            } else if constexpr (kHalf) {
+              score = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(bf16x8, uint4{qf[i][0], qf[i][1], qf[i][2], qf[i][3]}), score, 0, 0, 0);
             } else {
-              const float x[8] = {__uint_as_float(w[0].x), __uint_as_float(w[0].y), __uint_as_float(w[0].z), __uint_as_float(w[0].w),
-                                  __uint_as_float(w[kWords / 4 - 1].x), __uint_as_float(w[kWords / 4 - 1].y), __uint_as_float(w[kWords / 4 - 1].z), __uint_as_float(w[kWords / 4 - 1].w)};
 #pragma unroll
-              for (int e = 0; e < 8; ++e) score[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), x[e], score[j], 0, 0, 0);
+              for (int e = 0; e < 8; ++e) score = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[i][e % kWords]), score, 0, 0, 0);
             }
           }
-      }
-      const int at = p0 + t;  // the row's position
-      const int hi = p.causal ? min(at, s.len - 1) : s.len - 1, from = p.causal ? at : p0;
-      const int lo = p.window >= 0 && from > p.window ? from - p.window : 0;
-      const bool live = r0 + col < rows_end;
+        if (inside) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+          for (int r = 0; r < 4; ++r) got[j][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(score[r], factor, -less));
+        } else {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = key0 + 16 * j + 4 * quad + r;
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[j][r], p.scale_log2, -less));
-          got[j][r] += live && key >= lo && key <= hi ? e : 0.0f;
+          for (int r = 0; r < 4; ++r) {
+            const int key = key0 + 16 * j + 4 * quad + r;
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[r], factor, -less));
+            got[j][r] += less != -kNegInf && key >= seen_lo && key <= seen_hi ? e : 0.0f;
+          }
         }
+      }
+    };
+    const auto inside_of = [&](int r0) {  // whether all 16 rows from r0 on are rows and see all keys (uniform)
+      return whole_keys && r0 + 16 <= rows_all && r0 / p.group >= all0 && (r0 + 15) / p.group <= all1;
+    };
+
+#pragma unroll 1
+    for (int r0 = first_row; r0 < row_count; r0 += SPLIT ? 16 * kWaves : 16) {
+      if (!rows_held) take_rows(r0);
+      if (r0 + (SPLIT ? 16 * kWaves : 16) < row_count) fetch_rows(r0 + (SPLIT ? 16 * kWaves : 16));
+      if (inside_of(r0)) add(true);
+      else add(false);
     }
-    // over the 16 rows of a block; lane r of a quarter then stores its key r's of the first block, lane 4 + r of the second
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) got[j][r] += __shfl_xor(got[j][r], m);
-    const int j = col >> 2 & 1;
+    rows_held = rows_held || (!SPLIT && row_count > 0 && row_count <= 16);
+
+    // over the 16 rows of a block; lane r of a quarter then has its key r's of the first block, lane 4 + r of the second, ..
     float sum = 0.0f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) sum = (col & 3) == r ? (j ? got[1][r] : got[0][r]) : sum;
-    const int local = 16 * j + 4 * quad + (col & 3), key = key0 + local;
+    for (int j = 0; j < BLOCKS; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) got[j][r] += __shfl_xor(got[j][r], m);
+        sum = col == 4 * j + r ? got[j][r] : sum;
+      }
+    const int local = 16 * (col >> 2) + 4 * quad + (col & 3), key = key0 + local;
+    const bool mine_to_store = col < 4 * BLOCKS && key < s.len;
     if constexpr (SPLIT) {
-      if (col < 8) shares[wave][local] = sum;
+      if (col < 4 * BLOCKS) shares[wave][local] = sum;
       __syncthreads();
       sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) sum += shares[w][local];
+      for (int w = 0; w < kWaves; ++w) sum += shares[w][col < 4 * BLOCKS ? local : 0];
       __syncthreads();  // read before the next unit writes
     }
-    if (col < 8 && key < s.len && (!SPLIT || wave == 0)) {
+    if (mine_to_store && (!SPLIT || wave == 0)) {
       const int i = page_of(p.c, key);
       const int page = i < p.c.width ? p.c.table[(int64_t)b * p.c.width + i] : -1;
       if (page >= 0 && page < p.c.pages) {
@@ -188,7 +297,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) weigh_kernel(WeighParams p) {
 template <int KIND, int NG>
 hipError_t launch(const WeighParams& p, bool split, hipStream_t stream) {
   const int64_t most = (int64_t)p.c.batch * p.kv_heads * p.tiles;
-  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(most, 1), 2048)), block(64 * kWaves);
+  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(most, 1), split ? 1024 : 2048)), block(64 * kWaves);
   if (split) weigh_kernel<KIND, NG, true><<<grid, block, 0, stream>>>(p);
   else weigh_kernel<KIND, NG, false><<<grid, block, 0, stream>>>(p);
   return hipGetLastError();
