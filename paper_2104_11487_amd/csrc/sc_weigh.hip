@@ -28,11 +28,14 @@ struct Weigh {
   static constexpr bool kScaled = KIND == 2 && !SPLIT;  // products in fp16
   static constexpr int kParts = KIND == 2 && SPLIT ? 2 : 1;
   static constexpr int kWords = kHalf ? 4 : 8;          // registers of eight elements
-  static constexpr int kRegs = NG * kParts * kWords;    // of a block of 16 keys
-  static constexpr int kBlocks = SPLIT && kRegs <= 16 ? 4 : kRegs <= 32 ? 2 : 1;  // that a wave holds
+  static constexpr int kRegs = NG * kParts * kWords;    // of an operand of 16 keys
+  static constexpr int kRaw = kPacked ? 2 * NG : NG * kWords;  // of 16 keys as they lie in memory: codes and pairs, or elements
+  // 16-key blocks of a wave: where rows are many it holds their operands; otherwise they are formed for each block of rows, from
+  // what was loaded, all blocks' loads in flight together
+  static constexpr int kBlocks = SPLIT ? (kRegs <= 16 ? 4 : kRegs <= 32 ? 2 : 1) : kRaw <= 16 ? 4 : kRaw <= 32 ? 2 : 1;
   static constexpr int kKeys = 16 * kBlocks * (SPLIT ? 1 : kWaves);  // of a unit
-  static constexpr int kOperands = kBlocks * kRegs + 2 * NG * kWords;
-  static constexpr int kWavesPerSimd = kOperands <= 48 ? (SPLIT ? 3 : 4) : kOperands <= 64 ? 3 : 2;
+  static constexpr int kOperands = (SPLIT ? kBlocks * kRegs : kBlocks * kRaw + kRegs) + 2 * NG * kWords;
+  static constexpr int kWavesPerSimd = kOperands <= 48 ? (SPLIT ? 3 : 4) : kOperands <= 80 ? 3 : 2;
   using Q = std::conditional_t<kHalf, uint16_t, float>;
 };
 
@@ -45,6 +48,15 @@ __device__ __forceinline__ int64_t scan64(int64_t v) {
     const int64_t t = __shfl_up(v, d);
     if (lane >= d) v += t;
   }
+  return v;
+}
+
+// Sum over each row of 16 lanes, in all of them: rotations within the row.
+__device__ __forceinline__ float sum16(float v) {
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xf, 0xf, false));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x124, 0xf, 0xf, false));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x122, 0xf, 0xf, false));
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x121, 0xf, 0xf, false));
   return v;
 }
 
@@ -168,51 +180,78 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     const int row_count = rows_end > 0 ? rows_all : 0;
     if (first_row < row_count && !rows_held) fetch_rows(first_row);
 
+    // what the lane will store: its key's place, and what that held
+    const int local = 16 * (col >> 2) + 4 * quad + (col & 3), own_key = key0 + local;
+    const bool stores = col < 4 * BLOCKS && own_key < s.len && (!SPLIT || wave == 0);
+    int own_entry = -1;
+    const int own_page = min(page_of(p.c, min(own_key, kMostKeys - 1)), p.c.width - 1);
+    if (stores) own_entry = p.c.table[(int64_t)b * p.c.width + own_page];
+
     // the keys, in the left operand's layout: lane (key of the block, quarter) holds elements 32 i + 8 quad ..
-    uint32_t kf[BLOCKS][PARTS][NG][kWords];
+    uint32_t raw_keys[BLOCKS][W::kRaw];
     if (first_row < row_count) {
+      int entry[BLOCKS], slot[BLOCKS];
+#pragma unroll
+      for (int j = 0; j < BLOCKS; ++j) entry[j] = entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot[j]);
 #pragma unroll
       for (int j = 0; j < BLOCKS; ++j) {
-        int slot;
-        const int64_t page = page_of_entry(p.c, entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot));
-        const char* const row = p.c.k + page * p.c.k_page + (int64_t)head * p.c.k_head + slot * p.c.k_slot;
-        const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot * p.s.k_slot;
-        uint32_t codes[NG], pair[NG];
+        const int64_t page = page_of_entry(p.c, entry[j]);
+        const char* const row = p.c.k + page * p.c.k_page + (int64_t)head * p.c.k_head + slot[j] * p.c.k_slot;
         if constexpr (W::kPacked) {
+          const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot[j] * p.s.k_slot;
 #pragma unroll
           for (int i = 0; i < NG; ++i) {
             const int g = min(i, p.groups - 1);  // groups past the head's: the queries are zero there
-            codes[i] = reinterpret_cast<const uint32_t*>(row)[4 * g + quad], pair[i] = reinterpret_cast<const uint32_t*>(pairs)[g];
+            raw_keys[j][2 * i] = reinterpret_cast<const uint32_t*>(row)[4 * g + quad], raw_keys[j][2 * i + 1] = reinterpret_cast<const uint32_t*>(pairs)[g];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < NG; ++i) {
+            const int d = 32 * i + 8 * quad;
+#pragma unroll
+            for (int e = 0; e < kWords; e += 4) {
+              const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[e / 4] : uint4{0u, 0u, 0u, 0u};
+              uint32_t* const to = &raw_keys[j][i * kWords + e];
+              to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+            }
           }
         }
+      }
+    }
+    using Operand = uint32_t[PARTS][NG][kWords];
+    const auto form = [&](int j, Operand& kf) {
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const int d = 32 * i + 8 * quad;
+      for (int i = 0; i < NG; ++i) {
+        if constexpr (!W::kPacked) {
+#pragma unroll
+          for (int e = 0; e < kWords; ++e) kf[0][i][e] = raw_keys[j][i * kWords + e];
+        } else {
+          const half8 v = values8(raw_keys[j][2 * i], raw_keys[j][2 * i + 1], bits);
           if constexpr (W::kScaled) {
-            const uint4 v = __builtin_bit_cast(uint4, values8(codes[i], pair[i], bits));
-            kf[j][0][i][0] = v.x, kf[j][0][i][1] = v.y, kf[j][0][i][2] = v.z, kf[j][0][i][3] = v.w;
-          } else if constexpr (W::kPacked) {
-            const half8 v = values8(codes[i], pair[i], bits);
+            const uint4 w = __builtin_bit_cast(uint4, v);
+            kf[0][i][0] = w.x, kf[0][i][1] = w.y, kf[0][i][2] = w.z, kf[0][i][3] = w.w;
+          } else {
             const float x[8] = {(float)v[0], (float)v[2], (float)v[4], (float)v[6], (float)v[1], (float)v[3], (float)v[5], (float)v[7]};
             if constexpr (kHalf) {
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const uint32_t hi = pack2(x[2 * e], x[2 * e + 1]);
-                kf[j][0][i][e] = hi;
-                kf[j][PARTS - 1][i][e] = pack2(x[2 * e] - __uint_as_float(hi << 16), x[2 * e + 1] - __uint_as_float(hi & 0xffff0000u));
+                kf[0][i][e] = hi;
+                kf[PARTS - 1][i][e] = pack2(x[2 * e] - __uint_as_float(hi << 16), x[2 * e + 1] - __uint_as_float(hi & 0xffff0000u));
               }
             } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) kf[j][0][i][e] = __float_as_uint(x[e]);
-            }
-          } else {
-#pragma unroll
-            for (int part = 0; part < kWords / 4; ++part) {
-              const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[part] : uint4{0u, 0u, 0u, 0u};
-              kf[j][0][i][4 * part] = w.x, kf[j][0][i][4 * part + 1] = w.y, kf[j][0][i][4 * part + 2] = w.z, kf[j][0][i][4 * part + 3] = w.w;
+              for (int e = 0; e < 8; ++e) kf[0][i][e] = __float_as_uint(x[e]);
             }
           }
         }
+      }
+    };
+    Operand held[SPLIT ? BLOCKS : 1];
+    if constexpr (SPLIT) {
+      if (first_row < row_count) {
+#pragma unroll
+        for (int j = 0; j < BLOCKS; ++j) form(j, held[j]);
       }
     }
     floatx4 got[BLOCKS];
@@ -223,11 +262,18 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 #pragma unroll
       for (int j = 0; j < BLOCKS; ++j) {
         floatx4 score = floatx4{};
+        if constexpr (!SPLIT) {  // here, not ahead of the loop over rows: no registers hold all blocks' operands
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < W::kRaw; ++e) raw_keys[j][e] = here(raw_keys[j][e]);
+          form(j, held[0]);
+        }
+        Operand& kf = held[SPLIT ? j : 0];
 #pragma unroll
         for (int i = 0; i < NG; ++i)
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) {
-            const uint32_t* const k = kf[j][part][i];
+            const uint32_t* const k = kf[part][i];
             if constexpr (W::kScaled) {
               score = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(half8, uint4{qf[i][0], qf[i][1], qf[i][2], qf[i][3]}), score, 0, 0, 0);
             } else if constexpr (kHalf) {
@@ -258,10 +304,20 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     for (int r0 = first_row; r0 < row_count; r0 += SPLIT ? 16 * kWaves : 16) {
       if (!rows_held) take_rows(r0);
       if (r0 + (SPLIT ? 16 * kWaves : 16) < row_count) fetch_rows(r0 + (SPLIT ? 16 * kWaves : 16));
-      if (inside_of(r0)) add(true);
-      else add(false);
+      const bool inside = inside_of(r0);
+      if constexpr (SPLIT) {
+        if (inside) add(true);
+        else add(false);
+      } else {
+        add(inside);
+      }
     }
     rows_held = rows_held || (!SPLIT && row_count > 0 && row_count <= 16);
+
+    const bool there = stores && own_entry >= 0 && own_entry < p.c.pages && page_of(p.c, own_key) == own_page;
+    float* const to = p.weights + ((int64_t)(there ? own_entry : 0) * p.kv_heads + head) * p.c.page_size + (there ? own_key - own_page * p.c.page_size : 0);
+    const bool is_new = own_key >= p0;
+    const float before = there && !is_new ? *to : 0.0f;
 
     // over the 16 rows of a block; lane r of a quarter then has its key r's of the first block, lane 4 + r of the second, ..
     float sum = 0.0f;
@@ -269,12 +325,9 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     for (int j = 0; j < BLOCKS; ++j)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) got[j][r] += __shfl_xor(got[j][r], m);
-        sum = col == 4 * j + r ? got[j][r] : sum;
+        const float v = sum16(got[j][r]);
+        sum = col == 4 * j + r ? v : sum;
       }
-    const int local = 16 * (col >> 2) + 4 * quad + (col & 3), key = key0 + local;
-    const bool mine_to_store = col < 4 * BLOCKS && key < s.len;
     if constexpr (SPLIT) {
       if (col < 4 * BLOCKS) shares[wave][local] = sum;
       __syncthreads();
@@ -283,21 +336,16 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       for (int w = 0; w < kWaves; ++w) sum += shares[w][col < 4 * BLOCKS ? local : 0];
       __syncthreads();  // read before the next unit writes
     }
-    if (mine_to_store && (!SPLIT || wave == 0)) {
-      const int i = page_of(p.c, key);
-      const int page = i < p.c.width ? p.c.table[(int64_t)b * p.c.width + i] : -1;
-      if (page >= 0 && page < p.c.pages) {
-        float* const to = p.weights + ((int64_t)page * p.kv_heads + head) * p.c.page_size + (key - i * p.c.page_size);
-        *to = key >= p0 ? sum : p.decay * *to + sum;
-      }
-    }
+    if (there) *to = is_new ? sum : p.decay * before + sum;
   }
 }
 
 template <int KIND, int NG>
 hipError_t launch(const WeighParams& p, bool split, hipStream_t stream) {
   const int64_t most = (int64_t)p.c.batch * p.kv_heads * p.tiles;
-  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(most, 1), split ? 1024 : 2048)), block(64 * kWaves);
+  // as many workgroups as the GPU holds: a wave of each on every SIMD
+  const int holds = 256 * (split ? Weigh<KIND, NG, true>::kWavesPerSimd : Weigh<KIND, NG, false>::kWavesPerSimd);
+  const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(most, 1), holds)), block(64 * kWaves);
   if (split) weigh_kernel<KIND, NG, true><<<grid, block, 0, stream>>>(p);
   else weigh_kernel<KIND, NG, false><<<grid, block, 0, stream>>>(p);
   return hipGetLastError();
