@@ -46,15 +46,12 @@ struct PackedAttendParams {
   ScaleView s;
   int groups;
 };
-// Rows of a unit are 16 << blocks_log, times the waves of a workgroup where these take rows of their own.
 constexpr int kPackedKeys = 32;      // of a key tile
-constexpr int kPackedFewWaves = 8;   // of a workgroup whose waves share an item's keys
-constexpr int kPackedManyWaves = 4;  // of one whose waves take rows of their own
-hipError_t launch_packed_few_bf16(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
-hipError_t launch_packed_few_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
+constexpr int kPackedManyWaves = 4;  // of a workgroup whose waves take 16 rows each
+// Few rows: a unit is 16 rows, whose keys the workgroup's waves share.
+hipError_t launch_packed_few_bf16(const PackedAttendParams& p, int waves, int whole_pages, hipStream_t stream);
+hipError_t launch_packed_few_f32(const PackedAttendParams& p, int waves, int whole_pages, hipStream_t stream);
 hipError_t launch_packed_many_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
-// log2 of the row blocks (of 16 rows) that a wave of the kernel for many rows takes.
-inline int packed_many_blocks_log(int elem_bytes, int dim) { return dim > 128 || elem_bytes == 4 ? 0 : 1; }
 // Many rows of bf16 sharing key tiles in LDS: rows of a unit, of which heads of up to kWideDoubleDim also take twice as many; keys of a tile.
 inline int log_packed_wide_rows(int dim) { return dim <= 128 ? 8 : 7; }
 constexpr int packed_wide_keys(int dim) { return dim <= 64 ? 128 : 64; }

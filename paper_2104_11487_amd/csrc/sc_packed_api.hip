@@ -28,7 +28,7 @@ void fill_packing(ScaleView* v, const skipconv_cache* c, const skipconv_packing*
 // The kernel and the cut of a launch, from the shapes alone (the lengths are on the device).
 struct PackedPlan {
   bool few, wide;
-  int log_rows, keys, target, min_chunk, slack, units, slots;
+  int waves, log_rows, keys, target, min_chunk, slack, units, slots;
   size_t part_o, part_ml;
 };
 
@@ -42,7 +42,7 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
   p->few = most * group <= 32;
   p->wide = !p->few && c->dtype == SKIPCONV_BF16;
   const bool twice = p->wide && c->head_dim <= kWideDoubleDim && most * group > 256 && (rows >> 9) * c->kv_heads >= 128;
-  p->log_rows = p->few ? 4 : p->wide ? log_packed_wide_rows(c->head_dim) + twice : 6 + packed_many_blocks_log(elem_of(c), c->head_dim);
+  p->log_rows = p->few ? 4 : p->wide ? log_packed_wide_rows(c->head_dim) + twice : 6;
   p->keys = p->wide ? packed_wide_keys(c->head_dim) : kPackedKeys;
   int64_t units = items(p->log_rows);
   // Workgroups that share keys: `want`, or as many as all items' keys are least shares.
@@ -51,8 +51,10 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
     return (int)std::min<int64_t>(want, units * ((tiles + p->min_chunk - 1) / p->min_chunk));
   };
   if (p->few) {
-    p->min_chunk = 2 * kPackedFewWaves;
-    p->target = reach <= 4 * kPackedKeys * kPackedFewWaves ? 0 : shares(256);
+    const bool alone = reach <= (c->head_dim <= 128 ? 1024 : 512);
+    p->waves = c->head_dim <= 128 && alone && units <= 256 ? 8 : 4;
+    p->min_chunk = 8;
+    p->target = alone ? 0 : shares(c->head_dim <= 128 ? 512 : 256);
     p->slack = 0;
   } else {
     const int want = p->wide ? 256 : 512;  // workgroups that the GPU holds
@@ -139,7 +141,7 @@ int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, c
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int whole = whole_pages(p.a.c, p.s);
   const bool half = c->dtype == SKIPCONV_BF16;
-  hipError_t e = plan.few    ? (half ? launch_packed_few_bf16(p, whole, st) : launch_packed_few_f32(p, whole, st))
+  hipError_t e = plan.few    ? (half ? launch_packed_few_bf16(p, plan.waves, whole, st) : launch_packed_few_f32(p, plan.waves, whole, st))
                  : plan.wide ? launch_packed_wide_bf16(p, st) : launch_packed_many_f32(p, whole, st);
   if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), st);
   return hip_result(e, "attend launch");

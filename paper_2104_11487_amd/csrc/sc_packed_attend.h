@@ -2,7 +2,8 @@
 //
 //   o = sum_l exp(s_l - m) v_l / sum_l exp(s_l - m),   s_l = scale q . k_l,   over the keys l that the row sees
 //
-// Codes go from memory into registers in the layout of the matrix unit's operands and become fp16 there: nothing passes through LDS.
+// Codes come into LDS by copies, each wave's own tiles into a ring of its own, two tiles ahead and without a barrier, and from there into registers
+// in the layout of the matrix unit's operands, where they become fp16.
 //   Scores, transposed: S' = K Q' on 16 x 16 x 32 products, K the left operand. Lane (c, g) = (lane & 15, lane >> 4) holds of key c the g-th
 //   quarter of the row's bytes; which elements a step's k indexes stand for is free as long as the queries follow, so those are loaded in the
 //   order in which a mask leaves the codes (0 4 1 5 2 6 3 7 of each eight).
@@ -17,6 +18,7 @@
 
 #include <type_traits>
 
+#include "sc_attend_tile.h"
 #include "sc_packed_device.h"
 
 #pragma clang fp contract(off)
@@ -26,21 +28,33 @@ namespace sc {
 constexpr float kPackedSlack = 8.0f;  // powers of two that an exponential may exceed the reference's by
 constexpr float kPackedLift = 7.0f;   // powers of two that exponentials are formed too large by: 2^15 at most
 
-// Where a tile's keys lie, looked up ahead: with whole pages of 16-key blocks a block's page and first slot, alike in all lanes; otherwise the
-// lane's key's (lane & 31).
-template <bool WHOLE>
-struct PackedPlace {
-  int entry[WHOLE ? 2 : 1], slot[WHOLE ? 2 : 1];
+// Copies 4 bytes a lane from `base` + off into LDS at `to` + 4 lane, as copy16 does 16.
+__device__ __forceinline__ void copy4(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dword %1, %2" ::"s"(uniform((int)to)), "v"(off), "s"(base) : "memory", "m0");
+}
+
+// A tile in LDS: 32 rows of keys and 32 of values, codes and then pairs. The 16-byte pieces of a row are permuted by an exclusive or, so that
+// the lanes of a read, which go through 16 rows at one place or through four rows 4 apart, touch every bank.
+template <int NG>
+struct PackedRing {
+  static constexpr int kRow = 16 * NG, kPairs = 64 * kRow, kStage = kPairs + 256 * NG;
+  static constexpr int kOps = 2 * NG;   // copies of a tile
+  static constexpr int kStages = 3;
+  __device__ __forceinline__ static int swizzle(int row) { return NG == 8 ? (row >> 1) & 7 : NG == 4 ? (row >> 2) & 3 : NG == 2 ? (row >> 3) & 1 : 0; }
 };
 
-// NG: groups of a head, rounded up to a power of two. NB: 16-row blocks of a wave. PARTS: fp16 parts of a query and an exponential.
-// MANY: the waves take rows of their own and all keys; otherwise they take the same rows and every NW-th key tile.
-template <int NG, int NB, int PARTS, bool MANY, bool WHOLE>
-__global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWaves), MANY ? 2 : 1) attend_packed_kernel(PackedAttendParams pp) {
-  constexpr int NW = MANY ? kPackedManyWaves : kPackedFewWaves, WROWS = 16 * NB, ROWS = MANY ? NW * WROWS : WROWS;
+// NG: groups of a head, rounded up to a power of two. PARTS: fp16 parts of a query and an exponential. NW: waves of a workgroup.
+// MANY: the waves take 16 rows each and all keys; otherwise they take the same 16 rows and every NW-th key tile. Rings take 127 KB of LDS at
+// most: a compute unit holds eight waves, for heads above 128 four.
+template <int NG, int PARTS, int NW, bool MANY, bool WHOLE>
+__global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel(PackedAttendParams pp) {
+  constexpr int WROWS = 16, ROWS = MANY ? NW * WROWS : WROWS;
   constexpr int KEYS = kPackedKeys, DP = 32 * NG, NJ = 2 * NG, PIECES = NG == 8 ? 2 : 1;
   constexpr int JP = DP + 4;  // joining: a row's stride in LDS, in floats
-  __shared__ alignas(16) float lds[MANY ? 4 : NW * ROWS * (JP + 2)];
+  using Ring = PackedRing<NG>;
+  constexpr int kWaveBytes = Ring::kStages * Ring::kStage + (WHOLE ? 0 : 512);  // with two buffers of page numbers
+  constexpr int kJoin = MANY ? 0 : NW * ROWS * (JP + 2) * 4;
+  __shared__ alignas(16) char lds[NW * kWaveBytes > kJoin ? NW * kWaveBytes : kJoin];
   const AttendParams& p = pp.a;
 
   const Units batch(p);
@@ -49,93 +63,46 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
   const int64_t first_unit = shares.at(blockIdx.x), end = shares.at(blockIdx.x + 1);
   Unit u;
   if (first_unit >= end || !unit_of(batch, first_unit, &u)) return;
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  const int col = lane & 15, quad = lane >> 4, last_group = pp.groups - 1;
-
-  // Byte offsets in a row: the lane's pieces of a key, of a value; of their pairs. Groups past the head's are led to the last one (the queries
-  // are zero there, and the outputs are not stored). With whole pages the lane's row of a block is in them.
-  uint32_t k_at[PIECES], kp_at[PIECES], v_at[WHOLE ? 4 : 1], vp_at[WHOLE ? 4 : 1];
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int g = NG >= 4 ? min(quad * (NG / 4) + i, last_group) : NG * quad / 4;
-    k_at[i] = (NG >= 4 ? 16 * g : 4 * NG * quad) + (WHOLE ? (uint32_t)(col * (int)p.c.k_slot) : 0u);
-    kp_at[i] = 4 * g + (WHOLE ? (uint32_t)(col * (int)pp.s.k_slot) : 0u);
-  }
-  const int v_group = min(NG * col / 16, last_group);
-  const uint32_t v_byte = NG >= 4 ? 16 * v_group + (NG * col) % 16 : (NG * col) & ~3;
-#pragma unroll
-  for (int r = 0; r < (WHOLE ? 4 : 1); ++r) {
-    v_at[r] = v_byte + (WHOLE ? (uint32_t)((4 * quad + r) * (int)p.c.v_slot) : 0u);
-    vp_at[r] = 4 * v_group + (WHOLE ? (uint32_t)((4 * quad + r) * (int)pp.s.v_slot) : 0u);
-  }
-  const CodeBits bits = code_bits();
-  // page and slot strides of the keys' codes and pairs, the values' codes and pairs
-  const uint32_t k_page = alone(p.c.k_page), k_slot = alone(p.c.k_slot), ks_page = alone(pp.s.k_page), ks_slot = alone(pp.s.k_slot);
-  const uint32_t v_page = alone(p.c.v_page), v_slot = alone(p.c.v_slot), vs_page = alone(pp.s.v_page), vs_slot = alone(pp.s.v_slot);
-  const uint32_t v_sel = NG >= 4 ? 0x0c040c00u : 0x0c040c00u + ((NG * col) & 3) * 0x00010001u;  // picks a byte of two words into 16-bit halves
-
   for (int64_t at = first_unit;;) {
     const int units = (int)min(end - at, (int64_t)(u.parts - u.part));  // of this item
     const bool whole = units == u.parts, begins = at == first_unit;
     at += units;
     u.hi = (int)min((int64_t)u.hi, u.lo + (int64_t)units * u.chunk);
+    // derived anew for each item, so that no register holds from one item to the next what only its ends need
+    int thread = (int)threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int lane = thread & 63, wave = uniform(thread >> 6);
+    const int col = lane & 15, quad = lane >> 4, last_group = pp.groups - 1;
+
+    // LDS offsets in a stage: the lane's pieces of a key of the first block, of a value of its first row; of their pairs
+    uint32_t k_at[PIECES], v_at[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      k_at[i] = col * Ring::kRow + (NG >= 4 ? ((quad * (NG / 4) + i) ^ Ring::swizzle(col)) << 4 : NG == 2 ? (((quad >> 1) ^ Ring::swizzle(col)) << 4) + (quad & 1) * 8 : quad * 4);
+      const int row = 4 * quad + 2 * i;  // the permutation changes from rows 0, 1 to 2, 3 of the lane's four where a row has eight pieces
+      v_at[i] = (32 + 4 * quad) * Ring::kRow + (((NG * col >> 4) ^ Ring::swizzle(row)) << 4) + (NG >= 4 ? (NG * col) & 15 : (NG * col & 15) & ~3);
+    }
+    const uint32_t kp_at = Ring::kPairs + col * (4 * NG) + (NG >= 4 ? quad * NG : NG * quad / 4 * 4);
+    const uint32_t vp_at = Ring::kPairs + (32 + 4 * quad) * (4 * NG) + 4 * (NG * col >> 4);
+    // of the copies: the lane's row of a copy of 64 pieces (pairs), and its piece
+    const int copy_row = lane / NG, copy_piece = lane % NG;
+    const CodeBits bits = code_bits();
+    // page and slot strides of the keys' codes and pairs, the values' codes and pairs
+    const uint32_t k_page = alone(p.c.k_page), k_slot = alone(p.c.k_slot), ks_page = alone(pp.s.k_page), ks_slot = alone(pp.s.k_slot);
+    const uint32_t v_page = alone(p.c.v_page), v_slot = alone(p.c.v_slot), vs_page = alone(pp.s.v_page), vs_slot = alone(pp.s.v_slot);
+    const uint32_t v_sel = NG >= 4 ? 0x0c040c00u : 0x0c040c00u + ((NG * col) & 3) * 0x00010001u;  // picks a byte of two words into 16-bit halves
     const int rows = u.n * p.group, row0 = u.row0 + (MANY ? wave * WROWS : 0);
 
-    // the rows' queries, in the operand's layout
-    half8 qf[NB][PARTS][NG];
-    Seen seen[NB];
-    float factor[NB];  // of a score, to powers of two
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      const int r = min(row0 + 16 * n + col, rows - 1), t = r / p.group, h = u.head * p.group + (r - t * p.group);
-      const int64_t q_at = (int64_t)(u.start + t) * p.q_token + (int64_t)h * p.q_head;
-      float x[NG][8];
-      float most = 0.0f;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int d = 8 * (NG * quad + i);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
-        if (d < p.dim) {
-          if constexpr (PARTS == 1) Elem<uint16_t>::load8(reinterpret_cast<const uint16_t*>(p.q), q_at + d, x[i]);
-          else Elem<float>::load8(reinterpret_cast<const float*>(p.q), q_at + d, x[i]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][e]));
-      }
-      most = max_across32(max_across16(most));
-      const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);  // the largest element comes into [2^14, 2^15)
-      factor[n] = ldexpf(p.scale_log2, -lift);
-#pragma unroll
-      for (int i = 0; i < NG; ++i)
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float a = ldexpf(x[i][e], lift), b = ldexpf(x[i][e + 4], lift);
-            w[e] = pack2h(a, b);
-            if (part == 1) {
-              const half2 hi = half2_of(w[e]);
-              w[e] = pack2h(a - (float)hi[0], b - (float)hi[1]);
-            }
-          }
-          qf[n][part][i] = __builtin_bit_cast(half8, uint4{w[0], w[1], w[2], w[3]});
-        }
-      seen[n] = seen_by(p, u, row0 + 16 * n + col);
-    }
     // keys that every row of the wave sees, that some row sees
     const Seen first = seen_by(p, u, row0), last = seen_by(p, u, row0 + WROWS - 1);
     const int all_lo = last.lo, all_hi = first.hi, any_lo = first.lo, any_hi = last.hi;
 
-    floatx4 o[NB][NJ];
-    float ref[NB], sum[NB], raised[NB];
+    floatx4 o[NJ];
+    float ref = kNegInf, sum = 0.0f, raised = kNegInf;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      ref[n] = raised[n] = kNegInf, sum[n] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) o[n][j] = floatx4{};
-    }
+    for (int j = 0; j < NJ; ++j) o[j] = floatx4{};
+
+    const int inside_lo = uniform(all_lo), inside_hi = uniform(all_hi) - KEYS + 1;  // first keys of tiles that all rows see whole
 
     // the wave's tiles
     constexpr int kStep = MANY ? KEYS : KEYS * NW;
@@ -151,161 +118,263 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
     const char* const ksb = pp.s.k + (int64_t)u.head * pp.s.k_head;
     const char* const vsb = pp.s.v + (int64_t)u.head * pp.s.v_head;
 
-    // A tile in the lane's registers: codes and pairs of keys and of values.
-    uint32_t kc[2][NG], kp[2][PIECES], vc[8][PIECES], vp[8];
-    PackedPlace<WHOLE> place;
-    const char* v_rows[2];  // whole pages: a block's first value, its pairs
-    const char* v_pairs[2];
-    int page_l = 0, slot_l = 0;  // otherwise: the lane's key's
+    char* const ring = lds + wave * kWaveBytes;
+    const uint32_t ring_at = (uint32_t)(uintptr_t)SC_LDS(lds, char) + wave * kWaveBytes, entries_at = ring_at + Ring::kStages * Ring::kStage;
+    // Where a tile's keys lie, looked up ahead: with whole pages of 16-key blocks a block's page and first slot, by the scalar unit; otherwise
+    // its 32 keys' page numbers, by copies into LDS.
+    int entry[2], slot[2];
+    auto find = [&](int it) {
+      const int key0 = begin + it * kStep;
+      if constexpr (WHOLE) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int i = min(page_of(p.c, key0 + 16 * j), p.c.width - 1);
+          slot[j] = min(key0 + 16 * j - i * p.c.page_size, p.c.page_size - 16);
+          entry[j] = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(p.c.table + (int64_t)u.b * p.c.width))[i];
+        }
+      } else {
+        sc::copy4(p.c.table + (int64_t)u.b * p.c.width + min(page_of(p.c, key0 + (lane & 31)), p.c.width - 1), entries_at + (it & 1) * 256);
+      }
+    };
+    auto copy = [&](int it, int stage) {  // the tile that was looked up
+      const uint32_t to = ring_at + stage;
+      if constexpr (WHOLE) {
+        const char* base[4];  // keys of both blocks, values; their pairs
+        const char* pairs[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint64_t page = (uint32_t)page_of_entry(p.c, entry[j]), at = (uint32_t)slot[j];
+          base[j] = kb + (page * k_page + at * k_slot), pairs[j] = ksb + (page * ks_page + at * ks_slot);
+          base[2 + j] = vb + (page * v_page + at * v_slot), pairs[2 + j] = vsb + (page * vs_page + at * vs_slot);
+        }
+        if constexpr (NG >= 4) {  // a copy's rows are of one block
+          constexpr int kRows = 64 / NG;
+#pragma unroll
+          for (int t = 0; t < NG; ++t) {
+            const int from = t * kRows, row = from % 16 + copy_row;
+            const bool val = from >= 32;
+            const int g = min(copy_piece ^ Ring::swizzle(row), last_group);
+            copy16(base[from / 16], here((uint32_t)row * (val ? v_slot : k_slot) + 16 * g), to + t * 1024);
+            copy4(pairs[from / 16], here((uint32_t)row * (val ? vs_slot : ks_slot) + 4 * min(copy_piece, last_group)), to + Ring::kPairs + t * 256);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < NG; ++t) {
+            const int row = t * (64 / NG) + copy_row, which = row / 16;
+            const char* b = NG == 2 ? (t ? base[2] : base[0]) : base[0];
+            const char* s = NG == 2 ? (t ? pairs[2] : pairs[0]) : pairs[0];
+            if constexpr (NG == 2) {
+              b = which & 1 ? (t ? base[3] : base[1]) : b, s = which & 1 ? (t ? pairs[3] : pairs[1]) : s;
+            } else {
+              b = which == 1 ? base[1] : which == 2 ? base[2] : which == 3 ? base[3] : b;
+              s = which == 1 ? pairs[1] : which == 2 ? pairs[2] : which == 3 ? pairs[3] : s;
+            }
+            const bool val = which >= 2;
+            copy16(b + (uint32_t)(row % 16) * (val ? v_slot : k_slot) + 16 * (copy_piece ^ Ring::swizzle(row)), to + t * 1024);
+            sc::copy4(s + (uint32_t)(row % 16) * (val ? vs_slot : ks_slot) + 4 * copy_piece, to + Ring::kPairs + t * 256);
+          }
+        }
+      } else {
+        const char* from[NG];
+        const char* pairs[NG];
+#pragma unroll
+        for (int t = 0; t < NG; ++t) {
+          const int row = t * (64 / NG) + copy_row, key = begin + it * kStep + (row & 31);
+          const bool val = row >= 32;
+          const int64_t page = page_of_entry(p.c, *reinterpret_cast<const int*>(ring + Ring::kStages * Ring::kStage + (it & 1) * 256 + (row & 31) * 4));
+          const int64_t at = min(key - min(page_of(p.c, key), p.c.width - 1) * p.c.page_size, p.c.page_size - 1);
+          from[t] = (val ? vb + page * p.c.v_page + at * p.c.v_slot : kb + page * p.c.k_page + at * p.c.k_slot) + 16 * min(copy_piece ^ Ring::swizzle(row), last_group);
+          pairs[t] = (val ? vsb + page * pp.s.v_page + at * pp.s.v_slot : ksb + page * pp.s.k_page + at * pp.s.k_slot) + 4 * min(copy_piece, last_group);
+        }
+#pragma unroll
+        for (int t = 0; t < NG; ++t) {
+          copy16(from[t], to + t * 1024);
+          sc::copy4(pairs[t], to + Ring::kPairs + t * 256);
+        }
+      }
+    };
+    int stage = 0;  // of the tile in the products
+    const auto after = [&](int at, int n) { return at + n * Ring::kStage >= Ring::kStages * Ring::kStage ? at + (n - Ring::kStages) * Ring::kStage : at + n * Ring::kStage; };
+    // This tile's copies have landed (the next one's may be outstanding, and the page numbers two further on); those of the one after leave, into
+    // the place of the tile before, whose reads have reached their products.
+    auto advance = [&](int it) {
+      wait_loads<Ring::kOps + (WHOLE ? 0 : 1)>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      copy(it + 2, after(stage, 2));
+      if constexpr (!WHOLE) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the page numbers are read before others take their place
+      find(WHOLE ? it + 3 : it + 4);
+    };
+    if (count > 0) {
+      if constexpr (WHOLE) {
+        find(0);
+        copy(0, 0);
+        find(1);
+        copy(1, Ring::kStage);
+        find(2);
+      } else {
+        find(0);
+        find(1);
+        wait_loads<0>();
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+          copy(it, it * Ring::kStage);
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          find(it + 2);
+        }
+      }
+    }
 
-    auto find = [&](int key0) {
-      if constexpr (WHOLE) {
+    // the rows' queries, in the operand's layout: loaded while the first tiles' copies are in flight
+    half8 qf[PARTS][NG];
+    const int r = min(row0 + col, rows - 1), t = r / p.group, h = u.head * p.group + (r - t * p.group);
+    const int64_t q_at = (int64_t)(u.start + t) * p.q_token + (int64_t)h * p.q_head;
+    float x[NG][8];
+    float most = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) place.entry[j] = entry_at(p.c, u.b, key0 + 16 * j, 16, &place.slot[j]);
-      } else {
-        place.entry[0] = entry_at(p.c, u.b, key0 + (lane & 31), 1, &place.slot[0]);
+    for (int i = 0; i < NG; ++i) {
+      const int d = 8 * (NG * quad + i);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
+      if (d < p.dim) {
+        if constexpr (PARTS == 1) Elem<uint16_t>::load8(reinterpret_cast<const uint16_t*>(p.q), q_at + d, x[i]);
+        else Elem<float>::load8(reinterpret_cast<const float*>(p.q), q_at + d, x[i]);
       }
-    };
-    auto load_key = [&](const char* row, const char* pairs, uint32_t* codes, uint32_t* pair) {
-      if constexpr (NG == 1) {
-        codes[0] = *reinterpret_cast<const uint32_t*>(row + here(k_at[0]));
-      } else if constexpr (NG == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + here(k_at[0]));
-        codes[0] = w[0], codes[1] = w[1];
-      } else {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-          const uint4 w = *reinterpret_cast<const uint4*>(row + here(k_at[i]));
-          codes[4 * i] = w.x, codes[4 * i + 1] = w.y, codes[4 * i + 2] = w.z, codes[4 * i + 3] = w.w;
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][e]));
+    }
+    most = max_across32(max_across16(most));
+    const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);  // the largest element comes into [2^14, 2^15)
+    const float factor = ldexpf(p.scale_log2, -lift);  // of a score, to powers of two
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float a = ldexpf(x[i][e], lift), b = ldexpf(x[i][e + 4], lift);
+          w[e] = pack2h(a, b);
+          if (part == 1) {
+            const half2 hi = half2_of(w[e]);
+            w[e] = pack2h(a - (float)hi[0], b - (float)hi[1]);
+          }
         }
+        qf[part][i] = __builtin_bit_cast(half8, uint4{w[0], w[1], w[2], w[3]});
       }
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) pair[i] = *reinterpret_cast<const uint32_t*>(pairs + here(kp_at[i]));
-    };
-    auto load_value = [&](const char* row, const char* pairs, int r, uint32_t* codes, uint32_t* pair) {
-      if constexpr (PIECES == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(row + here(v_at[r]));
-        codes[0] = w[0], codes[1] = w[1];
-      } else {
-        codes[0] = *reinterpret_cast<const uint32_t*>(row + here(v_at[r]));
-      }
-      *pair = *reinterpret_cast<const uint32_t*>(pairs + here(vp_at[r]));
-    };
-    auto fetch_keys = [&]() {  // of the tile at `place`, which then is free
-      if constexpr (WHOLE) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint64_t page = (uint32_t)page_of_entry(p.c, uniform(place.entry[j])), slot = (uint32_t)uniform(place.slot[j]);
-          load_key(kb + (page * k_page + slot * k_slot), ksb + (page * ks_page + slot * ks_slot), kc[j], kp[j]);
-          v_rows[j] = vb + (page * v_page + slot * v_slot);
-          v_pairs[j] = vsb + (page * vs_page + slot * vs_slot);
-        }
-      } else {
-        page_l = page_of_entry(p.c, place.entry[0]), slot_l = place.slot[0];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int64_t page = __shfl(page_l, 16 * j + col), slot = __shfl(slot_l, 16 * j + col);
-          load_key(kb + page * p.c.k_page + slot * p.c.k_slot, ksb + page * pp.s.k_page + slot * pp.s.k_slot, kc[j], kp[j]);
-        }
-      }
-    };
-    auto fetch_values = [&]() {  // of the tile whose keys were fetched last
+    const Seen seen = seen_by(p, u, row0 + col);
+
+    // One tile's work. What is seldom needed ends it early, so that in the loop over tiles products alone touch the outputs' registers, which keep
+    // their places:
+    //   kRaise  a score passes the reference by more than the slack: nothing is done but to say by how much;
+    //   kOdd    some row does not see a value that is not finite: all is done but to add those values.
+    constexpr int kDone = 0, kRaise = 1, kOdd = 2;
+    half8 pf[PARTS];  // exponentials
+    auto load_values = [&](const char* tile_at, uint32_t (&vc)[8][PIECES], uint32_t (&vp)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if constexpr (WHOLE) {
-          load_value(v_rows[e / 4], v_pairs[e / 4], e % 4, vc[e], &vp[e]);
+        const char* const at = tile_at + v_at[PIECES == 2 ? (e % 4) / 2 : 0] + ((e / 4) * 16 + e % 4) * Ring::kRow;
+        if constexpr (PIECES == 2) {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(at);
+          vc[e][0] = w[0], vc[e][1] = w[1];
         } else {
-          const int64_t page = __shfl(page_l, 16 * (e / 4) + 4 * quad + e % 4), slot = __shfl(slot_l, 16 * (e / 4) + 4 * quad + e % 4);
-          load_value(vb + page * p.c.v_page + slot * p.c.v_slot, vsb + page * pp.s.v_page + slot * pp.s.v_slot, 0, vc[e], &vp[e]);
+          vc[e][0] = *reinterpret_cast<const uint32_t*>(at);
         }
+        vp[e] = *reinterpret_cast<const uint32_t*>(tile_at + vp_at + ((e / 4) * 16 + e % 4) * (4 * NG));
       }
     };
-
-    // One tile's work, and the loads of the next one, whose keys take the place of this one's as soon as these are in the product, and values
-    // likewise. edge: some row does not see some of its keys. Where a score passes the reference by more than the slack nothing is done but to
-    // raise it, and the tile is to be gone through again: so the outputs' registers are touched by products alone in the loop, and keep their places.
-    auto tile = [&](auto edge_, int it) {
-      constexpr bool edge = edge_;
+    // Whether a key's group holds values that are not finite: between minimum and largest value all are, or they show it.
+    auto infinite = [&](uint32_t pair) {
+      const half2 x = half2_of(pair);
+      const uint32_t ends = bits_of(half2{x[1], (_Float16)__builtin_fmaf((float)x[0], 15.0f, (float)x[1])});
+      return (ends & 0x7c00u) == 0x7c00u || (ends & 0x7c000000u) == 0x7c000000u;
+    };
+    auto tile = [&](int it) {
       const int key0 = begin + it * kStep;
-      floatx4 s[NB][2];
+      const bool edge = key0 < inside_lo || key0 > inside_hi;  // some row does not see some of the keys
+      const char* const tile_at = ring + stage;
+      floatx4 s[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
+        uint32_t kc[NG], kp[PIECES];
+        if constexpr (NG == 1) {
+          kc[0] = *reinterpret_cast<const uint32_t*>(tile_at + k_at[0] + j * 16 * Ring::kRow);
+        } else if constexpr (NG == 2) {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(tile_at + k_at[0] + j * 16 * Ring::kRow);
+          kc[0] = w[0], kc[1] = w[1];
+        } else {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) s[n][j] = floatx4{};
+          for (int i = 0; i < PIECES; ++i) {
+            const uint4 w = *reinterpret_cast<const uint4*>(tile_at + k_at[i] + j * 16 * Ring::kRow);
+            kc[4 * i] = w.x, kc[4 * i + 1] = w.y, kc[4 * i + 2] = w.z, kc[4 * i + 3] = w.w;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) kp[i] = *reinterpret_cast<const uint32_t*>(tile_at + kp_at + j * 64 * NG + 4 * i);
+        s[j] = floatx4{};
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const half8 kf = values8(kc[j][i], kp[j][NG == 8 ? i / 4 : 0], bits);
+          const half8 kf = values8(kc[i], kp[NG == 8 ? i / 4 : 0], bits);
 #pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int part = 0; part < PARTS; ++part) s[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][part][i], s[n][j], 0, 0, 0);
+          for (int part = 0; part < PARTS; ++part) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[part][i], s[j], 0, 0, 0);
         }
       }
-      bool past = false;
-      float top[NB];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        if constexpr (edge) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int key = key0 + 16 * j + 4 * quad + r;
-              s[n][j][r] = key >= seen[n].lo && key <= seen[n].hi ? s[n][j][r] : kNegInf;
-            }
-        }
-        top[n] = s[n][0][0];
+      if (edge) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top[n] = fmaxf(top[n], s[n][j][r]);
-        top[n] = max_across32(max_across16(top[n])) * factor[n];
-        past = past || top[n] > ref[n] + kPackedSlack;
-      }
-      if (__any(past)) {
-#pragma unroll
-        for (int n = 0; n < NB; ++n) raised[n] = fmaxf(ref[n], top[n]);
-        return false;
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      fetch_keys();
-      find(key0 + 2 * kStep);
-      __builtin_amdgcn_sched_barrier(0);
-      half8 pf[NB][PARTS];
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const float base = ref[n] == kNegInf ? 0.0f : ref[n] - kPackedLift;
-        uint32_t w[PARTS][4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; r += 2) {
-            const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][j][r], factor[n], -base));
-            const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][j][r + 1], factor[n], -base));
-            sum[n] += a;
-            sum[n] += b;
-            const uint32_t hi = pack2h(a, b);
-            w[0][2 * j + r / 2] = hi;
-            if constexpr (PARTS == 2) w[PARTS - 1][2 * j + r / 2] = pack2h(a - (float)half2_of(hi)[0], b - (float)half2_of(hi)[1]);
+          for (int r = 0; r < 4; ++r) {
+            const int key = key0 + 16 * j + 4 * quad + r;
+            s[j][r] = key >= seen.lo && key <= seen.hi ? s[j][r] : kNegInf;
           }
-#pragma unroll
-        for (int part = 0; part < PARTS; ++part) pf[n][part] = __builtin_bit_cast(half8, uint4{w[part][0], w[part][1], w[part][2], w[part][3]});
       }
-      // Values. Where some row does not see some key, a masked key's exponential is zero, but zero times an infinity or a
-      // NaN is not: values of keys that no row sees are cleared, and those that are not finite leave the product and
-      // are added to the rows that see their key.
-      __builtin_amdgcn_sched_barrier(0);
-      int odd = 0;
-      half2 scale[4], low[4];
-      uint32_t mask[4];
+      float top = s[0][0];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {  // pairs of keys
-        scale[e] = scales2(vp[2 * e], vp[2 * e + 1]), low[e] = lows2(vp[2 * e], vp[2 * e + 1]);
-        if constexpr (edge) {
-          const int key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
-          mask[e] = (key >= any_lo && key <= any_hi ? 0xffffu : 0u) | (key + 1 >= any_lo && key + 1 <= any_hi ? 0xffff0000u : 0u);
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[j][r]);
+      top = max_across32(max_across16(top)) * factor;
+      if (__any(top > ref + kPackedSlack)) {
+        if (it > 0) {
+          raised = fmaxf(ref, top);
+          return kRaise;
+        }
+        ref = fmaxf(ref, top);  // nothing to rescale yet
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      const float base = ref == kNegInf ? 0.0f : ref - kPackedLift;
+      uint32_t w[PARTS][4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; r += 2) {
+          const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r], factor, -base));
+          const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][r + 1], factor, -base));
+          sum += a;
+          sum += b;
+          const uint32_t hi = pack2h(a, b);
+          w[0][2 * j + r / 2] = hi;
+          if constexpr (PARTS == 2) w[PARTS - 1][2 * j + r / 2] = pack2h(a - (float)half2_of(hi)[0], b - (float)half2_of(hi)[1]);
+        }
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) pf[part] = __builtin_bit_cast(half8, uint4{w[part][0], w[part][1], w[part][2], w[part][3]});
+      // Where some row does not see some key, that key's exponential is zero, but zero times an infinity or a NaN is not: pairs of keys that
+      // no row sees become zero, and so do those whose smallest or largest value is not finite, which are added by themselves.
+      bool odd = false;
+      uint32_t vc[8][PIECES], pairs[8];
+      load_values(tile_at, vc, pairs);
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = key0 + 16 * (e / 4) + 4 * quad + e % 4;
+          const bool seen_by_some = key >= any_lo && key <= any_hi, bad = infinite(pairs[e]);
+          pairs[e] = seen_by_some && !bad ? pairs[e] : 0u;
+          odd = odd || (seen_by_some && bad);
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      half2 scale[4], low[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) scale[e] = scales2(pairs[2 * e], pairs[2 * e + 1]), low[e] = lows2(pairs[2 * e], pairs[2 * e + 1]);  // pairs of keys
 #pragma unroll
       for (int b = 0; b < NG; ++b) {
         uint32_t even[4], odds[4];
@@ -314,89 +383,83 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
           const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
           even[e] = values2(codes_low(w, bits), scale[e], low[e]);
           odds[e] = values2(codes_high(w, bits), scale[e], low[e]);
-          if constexpr (edge) even[e] = finite2h(even[e], mask[e], &odd), odds[e] = finite2h(odds[e], mask[e], &odd);
         }
         const half8 v0 = __builtin_bit_cast(half8, uint4{even[0], even[1], even[2], even[3]});
         const half8 v1 = __builtin_bit_cast(half8, uint4{odds[0], odds[1], odds[2], odds[3]});
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
-            o[n][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[n][part], o[n][2 * b], 0, 0, 0);
-            o[n][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[n][part], o[n][2 * b + 1], 0, 0, 0);
-          }
+        for (int part = 0; part < PARTS; ++part) {
+          o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[part], o[2 * b], 0, 0, 0);
+          o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[part], o[2 * b + 1], 0, 0, 0);
+        }
       }
-      if (edge && __any(odd)) {
-        // A key at a time: its values alone in the left operand, ones in the other, give every row its values; those that are not finite
-        // are added where the row sees the key.
-        const uint32_t one2 = bits_of(half2{1.0f16, 1.0f16});
-        const half8 ones = __builtin_bit_cast(half8, uint4{one2, one2, one2, one2});
-        const int from = max(key0, any_lo), to = min(key0 + KEYS - 1, any_hi);
+      return edge && __any(odd) ? kOdd : kDone;
+    };
+    // A key at a time: the product of its bad groups' values alone, added for the rows that see the key.
+    auto add_odd = [&](int it) {
+      const int key0 = begin + it * kStep;
+      uint32_t vc[8][PIECES], vp[8];
+      load_values(ring + stage, vc, vp);
+      const int from = max(key0, any_lo), to = min(key0 + KEYS - 1, any_hi);
 #pragma unroll 1
-        for (int key = from; key <= to; ++key) {
+      for (int key = from; key <= to; ++key) {
 #pragma unroll
-          for (int b = 0; b < NG; ++b) {
-            uint32_t x[2][4];
+        for (int b = 0; b < NG; ++b) {
+          uint32_t x[2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int first_key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
-              const uint32_t only = first_key == key ? 0xffffu : first_key + 1 == key ? 0xffff0000u : 0u;
-              const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
-              x[0][e] = values2(codes_low(w, bits), scale[e], low[e]) & only;
-              x[1][e] = values2(codes_high(w, bits), scale[e], low[e]) & only;
-            }
+          for (int e = 0; e < 4; ++e) {
+            const int first_key = key0 + 16 * (e / 2) + 4 * quad + 2 * (e & 1);
+            const uint32_t only = (first_key == key && infinite(vp[2 * e]) ? 0xffffu : 0u) | (first_key + 1 == key && infinite(vp[2 * e + 1]) ? 0xffff0000u : 0u);
+            const uint32_t w = __builtin_amdgcn_perm(vc[2 * e + 1][b / 4], vc[2 * e][b / 4], v_sel + (b % 4) * 0x00010001u);
+            const half2 scale = scales2(vp[2 * e], vp[2 * e + 1]), low = lows2(vp[2 * e], vp[2 * e + 1]);
+            x[0][e] = values2(codes_low(w, bits), scale, low) & only;
+            x[1][e] = values2(codes_high(w, bits), scale, low) & only;
+          }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const floatx4 got = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{x[k][0], x[k][1], x[k][2], x[k][3]}), ones, floatx4{}, 0, 0, 0);
+          for (int k = 0; k < 2; ++k) {
 #pragma unroll
-              for (int n = 0; n < NB; ++n)
+            for (int part = 0; part < PARTS; ++part) {
+              const floatx4 got = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{x[k][0], x[k][1], x[k][2], x[k][3]}), pf[part], floatx4{}, 0, 0, 0);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                  if ((__float_as_uint(got[r]) & 0x7f800000u) == 0x7f800000u && key >= seen[n].lo && key <= seen[n].hi) o[n][2 * b + k][r] += got[r];
+              for (int r = 0; r < 4; ++r)
+                if (key >= seen.lo && key <= seen.hi) o[2 * b + k][r] += got[r];
             }
           }
         }
       }
-      __builtin_amdgcn_sched_barrier(0);
-      fetch_values();
-      return true;
     };
     auto raise = [&]() {
+      const float keep = raised == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref - raised);
+      ref = raised;
+      sum *= keep;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const float keep = raised[n] == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(ref[n] - raised[n]);
-        ref[n] = raised[n];
-        sum[n] *= keep;
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[n][j][r] *= keep;
-      }
+        for (int r = 0; r < 4; ++r) o[j][r] *= keep;
     };
 
-    if (count > 0) {
-      find(begin);
-      fetch_keys();
-      fetch_values();
-      find(begin + kStep);
-    }
-    // Tiles that all rows see whole have a loop of their own. The last tile's loads are of tiles past it, which no product takes.
-    const int inside_lo = uniform(all_lo), inside_hi = uniform(all_hi) - KEYS + 1;
+    bool again = false;  // the tile was gone through as far as its scores
     for (int it = 0; it < count;) {
+      int end = kDone;
 #pragma unroll 1
-      for (; it < count && begin + it * kStep >= inside_lo && begin + it * kStep <= inside_hi && tile(std::false_type{}, it); ++it) {}
-      if (it >= count) break;
-      if (begin + it * kStep >= inside_lo && begin + it * kStep <= inside_hi) raise();
-      else if (tile(std::true_type{}, it)) ++it;
-      else raise();
+      for (; it < count; ++it, stage = after(stage, 1)) {
+        if (!again) advance(it);
+        again = false;
+        end = tile(it);
+        if (end != kDone) break;
+      }
+      if (end == kRaise) {
+        raise();
+        again = true;
+      } else if (end == kOdd) {
+        add_odd(it);
+        ++it, stage = after(stage, 1);
+      }
     }
+    wait_loads<0>();  // copies of tiles past the last one too: their place is used otherwise
 
     // A row's statistics: the reference that its exponentials and their sum are relative to.
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      sum[n] = sum_across32(sum_across16(sum[n]));
-      ref[n] = ref[n] == kNegInf ? kNegInf : ref[n] - kPackedLift;
-    }
+    sum = sum_across32(sum_across16(sum));
+    ref = ref == kNegInf ? kNegInf : ref - kPackedLift;
     auto store_out = [&](int row, int e, const float* v, int n, float inv) {  // n elements of a row, from e on
       const int t = row / p.group, h = u.head * p.group + (row - t * p.group);
       const int64_t to = (int64_t)(u.start + t) * p.o_token + (int64_t)h * p.o_head + e;
@@ -410,18 +473,16 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
       p.lse[(int64_t)(u.start + t) * p.q_heads + h] = total == 0.0f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.69314718055994531f;
     };
     if constexpr (MANY) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int row = row0 + 16 * n + col;
-        if (row >= rows) continue;
+      const int row = row0 + col;
+      if (row < rows) {
         const int64_t part = (2 * (int64_t)blockIdx.x + (begins ? 0 : 1)) * ROWS + (row - u.row0);
-        const float inv = sum[n] == 0.0f ? 0.0f : 1.0f / sum[n];
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int e = NJ * (4 * quad + r);
           float v[NJ];
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) v[j] = o[n][j][r];
+          for (int j = 0; j < NJ; ++j) v[j] = o[j][r];
           constexpr int kRun = NJ < 8 ? NJ : 8;  // heads are multiples of 8
 #pragma unroll
           for (int i = 0; i < NJ; i += kRun) {
@@ -435,26 +496,23 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
           }
         }
         if (quad == 0) {
-          if (!whole) *reinterpret_cast<floatx2*>(p.part_ml + part * 2) = floatx2{ref[n], sum[n]};
-          else if (p.lse) store_lse(row, ref[n], sum[n]);
+          if (!whole) *reinterpret_cast<floatx2*>(p.part_ml + part * 2) = floatx2{ref, sum};
+          else if (p.lse) store_lse(row, ref, sum);
         }
       }
     } else {
       __syncthreads();
-      float* const joined = lds;                    // [wave][row][JP]
+      float* const joined = reinterpret_cast<float*>(lds);                    // [wave][row][JP]
       float* const stats = joined + NW * ROWS * JP;  // [wave][row][2]
+      const int r = wave * ROWS + col;
 #pragma unroll
-      for (int n = 0; n < NB; ++n) {
-        const int r = wave * ROWS + 16 * n + col;
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int j = 0; j < NJ; j += 2) *reinterpret_cast<floatx2*>(joined + r * JP + NJ * (4 * quad + k) + j) = floatx2{o[n][j][k], o[n][j + 1][k]};
-        if (quad == 0) stats[r * 2] = ref[n], stats[r * 2 + 1] = sum[n];
-      }
+        for (int j = 0; j < NJ; j += 2) *reinterpret_cast<floatx2*>(joined + r * JP + NJ * (4 * quad + k) + j) = floatx2{o[j][k], o[j + 1][k]};
+      if (quad == 0) stats[r * 2] = ref, stats[r * 2 + 1] = sum;
       __syncthreads();
       constexpr int kQuads = DP / 4;
-      for (int i = threadIdx.x; i < ROWS * kQuads; i += 64 * NW) {
+      for (int i = thread; i < ROWS * kQuads; i += 64 * NW) {
         const int r = i / kQuads, e = (i % kQuads) * 4, row = u.row0 + r;
         if (row >= rows || e >= p.dim) continue;
         float top = kNegInf;
@@ -486,22 +544,22 @@ __global__ void __launch_bounds__(64 * (MANY ? kPackedManyWaves : kPackedFewWave
   }
 }
 
-template <int NG, int NB, int PARTS, bool MANY>
+template <int NG, int PARTS, int NW, bool MANY>
 hipError_t launch_packed(const PackedAttendParams& p, int whole_pages, hipStream_t stream) {
-  const dim3 grid((unsigned)p.a.units), block(64 * (MANY ? kPackedManyWaves : kPackedFewWaves));
-  if (p.a.keys != kPackedKeys || (1 << p.a.log_rows) != 16 * NB * (MANY ? kPackedManyWaves : 1)) return hipErrorInvalidValue;
-  if (whole_pages) attend_packed_kernel<NG, NB, PARTS, MANY, true><<<grid, block, 0, stream>>>(p);
-  else attend_packed_kernel<NG, NB, PARTS, MANY, false><<<grid, block, 0, stream>>>(p);
+  const dim3 grid((unsigned)p.a.units), block(64 * NW);
+  if (p.a.keys != kPackedKeys || (1 << p.a.log_rows) != 16 * (MANY ? NW : 1)) return hipErrorInvalidValue;
+  if (whole_pages) attend_packed_kernel<NG, PARTS, NW, MANY, true><<<grid, block, 0, stream>>>(p);
+  else attend_packed_kernel<NG, PARTS, NW, MANY, false><<<grid, block, 0, stream>>>(p);
   return hipGetLastError();
 }
 
-// NARROW, WIDE: row blocks for heads of up to 128, above.
-template <int NARROW, int WIDE, int PARTS, bool MANY>
+// NW: waves of a workgroup for heads of up to 128.
+template <int PARTS, int NW, bool MANY>
 hipError_t launch_packed_dim(const PackedAttendParams& p, int whole_pages, hipStream_t stream) {
-  if (p.a.dim <= 32) return launch_packed<1, NARROW, PARTS, MANY>(p, whole_pages, stream);
-  if (p.a.dim <= 64) return launch_packed<2, NARROW, PARTS, MANY>(p, whole_pages, stream);
-  if (p.a.dim <= 128) return launch_packed<4, NARROW, PARTS, MANY>(p, whole_pages, stream);
-  return launch_packed<8, WIDE, PARTS, MANY>(p, whole_pages, stream);
+  if (p.a.dim <= 32) return launch_packed<1, PARTS, NW, MANY>(p, whole_pages, stream);
+  if (p.a.dim <= 64) return launch_packed<2, PARTS, NW, MANY>(p, whole_pages, stream);
+  if (p.a.dim <= 128) return launch_packed<4, PARTS, NW, MANY>(p, whole_pages, stream);
+  return launch_packed<8, PARTS, 4, MANY>(p, whole_pages, stream);
 }
 
 }  // namespace sc

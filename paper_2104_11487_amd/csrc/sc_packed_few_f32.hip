@@ -3,6 +3,8 @@
 
 namespace sc {
 
-hipError_t launch_packed_few_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream) { return launch_packed_dim<1, 1, 2, false>(p, whole_pages, stream); }
+hipError_t launch_packed_few_f32(const PackedAttendParams& p, int waves, int whole_pages, hipStream_t stream) {
+  return waves == 8 ? launch_packed_dim<2, 8, false>(p, whole_pages, stream) : launch_packed_dim<2, 4, false>(p, whole_pages, stream);
+}
 
 }  // namespace sc

@@ -3,6 +3,6 @@
 
 namespace sc {
 
-hipError_t launch_packed_many_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream) { return launch_packed_dim<1, 1, 2, true>(p, whole_pages, stream); }
+hipError_t launch_packed_many_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream) { return launch_packed_dim<2, kPackedManyWaves, true>(p, whole_pages, stream); }
 
 }  // namespace sc
