@@ -29,7 +29,8 @@ struct Weigh {
   static constexpr int kParts = KIND == 2 && SPLIT ? 2 : 1;
   static constexpr int kWords = kHalf ? 4 : 8;          // registers of eight elements
   static constexpr int kRegs = NG * kParts * kWords;    // of an operand of 16 keys
-  static constexpr int kRaw = kPacked ? 2 * NG : NG * kWords;  // of 16 keys as they lie in memory: codes and pairs, or elements
+  static constexpr int kPieces = NG == 8 ? 2 : 1;       // 16-byte pieces of codes, and pairs, of a lane
+  static constexpr int kRaw = kPacked ? NG + kPieces : NG * kWords;  // of 16 keys as they lie in memory: codes and pairs, or elements
   // 16-key blocks of a wave: where rows are many it holds their operands; otherwise they are formed for each block of rows, from
   // what was loaded, all blocks' loads in flight together
   static constexpr int kBlocks = SPLIT ? (kRegs <= 16 ? 4 : kRegs <= 32 ? 2 : 1) : kRaw <= 16 ? 4 : kRaw <= 32 ? 2 : 1;
@@ -86,7 +87,10 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
   int64_t base = 0, sequence_end = 0;
   Sequence s = {0, 0, 0};
 
-  // a block of rows, in the right operand's layout: lane (row of the block, quarter) holds elements 32 i + 8 quad ..
+  // Step i of a product takes of lane (row or key, quarter) eight elements from here on: where keys are codes a quarter's lie in a row, so
+  // that one load brings a key's codes of all steps; otherwise the quarters' lie side by side, 64 or 128 bytes a load and key.
+  const auto element = [&](int i) { return W::kPacked ? 8 * (NG * quad + i) : 32 * i + 8 * quad; };
+  // a block of rows, in the right operand's layout
   uint32_t qf[NG][kWords];
   float less = 0.0f, factor = 0.0f;  // of the lane's row: lse in powers of two (infinite: it gives nothing); of a score, to powers of two
   int seen_lo = 0, seen_hi = -1;
@@ -135,7 +139,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       const Q* const q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + t) * p.q_token + (int64_t)h * p.q_head;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        const int d = 32 * i + 8 * quad;
+        const int d = element(i);
 #pragma unroll
         for (int part = 0; part < kWords / 4; ++part) {
           const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(q + d)[part] : uint4{0u, 0u, 0u, 0u};
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     const int own_page = min(page_of(p.c, min(own_key, kMostKeys - 1)), p.c.width - 1);
     if (stores) own_entry = p.c.table[(int64_t)b * p.c.width + own_page];
 
-    // the keys, in the left operand's layout: lane (key of the block, quarter) holds elements 32 i + 8 quad ..
+    // the keys, in the left operand's layout
     uint32_t raw_keys[BLOCKS][W::kRaw];
     if (first_row < row_count) {
       int entry[BLOCKS], slot[BLOCKS];
@@ -200,14 +204,24 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
         if constexpr (W::kPacked) {
           const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot[j] * p.s.k_slot;
 #pragma unroll
-          for (int i = 0; i < NG; ++i) {
-            const int g = min(i, p.groups - 1);  // groups past the head's: the queries are zero there
-            raw_keys[j][2 * i] = reinterpret_cast<const uint32_t*>(row)[4 * g + quad], raw_keys[j][2 * i + 1] = reinterpret_cast<const uint32_t*>(pairs)[g];
+          for (int i = 0; i < W::kPieces; ++i) {
+            const int g = min(NG >= 4 ? W::kPieces * quad + i : NG * quad / 4, p.groups - 1);  // groups past the head's: the queries are zero there
+            if constexpr (NG >= 4) {
+              const uint4 w = *reinterpret_cast<const uint4*>(row + 16 * g);
+              uint32_t* const to = &raw_keys[j][4 * i];
+              to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+            } else if constexpr (NG == 2) {
+              const u32x2 w = *reinterpret_cast<const u32x2*>(row + 16 * g + 8 * (quad & 1));
+              raw_keys[j][0] = w[0], raw_keys[j][1] = w[1];
+            } else {
+              raw_keys[j][0] = *reinterpret_cast<const uint32_t*>(row + 4 * quad);
+            }
+            raw_keys[j][NG + i] = reinterpret_cast<const uint32_t*>(pairs)[g];
           }
         } else {
 #pragma unroll
           for (int i = 0; i < NG; ++i) {
-            const int d = 32 * i + 8 * quad;
+            const int d = element(i);
 #pragma unroll
             for (int e = 0; e < kWords; e += 4) {
               const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[e / 4] : uint4{0u, 0u, 0u, 0u};
@@ -226,7 +240,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 #pragma unroll
           for (int e = 0; e < kWords; ++e) kf[0][i][e] = raw_keys[j][i * kWords + e];
         } else {
-          const half8 v = values8(raw_keys[j][2 * i], raw_keys[j][2 * i + 1], bits);
+          const half8 v = values8(raw_keys[j][i], raw_keys[j][NG + i / 4], bits);
           if constexpr (W::kScaled) {
             const uint4 w = __builtin_bit_cast(uint4, v);
             kf[0][i][0] = w.x, kf[0][i][1] = w.y, kf[0][i][2] = w.z, kf[0][i][3] = w.w;
