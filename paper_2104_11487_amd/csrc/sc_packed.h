@@ -66,7 +66,7 @@ struct WeighParams {
   float* weights;     // pages x kv_heads x page_size
   int64_t q_token, q_head;
   int q_heads, kv_heads, group, dim, groups;
-  int causal, window, packed;
+  int causal, window, packed, whole;  // whole: 16-key blocks lie in one page each
   float scale_log2, decay;
   int64_t tiles;      // units of a sequence and key head, at most
 };

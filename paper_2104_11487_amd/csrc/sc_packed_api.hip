@@ -185,6 +185,7 @@ int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, con
   p.q = static_cast<const char*>(w->q), p.lse = w->lse, p.weights = w->weights;
   p.q_heads = w->q_heads, p.kv_heads = c->kv_heads, p.group = w->q_heads / c->kv_heads, p.dim = c->head_dim, p.groups = pack_groups(c->head_dim);
   p.causal = w->causal, p.window = w->window < 0 ? -1 : w->window, p.packed = s != nullptr;
+  p.whole = c->page_size % 16 == 0 && 16 * std::max(p.c.k_slot, p.s.k_slot) < (1ll << 30) && std::max(p.c.k_page, p.s.k_page) < (1ll << 32);
   p.scale_log2 = (float)((double)w->scale * 1.4426950408889634), p.decay = w->decay;
   p.tiles = ((int64_t)c->table_width * c->page_size + 31) / 32;
   const int64_t most = w->max_new > 0 ? std::min<int64_t>(w->max_new, c->tokens) : c->tokens;

@@ -52,13 +52,37 @@ __device__ __forceinline__ int64_t scan64(int64_t v) {
   return v;
 }
 
-// Sum over each row of 16 lanes, in all of them: rotations within the row.
-__device__ __forceinline__ float sum16(float v) {
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128, 0xf, 0xf, false));
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x124, 0xf, 0xf, false));
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x122, 0xf, 0xf, false));
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x121, 0xf, 0xf, false));
-  return v;
+// Sums of N values (16, 8 or 4) over each row of 16 lanes; lane c of a row has value c % N's. Lanes exchange halves of what they hold, with
+// partners that differ by 8, 7, 2 and 1 (exclusive or): 15 exchanges for 16 values, where sums by themselves take 64.
+template <int CONTROL>
+__device__ __forceinline__ float from_partner(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CONTROL, 0xf, 0xf, true));
+}
+template <int N, int CONTROL>
+__device__ __forceinline__ void exchange(float (&v)[16], bool upper) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float keep = upper ? v[i + N] : v[i], give = upper ? v[i] : v[i + N];
+    v[i] = keep + from_partner<CONTROL>(give);
+  }
+}
+template <int N>
+__device__ __forceinline__ float sums16(float (&v)[16], int col) {
+  if constexpr (N == 16) {
+    exchange<8, 0x128>(v, col & 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += from_partner<0x128>(v[i]);
+  }
+  if constexpr (N >= 8) {
+    exchange<4, 0x141>(v, col & 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += from_partner<0x141>(v[i]);
+  }
+  exchange<2, 0x4e>(v, col & 2);
+  exchange<1, 0xb1>(v, col & 1);
+  return v[0];
 }
 
 template <int KIND, int NG, bool SPLIT>
@@ -193,42 +217,62 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 
     // the keys, in the left operand's layout
     uint32_t raw_keys[BLOCKS][W::kRaw];
+    // Block j's, where the lane's key begins at `row`, its pairs at `pairs`.
+    const auto bring = [&](int j, const char* row, const char* pairs) {
+      if constexpr (W::kPacked) {
+#pragma unroll
+        for (int i = 0; i < W::kPieces; ++i) {
+          const int g = min(NG >= 4 ? W::kPieces * quad + i : NG * quad / 4, p.groups - 1);  // groups past the head's: the queries are zero there
+          if constexpr (NG >= 4) {
+            const uint4 w = *reinterpret_cast<const uint4*>(row + 16 * g);
+            uint32_t* const to = &raw_keys[j][4 * i];
+            to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+          } else if constexpr (NG == 2) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(row + 16 * g + 8 * (quad & 1));
+            raw_keys[j][0] = w[0], raw_keys[j][1] = w[1];
+          } else {
+            raw_keys[j][0] = *reinterpret_cast<const uint32_t*>(row + 4 * quad);
+          }
+          raw_keys[j][NG + i] = *reinterpret_cast<const uint32_t*>(pairs + 4 * g);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int d = element(i);
+#pragma unroll
+          for (int e = 0; e < kWords; e += 4) {
+            const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + d * (int)sizeof(Q))[e / 4] : uint4{0u, 0u, 0u, 0u};
+            uint32_t* const to = &raw_keys[j][i * kWords + e];
+            to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+          }
+        }
+      }
+    };
     if (first_row < row_count) {
-      int entry[BLOCKS], slot[BLOCKS];
+      const char* const k = p.c.k + (int64_t)head * p.c.k_head;
+      const char* const ks = p.s.k + (int64_t)head * p.s.k_head;
+      if (p.whole) {  // a block lies in one page, which the scalar unit looks up
+        int entry[BLOCKS], slot[BLOCKS];
 #pragma unroll
-      for (int j = 0; j < BLOCKS; ++j) entry[j] = entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot[j]);
+        for (int j = 0; j < BLOCKS; ++j) {
+          const int at = min(uniform(key0) + 16 * j, kMostKeys - 16), i = min(page_of(p.c, at), p.c.width - 1);
+          slot[j] = min(at - i * p.c.page_size, p.c.page_size - 16);
+          entry[j] = ((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(p.c.table + (int64_t)b * p.c.width))[i];
+        }
+        const uint32_t off = (uint32_t)col * (uint32_t)p.c.k_slot, pairs_off = (uint32_t)col * (uint32_t)p.s.k_slot;
 #pragma unroll
-      for (int j = 0; j < BLOCKS; ++j) {
-        const int64_t page = page_of_entry(p.c, entry[j]);
-        const char* const row = p.c.k + page * p.c.k_page + (int64_t)head * p.c.k_head + slot[j] * p.c.k_slot;
-        if constexpr (W::kPacked) {
-          const char* const pairs = p.s.k + page * p.s.k_page + (int64_t)head * p.s.k_head + slot[j] * p.s.k_slot;
+        for (int j = 0; j < BLOCKS; ++j) {
+          const uint64_t page = (uint32_t)page_of_entry(p.c, entry[j]), at = (uint32_t)slot[j];
+          bring(j, k + (page * (uint32_t)p.c.k_page + at * (uint32_t)p.c.k_slot) + off, ks + (page * (uint32_t)p.s.k_page + at * (uint32_t)p.s.k_slot) + pairs_off);
+        }
+      } else {
+        int entry[BLOCKS], slot[BLOCKS];
 #pragma unroll
-          for (int i = 0; i < W::kPieces; ++i) {
-            const int g = min(NG >= 4 ? W::kPieces * quad + i : NG * quad / 4, p.groups - 1);  // groups past the head's: the queries are zero there
-            if constexpr (NG >= 4) {
-              const uint4 w = *reinterpret_cast<const uint4*>(row + 16 * g);
-              uint32_t* const to = &raw_keys[j][4 * i];
-              to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
-            } else if constexpr (NG == 2) {
-              const u32x2 w = *reinterpret_cast<const u32x2*>(row + 16 * g + 8 * (quad & 1));
-              raw_keys[j][0] = w[0], raw_keys[j][1] = w[1];
-            } else {
-              raw_keys[j][0] = *reinterpret_cast<const uint32_t*>(row + 4 * quad);
-            }
-            raw_keys[j][NG + i] = reinterpret_cast<const uint32_t*>(pairs)[g];
-          }
-        } else {
+        for (int j = 0; j < BLOCKS; ++j) entry[j] = entry_at(p.c, b, min(key0 + 16 * j + col, kMostKeys - 1), 1, &slot[j]);
 #pragma unroll
-          for (int i = 0; i < NG; ++i) {
-            const int d = element(i);
-#pragma unroll
-            for (int e = 0; e < kWords; e += 4) {
-              const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(row + (int64_t)d * (int)sizeof(Q))[e / 4] : uint4{0u, 0u, 0u, 0u};
-              uint32_t* const to = &raw_keys[j][i * kWords + e];
-              to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
-            }
-          }
+        for (int j = 0; j < BLOCKS; ++j) {
+          const int64_t page = page_of_entry(p.c, entry[j]);
+          bring(j, k + page * p.c.k_page + slot[j] * p.c.k_slot, ks + page * p.s.k_page + slot[j] * p.s.k_slot);
         }
       }
     }
@@ -271,8 +315,10 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     floatx4 got[BLOCKS];
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) got[j] = floatx4{};
-    // The held rows' scores with the held keys, and what they give. inside: every row sees every key.
-    const auto add = [&](bool inside) {
+    // The held rows' scores with the held keys, and what they give. kAll: 16 rows, which see every key; kRows: so do those that there are.
+    constexpr int kAll = 0, kRows = 1, kSome = 2;
+    const auto add = [&](int which) {
+      const bool gives = less != -kNegInf;
 #pragma unroll
       for (int j = 0; j < BLOCKS; ++j) {
         floatx4 score = floatx4{};
@@ -297,33 +343,40 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
               for (int e = 0; e < 8; ++e) score = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[i][e % kWords]), score, 0, 0, 0);
             }
           }
-        if (inside) {
+        if (which == kAll) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) got[j][r] += __builtin_amdgcn_exp2f(__builtin_fmaf(score[r], factor, -less));
+        } else if (which == kRows) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[r], factor, -less));
+            got[j][r] += gives ? e : 0.0f;
+          }
         } else {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int key = key0 + 16 * j + 4 * quad + r;
             const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[r], factor, -less));
-            got[j][r] += less != -kNegInf && key >= seen_lo && key <= seen_hi ? e : 0.0f;
+            got[j][r] += gives && key >= seen_lo && key <= seen_hi ? e : 0.0f;
           }
         }
       }
     };
-    const auto inside_of = [&](int r0) {  // whether all 16 rows from r0 on are rows and see all keys (uniform)
-      return whole_keys && r0 + 16 <= rows_all && r0 / p.group >= all0 && (r0 + 15) / p.group <= all1;
+    const auto which_of = [&](int r0) {  // of the 16 rows from r0 on (uniform)
+      const int to = min(r0 + 16, rows_all);
+      return !whole_keys || r0 / p.group < all0 || (to - 1) / p.group > all1 ? kSome : to < r0 + 16 ? kRows : kAll;
     };
 
 #pragma unroll 1
     for (int r0 = first_row; r0 < row_count; r0 += SPLIT ? 16 * kWaves : 16) {
       if (!rows_held) take_rows(r0);
       if (r0 + (SPLIT ? 16 * kWaves : 16) < row_count) fetch_rows(r0 + (SPLIT ? 16 * kWaves : 16));
-      const bool inside = inside_of(r0);
+      const int which = which_of(r0);
       if constexpr (SPLIT) {
-        if (inside) add(true);
-        else add(false);
+        if (which == kAll) add(kAll);
+        else add(kSome);
       } else {
-        add(inside);
+        add(which);
       }
     }
     rows_held = rows_held || (!SPLIT && row_count > 0 && row_count <= 16);
@@ -334,14 +387,10 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     const float before = there && !is_new ? *to : 0.0f;
 
     // over the 16 rows of a block; lane r of a quarter then has its key r's of the first block, lane 4 + r of the second, ..
-    float sum = 0.0f;
+    float each[16];
 #pragma unroll
-    for (int j = 0; j < BLOCKS; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float v = sum16(got[j][r]);
-        sum = col == 4 * j + r ? v : sum;
-      }
+    for (int i = 0; i < 4 * BLOCKS; ++i) each[i] = got[i / 4][i % 4];
+    float sum = sums16<4 * BLOCKS>(each, col);
     if constexpr (SPLIT) {
       if (col < 4 * BLOCKS) shares[wave][local] = sum;
       __syncthreads();
