@@ -111,6 +111,11 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
   int64_t base = 0, sequence_end = 0;
   Sequence s = {0, 0, 0};
 
+  constexpr int kStep = SPLIT ? 16 * kWaves : 16;  // rows from a block of the wave to its next one
+  const struct {
+    int token, of_group;
+    int64_t q, wrap;
+  } row_step = {kStep / p.group, kStep % p.group, kStep / p.group * p.q_token + kStep % p.group * p.q_head, p.q_token - p.group * p.q_head};
   // Step i of a product takes of lane (row or key, quarter) eight elements from here on: where keys are codes a quarter's lie in a row, so
   // that one load brings a key's codes of all steps; otherwise the quarters' lie side by side, 64 or 128 bytes a load and key.
   const auto element = [&](int i) { return W::kPacked ? 8 * (NG * quad + i) : 32 * i + 8 * quad; };
@@ -158,23 +163,32 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 
     uint32_t raw[NG][kWords];
     float raw_lse = 0.0f;
-    const auto fetch_rows = [&](int r0) {
-      const int row = min(r0 + col, rows_all - 1), t = row / p.group, h = head * p.group + (row - t * p.group);
-      const Q* const q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + t) * p.q_token + (int64_t)h * p.q_head;
+    int token = 0, of_group = 0;  // of the lane's row
+    const Q* row_q = nullptr;
+    const auto find_row = [&](int r0) {
+      token = (r0 + col) / p.group, of_group = r0 + col - token * p.group;
+      row_q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + token) * p.q_token + (int64_t)(head * p.group + of_group) * p.q_head;
+    };
+    const auto next_row = [&](int r0) {  // of the next block that the wave takes, at r0
+      if constexpr (!SPLIT) return find_row(r0);
+      token += row_step.token, of_group += row_step.of_group, row_q += row_step.q;
+      if (of_group >= p.group) of_group -= p.group, ++token, row_q += row_step.wrap;
+    };
+    const auto fetch_rows = [&]() {
+      const bool there = token < s.n;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int d = element(i);
 #pragma unroll
         for (int part = 0; part < kWords / 4; ++part) {
-          const uint4 w = d < p.dim ? reinterpret_cast<const uint4*>(q + d)[part] : uint4{0u, 0u, 0u, 0u};
+          const uint4 w = there && d < p.dim ? reinterpret_cast<const uint4*>(row_q + d)[part] : uint4{0u, 0u, 0u, 0u};
           raw[i][4 * part] = w.x, raw[i][4 * part + 1] = w.y, raw[i][4 * part + 2] = w.z, raw[i][4 * part + 3] = w.w;
         }
       }
-      raw_lse = p.lse[(int64_t)(s.start + t) * p.q_heads + h];
+      raw_lse = there ? p.lse[(int64_t)(s.start + token) * p.q_heads + head * p.group + of_group] : kNegInf;
     };
     const auto take_rows = [&](int r0) {  // what was fetched
-      less = raw_lse == kNegInf ? -kNegInf : raw_lse * kLog2e;
-      if (r0 + col >= rows_all) less = -kNegInf;
+      less = raw_lse == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse * kLog2e;
       factor = p.scale_log2;
       if constexpr (W::kScaled) {  // the largest element comes into [2^14, 2^15)
         float most = 0.0f;
@@ -199,14 +213,14 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 #pragma unroll
           for (int e = 0; e < kWords; ++e) qf[i][e] = raw[i][e];
       }
-      const int at = p0 + min(r0 + col, rows_all - 1) / p.group, from = p.causal ? at : p0;  // the row's position
+      const int at = p0 + min(token, s.n - 1), from = p.causal ? at : p0;  // the row's position
       seen_hi = p.causal ? min(at, s.len - 1) : s.len - 1;
       seen_lo = p.window >= 0 && from > p.window ? from - p.window : 0;
     };
 
     const int first_row = row_begin + (SPLIT ? 16 * wave : 0);
     const int row_count = rows_end > 0 ? rows_all : 0;
-    if (first_row < row_count && !rows_held) fetch_rows(first_row);
+    if (first_row < row_count && !rows_held) find_row(first_row), fetch_rows();
 
     // what the lane will store: its key's place, and what that held
     const int local = 16 * (col >> 2) + 4 * quad + (col & 3), own_key = key0 + local;
@@ -362,15 +376,16 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
         }
       }
     };
+    const int all_from = all0 * p.group, all_to = whole_keys ? (max(all1, -1) + 1) * p.group : 0;  // rows that see all of the wave's keys
     const auto which_of = [&](int r0) {  // of the 16 rows from r0 on (uniform)
       const int to = min(r0 + 16, rows_all);
-      return !whole_keys || r0 / p.group < all0 || (to - 1) / p.group > all1 ? kSome : to < r0 + 16 ? kRows : kAll;
+      return r0 < all_from || to > all_to ? kSome : to < r0 + 16 ? kRows : kAll;
     };
 
 #pragma unroll 1
-    for (int r0 = first_row; r0 < row_count; r0 += SPLIT ? 16 * kWaves : 16) {
+    for (int r0 = first_row; r0 < row_count; r0 += kStep) {
       if (!rows_held) take_rows(r0);
-      if (r0 + (SPLIT ? 16 * kWaves : 16) < row_count) fetch_rows(r0 + (SPLIT ? 16 * kWaves : 16));
+      if (r0 + kStep < row_count) next_row(r0 + kStep), fetch_rows();
       const int which = which_of(r0);
       if constexpr (SPLIT) {
         if (which == kAll) add(kAll);
