@@ -35,7 +35,8 @@ struct Weigh {
   // what was loaded, all blocks' loads in flight together
   static constexpr int kBlocks = SPLIT ? (kRegs <= 16 ? 4 : kRegs <= 32 ? 2 : 1) : kRaw <= 16 ? 4 : kRaw <= 32 ? 2 : 1;
   static constexpr int kKeys = 16 * kBlocks * (SPLIT ? 1 : kWaves);  // of a unit
-  static constexpr int kOperands = (SPLIT ? kBlocks * kRegs : kBlocks * kRaw + kRegs) + 2 * NG * kWords;
+  static constexpr int kDepth = !SPLIT ? 1 : NG * kWords <= 16 ? 3 : 2;  // blocks of rows in registers
+  static constexpr int kOperands = SPLIT ? kBlocks * kRegs + kDepth * NG * kWords : kBlocks * kRaw + kRegs + 2 * NG * kWords;
   static constexpr int kWavesPerSimd = kOperands <= 48 ? (SPLIT ? 3 : 4) : kOperands <= 80 ? 3 : 2;
   using Q = std::conditional_t<kHalf, uint16_t, float>;
 };
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
   using W = Weigh<KIND, NG, SPLIT>;
   using Q = typename W::Q;
   constexpr bool kHalf = W::kHalf;
-  constexpr int PARTS = W::kParts, KEYS = W::kKeys, BLOCKS = W::kBlocks, kWords = W::kWords;
+  constexpr int PARTS = W::kParts, KEYS = W::kKeys, BLOCKS = W::kBlocks, kWords = W::kWords, DEPTH = W::kDepth;
   __shared__ float shares[SPLIT ? kWaves : 1][16 * BLOCKS];
   const CodeBits bits = code_bits();
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
@@ -161,9 +162,12 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     // (few rows: all of them, so that the operand holds for every unit)
     const int rows_all = SPLIT ? rows_end : s.n * p.group;
 
-    uint32_t raw[NG][kWords];
-    float raw_lse = 0.0f;
-    int token = 0, of_group = 0;  // of the lane's row
+    // Blocks of rows that were fetched. Where rows are many, as many as the registers hold: products take them where they are, and the next
+    // ones take their place.
+    uint32_t raw[DEPTH][NG][kWords];
+    float raw_lse[DEPTH];
+    int raw_token[DEPTH];
+    int token = 0, of_group = 0;  // of the lane's row that was fetched last
     const Q* row_q = nullptr;
     const auto find_row = [&](int r0) {
       token = (r0 + col) / p.group, of_group = r0 + col - token * p.group;
@@ -174,7 +178,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       token += row_step.token, of_group += row_step.of_group, row_q += row_step.q;
       if (of_group >= p.group) of_group -= p.group, ++token, row_q += row_step.wrap;
     };
-    const auto fetch_rows = [&]() {
+    const auto fetch_rows = [&](int x) {
       const bool there = token < s.n;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
@@ -182,45 +186,52 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 #pragma unroll
         for (int part = 0; part < kWords / 4; ++part) {
           const uint4 w = there && d < p.dim ? reinterpret_cast<const uint4*>(row_q + d)[part] : uint4{0u, 0u, 0u, 0u};
-          raw[i][4 * part] = w.x, raw[i][4 * part + 1] = w.y, raw[i][4 * part + 2] = w.z, raw[i][4 * part + 3] = w.w;
+          uint32_t* const to = &raw[x][i][4 * part];
+          to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
         }
       }
-      raw_lse = there ? p.lse[(int64_t)(s.start + token) * p.q_heads + head * p.group + of_group] : kNegInf;
+      raw_token[x] = token;
+      raw_lse[x] = there ? p.lse[(int64_t)(s.start + token) * p.q_heads + head * p.group + of_group] : kNegInf;
     };
-    const auto take_rows = [&](int r0) {  // what was fetched
-      less = raw_lse == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse * kLog2e;
+    const auto take_rows = [&](int x, int r0) {  // what was fetched
+      less = raw_lse[x] == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse[x] * kLog2e;
       factor = p.scale_log2;
       if constexpr (W::kScaled) {  // the largest element comes into [2^14, 2^15)
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < NG; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(raw[i][e] << 16)), fabsf(__uint_as_float(raw[i][e] & 0xffff0000u))));
+          for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(raw[x][i][e] << 16)), fabsf(__uint_as_float(raw[x][i][e] & 0xffff0000u))));
         most = max_across32(max_across16(most));
         const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);
         factor = ldexpf(p.scale_log2, -lift);
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          float x[8];
+          float y[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[2 * e] = ldexpf(__uint_as_float(raw[i][e] << 16), lift), x[2 * e + 1] = ldexpf(__uint_as_float(raw[i][e] & 0xffff0000u), lift);
+          for (int e = 0; e < 4; ++e) y[2 * e] = ldexpf(__uint_as_float(raw[x][i][e] << 16), lift), y[2 * e + 1] = ldexpf(__uint_as_float(raw[x][i][e] & 0xffff0000u), lift);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) qf[i][e] = pack2h(x[e], x[e + 4]);  // in the order that the keys' codes come in
+          for (int e = 0; e < 4; ++e) qf[i][e] = pack2h(y[e], y[e + 4]);  // in the order that the keys' codes come in
         }
-      } else {
+      } else if constexpr (!SPLIT) {
 #pragma unroll
         for (int i = 0; i < NG; ++i)
 #pragma unroll
-          for (int e = 0; e < kWords; ++e) qf[i][e] = raw[i][e];
+          for (int e = 0; e < kWords; ++e) qf[i][e] = raw[x][i][e];
       }
-      const int at = p0 + min(token, s.n - 1), from = p.causal ? at : p0;  // the row's position
+      const int at = p0 + min(raw_token[x], s.n - 1), from = p.causal ? at : p0;  // the row's position
       seen_hi = p.causal ? min(at, s.len - 1) : s.len - 1;
       seen_lo = p.window >= 0 && from > p.window ? from - p.window : 0;
     };
 
     const int first_row = row_begin + (SPLIT ? 16 * wave : 0);
     const int row_count = rows_end > 0 ? rows_all : 0;
-    if (first_row < row_count && !rows_held) find_row(first_row), fetch_rows();
+    if (first_row < row_count && !rows_held) {
+      find_row(first_row), fetch_rows(0);
+#pragma unroll
+      for (int x = 1; x < DEPTH; ++x)
+        if (first_row + x * kStep < row_count) next_row(first_row + x * kStep), fetch_rows(x);
+    }
 
     // what the lane will store: its key's place, and what that held
     const int local = 16 * (col >> 2) + 4 * quad + (col & 3), own_key = key0 + local;
@@ -331,7 +342,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     for (int j = 0; j < BLOCKS; ++j) got[j] = floatx4{};
     // The held rows' scores with the held keys, and what they give. kAll: 16 rows, which see every key; kRows: so do those that there are.
     constexpr int kAll = 0, kRows = 1, kSome = 2;
-    const auto add = [&](int which) {
+    const auto add = [&](const uint32_t (&rows)[NG][kWords], int which) {
       const bool gives = less != -kNegInf;
 #pragma unroll
       for (int j = 0; j < BLOCKS; ++j) {
@@ -349,12 +360,12 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
           for (int part = 0; part < PARTS; ++part) {
             const uint32_t* const k = kf[part][i];
             if constexpr (W::kScaled) {
-              score = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(half8, uint4{qf[i][0], qf[i][1], qf[i][2], qf[i][3]}), score, 0, 0, 0);
+              score = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(half8, uint4{rows[i][0], rows[i][1], rows[i][2], rows[i][3]}), score, 0, 0, 0);
             } else if constexpr (kHalf) {
-              score = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(bf16x8, uint4{qf[i][0], qf[i][1], qf[i][2], qf[i][3]}), score, 0, 0, 0);
+              score = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, uint4{k[0], k[1], k[2], k[3]}), __builtin_bit_cast(bf16x8, uint4{rows[i][0], rows[i][1], rows[i][2], rows[i][3]}), score, 0, 0, 0);
             } else {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) score = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(qf[i][e % kWords]), score, 0, 0, 0);
+              for (int e = 0; e < 8; ++e) score = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(rows[i][e % kWords]), score, 0, 0, 0);
             }
           }
         if (which == kAll) {
@@ -382,16 +393,25 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       return r0 < all_from || to > all_to ? kSome : to < r0 + 16 ? kRows : kAll;
     };
 
+    if constexpr (SPLIT) {
+      int r0 = first_row;
+      while (r0 < row_count) {
+#pragma unroll
+        for (int x = 0; x < DEPTH; ++x) {
+          if (r0 >= row_count) break;
+          take_rows(x, r0);
+          if (which_of(r0) == kAll) add(raw[x], kAll);
+          else add(raw[x], kSome);
+          if (r0 + DEPTH * kStep < row_count) next_row(r0 + DEPTH * kStep), fetch_rows(x);
+          r0 += kStep;
+        }
+      }
+    } else {
 #pragma unroll 1
-    for (int r0 = first_row; r0 < row_count; r0 += kStep) {
-      if (!rows_held) take_rows(r0);
-      if (r0 + kStep < row_count) next_row(r0 + kStep), fetch_rows();
-      const int which = which_of(r0);
-      if constexpr (SPLIT) {
-        if (which == kAll) add(kAll);
-        else add(kSome);
-      } else {
-        add(which);
+      for (int r0 = first_row; r0 < row_count; r0 += kStep) {
+        if (!rows_held) take_rows(0, r0);
+        if (r0 + kStep < row_count) next_row(r0 + kStep), fetch_rows(0);
+        add(qf, which_of(r0));
       }
     }
     rows_held = rows_held || (!SPLIT && row_count > 0 && row_count <= 16);
