@@ -554,7 +554,8 @@ int skipconv_packed_unpack(const skipconv_cache* c, const skipconv_packing* s, c
  * as in skipconv_cache_attend, whose lse this takes (rows with lse = -inf
  * give nothing). s: NULL for a float cache. Sums are formed in 32 bits in a fixed
  * order: equal calls give equal bits. Tokens whose page number is outside the cache are
- * left out. max_new: as in skipconv_attend. */
+ * left out. Two tokens of sequences with new ones that share a slot (pages of a common prefix) race. max_new: as in
+ * skipconv_attend. */
 typedef struct skipconv_weigh {
   const void* q;         /* tokens x q_heads x head_dim, 16-byte aligned with strides of whole 16 bytes */
   const float* lse;      /* tokens x q_heads */

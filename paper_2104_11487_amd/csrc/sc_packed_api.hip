@@ -81,7 +81,7 @@ bool whole_pages(const CacheView& c, const ScaleView& s) {
 
 int check_weigh(const skipconv_cache* c, const skipconv_weigh* w) {
   if (w->q_heads < 1 || w->q_heads % c->kv_heads != 0) return invalid("weigh: q_heads must be a multiple of kv_heads");
-  if (c->tokens > kMostRows / w->q_heads) return fail(SKIPCONV_E_UNSUPPORTED, "weigh: too many rows");
+  if (c->tokens > (kMostRows - 1024) / w->q_heads) return fail(SKIPCONV_E_UNSUPPORTED, "weigh: too many rows");  // rows are counted ahead
   if (w->causal != 0 && w->causal != 1) return invalid("weigh: causal must be 0 or 1");
   if (!(w->scale > 0.0f) || !std::isfinite(w->scale)) return invalid("weigh: scale must be positive and finite");
   if (!std::isfinite(w->decay)) return invalid("weigh: decay must be finite");

@@ -386,7 +386,7 @@ class _Cache:
         """Adds the attention weight that each cached token received from the new tokens' queries to `weights` (float32, pages x kv_heads x
         page_size), and returns it: decay times what it held, plus the sum over the query heads and the new tokens that see it of exp(score - lse);
         a new token's own is set, so its slot needs no clearing. q, lse: what attend() took, and returned with return_lse; the mask and the
-        scale as there. Tokens of sequences without new ones stay as they are.
+        scale as there. Tokens of sequences without new ones stay as they are; sequences with new ones must not share slots.
         """
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
@@ -499,6 +499,8 @@ class PackedCache(_Cache):
         index = self._index
         if pages.dtype is not torch.int32 or pages.get_device() != index or not pages.is_contiguous():
             raise ValueError(f"pages must be a contiguous int32 tensor on {self._device}")
+        if self._graph():
+            _refuse_graph()
         k, v = (torch.empty((*pages.shape, self._kv_heads, self._page_size, self._head_dim), dtype=torch.float16, device=pages.device) for _ in range(2))
         _enqueue(_S.lib().skipconv_packed_unpack, index, *self._refs, pages.data_ptr(), pages.numel(), k.data_ptr(), v.data_ptr())
         return k, v

@@ -834,8 +834,13 @@ def test_no_gradient_is_lost():
                  lambda: cache.evict(weights.clone().requires_grad_(True), batch, into, keep=8)):
         with pytest.raises(ValueError, match="gradient"):
             call()
+    learned = A.PackedCache(*cache._tensors[:2], *(x.clone().requires_grad_(True) for x in cache._tensors[2:]), cache.head_dim)
+    for call in (lambda: learned.attend(q, batch), lambda: learned.unpack(into), lambda: learned.weigh(q, lse, batch, weights)):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
     with torch.no_grad():
         cache.attend(grad, batch)
+        learned.unpack(into)
 
 
 def test_what_a_call_writes_is_known_to_autograd():

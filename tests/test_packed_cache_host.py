@@ -244,6 +244,15 @@ def test_weigh_refusals(kw):
         assert "weigh" in S.skipconv_last_error()
 
 
+def test_weigh_refuses_rows_near_2_to_31():
+    """Blocks of rows are counted up to 192 rows ahead: the count stays a 32-bit integer."""
+    lib = S.lib()
+    for s in (R(_packing()), None):
+        for tokens in (((1 << 31) - 1025) // 16 + 1, ((1 << 31) - 1) // 16):
+            assert lib.skipconv_cache_weigh(R(_cache(tokens=tokens, kv_heads=2)), s, R(_weigh(q_heads=16)), None) == UNSUPPORTED
+            assert "weigh" in S.skipconv_last_error()
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(keep=0), INVALID), (dict(keep=-1), INVALID), (dict(recent=-1), INVALID), (dict(recent=61), INVALID), (dict(into_width=0), INVALID), (dict(into_width=3), INVALID),
     (dict(weights=None), INVALID), (dict(into=None), INVALID), (dict(lengths=None), INVALID), (dict(kept=None), INVALID), (dict(weights=A + 2), INVALID), (dict(into=A + 1), INVALID),
