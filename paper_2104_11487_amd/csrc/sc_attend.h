@@ -90,6 +90,6 @@ hipError_t launch_attend_wide_bf16(const AttendParams& p, int uniform_pages, hip
 hipError_t launch_attend_wide_f32(const AttendParams& p, int uniform_pages, hipStream_t stream);
 hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream);
 hipError_t launch_attend_few_f32(const AttendParams& p, hipStream_t stream);
-hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream);
+hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, int few, hipStream_t stream);  // fewer rows than `few`: a workgroup each
 
 }  // namespace sc

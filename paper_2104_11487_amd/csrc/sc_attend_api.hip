@@ -159,7 +159,7 @@ int skipconv_cache_attend(const skipconv_cache* c, const skipconv_attend* a, voi
     const int uniform = c->page_size % rows == 0 && reach < (1ll << 31) && page_bytes < (1ll << 32);
     e = elem == 2 ? sc::launch_attend_wide_bf16(p, uniform, s) : sc::launch_attend_wide_f32(p, uniform, s);
   }
-  if (e == hipSuccess && plan.slots) e = sc::launch_attend_join(p, elem, s);
+  if (e == hipSuccess && plan.slots) e = sc::launch_attend_join(p, elem, 512, s);
   return hip_result(e, "attend launch");
 }
 

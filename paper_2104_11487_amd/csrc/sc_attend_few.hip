@@ -157,13 +157,13 @@ __global__ void __launch_bounds__(64 * kRowWaves) attend_join_kernel(AttendParam
 }
 
 template <typename T>
-void launch_join(const AttendParams& p, hipStream_t stream) {
+void launch_join(const AttendParams& p, int few, hipStream_t stream) {
   const int rows = p.c.tokens * p.q_heads;
   int width = 8;
   while (width * 4 < p.dim) width *= 2;  // lanes of a row: 8..64
   // A workgroup a row while those do not fill the GPU (one token over 262141 keys, 8 rows of 241 parts); then lane groups, of
   // which many rows of few parts need no exchange.
-  if (rows < 512) {
+  if (rows < few) {
     attend_join_kernel<T><<<dim3((unsigned)rows), dim3(64 * kRowWaves), 0, stream>>>(p, width);
   } else {
     const int each = kJoinWaves * (64 / width);
@@ -180,10 +180,10 @@ int few_waves_of(int elem_bytes, int dim) {
 
 hipError_t launch_attend_few_bf16(const AttendParams& p, hipStream_t stream) { return launch_few_dim<uint16_t>(p, stream); }
 
-hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, hipStream_t stream) {
+hipError_t launch_attend_join(const AttendParams& p, int elem_bytes, int few, hipStream_t stream) {
   if (p.target > kMostShared) return hipErrorInvalidValue;
-  if (elem_bytes == 2) launch_join<uint16_t>(p, stream);
-  else launch_join<float>(p, stream);
+  if (elem_bytes == 2) launch_join<uint16_t>(p, few, stream);
+  else launch_join<float>(p, few, stream);
   return hipGetLastError();
 }
 

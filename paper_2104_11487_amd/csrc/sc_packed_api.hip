@@ -39,9 +39,19 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
   const int64_t room = (int64_t)c->table_width * c->page_size;
   const int64_t reach = std::min(room, a->window < 0 ? room : (int64_t)a->window + most);  // keys that an item may have
   const auto items = [&](int log_rows) { return ((rows >> log_rows) + std::min<int64_t>(c->batch, c->tokens)) * c->kv_heads; };
-  p->few = most * group <= 32;
-  p->wide = !p->few && c->dtype == SKIPCONV_BF16;
-  const bool twice = p->wide && c->head_dim <= kWideDoubleDim && most * group > 256 && (rows >> 9) * c->kv_heads >= 128;
+  // Few rows: 16 a workgroup, whose waves share the keys, while a second block of rows costs less than rows that share keys in LDS or with
+  // waves of their own. 16 sequences over 4000, heads of 64: 8 rows of bf16 21 us, by the other kernel 25, 32 rows 30 and 26, but over 300 keys
+  // 10 and 12, and 64 sequences over 4000 40 and 47 (64 rows: 61 and 49); of fp32, 64 rows 34 and 33, over 300 keys 10 and 18, 128 rows 40 and 41,
+  // of 64 sequences 112 and 105. Heads of 256, 64 sequences over 4000: 128 rows of bf16 290 and 281, of fp32 335 and 320, of 16 sequences 83
+  // and 101, 94 and 113.
+  const bool half = c->dtype == SKIPCONV_BF16, large = c->head_dim > 128;
+  p->few = most * group <= (large ? 128 : half ? 32 : 64);
+  // Heads of 192, 8192 rows of two sequences: 1037 us with tiles shared in LDS, 2090 without; of 256, where the outputs leave those too few
+  // registers, 3895 and 2099.
+  p->wide = !p->few && half && c->head_dim <= kPackedWideDim;
+  // 512 rows a unit read LDS less than 256, where they are enough to fill the GPU: 4096 rows, 8 heads of 64 over 8192 269 and 323 us, 2048 rows over
+  // 4096 123 and 91.
+  const bool twice = p->wide && c->head_dim <= kWideDoubleDim && most * group > 256 && items(9) >= 256;
   p->log_rows = p->few ? 4 : p->wide ? log_packed_wide_rows(c->head_dim) + twice : 6;
   p->keys = p->wide ? packed_wide_keys(c->head_dim) : kPackedKeys;
   int64_t units = items(p->log_rows);
@@ -51,15 +61,19 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
     return (int)std::min<int64_t>(want, units * ((tiles + p->min_chunk - 1) / p->min_chunk));
   };
   if (p->few) {
-    const bool alone = reach <= (c->head_dim <= 128 ? 1024 : 512);
-    p->waves = c->head_dim <= 128 && alone && units <= 256 ? 8 : 4;
-    p->min_chunk = 8;
-    p->target = alone ? 0 : shares(c->head_dim <= 128 ? 512 : 256);
+    // A second launch, which joins shares of keys, costs some 7 us: short items are not shared, longer ones neither where they fill the GPU. Heads of 64,
+    // one token of 1 sequence over 1536: 15.2 us, shared 16.9, over 2048 17.6 and 16.8; of 128 sequences over 2048 25 and 36. Where each compute unit
+    // has one item or none its workgroup is of eight waves (1024 keys: 12.6 us, of four 13.6; 256 keys: 8.7 and 7.9).
+    const bool alone = reach <= (units >= 256 ? 2048 : large ? 1024 : 1536);
+    p->waves = !large && alone && reach > 512 && units <= 256 ? 8 : 4;
+    p->min_chunk = 8;  // 256 keys, of 4096 17.6 us, 512 19.4
+    p->target = alone ? 0 : shares(large ? 256 : 512);  // workgroups that the GPU holds
     p->slack = 0;
   } else {
-    const int want = p->wide ? 256 : 512;  // workgroups that the GPU holds
+    // 64 rows of 8 sequences over 700, heads of 128: shared 29 us, else 33; 64 rows over 500, heads of 64, 21 and 19.
+    const int want = p->wide || large ? 256 : 512;
     p->min_chunk = 256 / p->keys;
-    p->target = units < want && reach > 3 * 256 ? shares(want) : 0;
+    p->target = units < want && reach > 512 ? shares(want) : 0;
     p->slack = p->target ? 256 / p->keys : 0;
   }
   p->slots = 2 * p->target;
@@ -142,8 +156,9 @@ int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, c
   const int whole = whole_pages(p.a.c, p.s);
   const bool half = c->dtype == SKIPCONV_BF16;
   hipError_t e = plan.few    ? (half ? launch_packed_few_bf16(p, plan.waves, whole, st) : launch_packed_few_f32(p, plan.waves, whole, st))
-                 : plan.wide ? launch_packed_wide_bf16(p, st) : launch_packed_many_f32(p, whole, st);
-  if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), st);
+                 : plan.wide ? launch_packed_wide_bf16(p, st) : half ? launch_packed_many_bf16(p, whole, st) : launch_packed_many_f32(p, whole, st);
+  // (512 rows of 16 sequences over 4000: a workgroup a row 22 us, lane groups 28; 2048 rows of 64 sequences over 8192 74 and 67)
+  if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), 1024, st);
   return hip_result(e, "attend launch");
 }
 
