@@ -344,6 +344,12 @@ ATTENDS = [
     ([(40, 100)], 2, 1, 192, 4, "f32", "heads"),
     ([(5, 400)], 4, 1, 96, 8, "f32", "heads"),
     ([(1, 9)] * 70 + [(3, 60)] * 70, 2, 1, 64, 16, "bf16", "heads"),
+    ([(70, 150), (9, 400)], 4, 2, 192, 16, "bf16", "heads"),
+    ([(150, 170)], 2, 1, 160, 5, "bf16", "slots"),
+    ([(200, 333), (1, 50)], 2, 2, 256, 7, "bf16", "heads"),
+    ([(70, 90), (40, 500)], 4, 1, 200, 16, "bf16", "slots"),
+    ([(30, 100), (3, 650)], 2, 1, 64, 16, "f32", "heads"),
+    ([(16, 300)] * 300, 4, 1, 32, 16, "bf16", "heads"),
 ]
 
 
@@ -496,6 +502,8 @@ LARGE = [
     ([(2, 900 - 10 * b) for b in range(70)], 8, 2, 256, 16, "bf16"), ([(300, 300), (1, 4000), (700, 2100)], 4, 2, 128, 64, "bf16"), ([(513, 1025)], 2, 2, 256, 32, "bf16"),
     ([(260, 900), (40, 5000)], 4, 2, 96, 48, "bf16"), ([(600, 1300)], 8, 2, 32, 16, "bf16"), ([(300, 700), (1, 2500)], 4, 2, 64, 16, "f32"), ([(130, 600)], 2, 1, 256, 16, "f32"),
     ([(1500, 1500)], 2, 1, 64, 64, "bf16"), ([(257, 1000)] * 5, 4, 4, 40, 16, "bf16"),
+    ([(300, 2500), (3, 70)], 2, 1, 192, 16, "bf16"), ([(600, 3000)], 1, 1, 256, 48, "bf16"), ([(140, 3000)], 2, 1, 200, 9, "bf16"), ([(16, 4000), (2, 9)], 4, 2, 128, 64, "f32"),
+    ([(512, 700)] * 40, 4, 4, 64, 16, "bf16"), ([(8, 1500 + b) for b in range(40)], 4, 2, 64, 16, "bf16"),
 ]
 
 
