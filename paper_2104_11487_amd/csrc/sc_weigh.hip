@@ -115,8 +115,9 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
   constexpr int kStep = SPLIT ? 16 * kWaves : 16;  // rows from a block of the wave to its next one
   const struct {
     int token, of_group;
-    int64_t q, wrap;
-  } row_step = {kStep / p.group, kStep % p.group, kStep / p.group * p.q_token + kStep % p.group * p.q_head, p.q_token - p.group * p.q_head};
+    int64_t q, wrap, lse;
+  } row_step = {kStep / p.group, kStep % p.group, kStep / p.group * p.q_token + kStep % p.group * p.q_head, p.q_token - p.group * p.q_head,
+                (int64_t)(kStep / p.group) * p.q_heads + kStep % p.group};
   // Step i of a product takes of lane (row or key, quarter) eight elements from here on: where keys are codes a quarter's lie in a row, so
   // that one load brings a key's codes of all steps; otherwise the quarters' lie side by side, 64 or 128 bytes a load and key.
   const auto element = [&](int i) { return W::kPacked ? 8 * (NG * quad + i) : 32 * i + 8 * quad; };
@@ -164,34 +165,44 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
 
     // Blocks of rows that were fetched. Where rows are many, as many as the registers hold: products take them where they are, and the next
     // ones take their place.
+    // What the head has no elements for, and what no row is there for, stays as it begins here.
     uint32_t raw[DEPTH][NG][kWords];
     float raw_lse[DEPTH];
     int raw_token[DEPTH];
     int token = 0, of_group = 0;  // of the lane's row that was fetched last
     const Q* row_q = nullptr;
+    const float* row_lse = nullptr;
     const auto find_row = [&](int r0) {
       token = (r0 + col) / p.group, of_group = r0 + col - token * p.group;
-      row_q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + token) * p.q_token + (int64_t)(head * p.group + of_group) * p.q_head;
+      const int h = head * p.group + of_group;
+      row_q = reinterpret_cast<const Q*>(p.q) + (int64_t)(s.start + token) * p.q_token + (int64_t)h * p.q_head;
+      row_lse = p.lse + (int64_t)(s.start + token) * p.q_heads + h;
     };
     const auto next_row = [&](int r0) {  // of the next block that the wave takes, at r0
       if constexpr (!SPLIT) return find_row(r0);
-      token += row_step.token, of_group += row_step.of_group, row_q += row_step.q;
-      if (of_group >= p.group) of_group -= p.group, ++token, row_q += row_step.wrap;
+      token += row_step.token, row_q += row_step.q, row_lse += row_step.lse;
+      if (row_step.of_group > 0) {
+        of_group += row_step.of_group;
+        if (of_group >= p.group) of_group -= p.group, ++token, row_q += row_step.wrap, row_lse += p.q_heads - p.group;
+      }
     };
     const auto fetch_rows = [&](int x) {
-      const bool there = token < s.n;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int d = element(i);
-#pragma unroll
-        for (int part = 0; part < kWords / 4; ++part) {
-          const uint4 w = there && d < p.dim ? reinterpret_cast<const uint4*>(row_q + d)[part] : uint4{0u, 0u, 0u, 0u};
-          uint32_t* const to = &raw[x][i][4 * part];
-          to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
-        }
-      }
       raw_token[x] = token;
-      raw_lse[x] = there ? p.lse[(int64_t)(s.start + token) * p.q_heads + head * p.group + of_group] : kNegInf;
+      if (token < s.n) {
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int d = element(i);
+          if (d < p.dim) {
+#pragma unroll
+            for (int part = 0; part < kWords / 4; ++part) {
+              const uint4 w = reinterpret_cast<const uint4*>(row_q + d)[part];
+              uint32_t* const to = &raw[x][i][4 * part];
+              to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+            }
+          }
+        }
+        raw_lse[x] = *row_lse;
+      }
     };
     const auto take_rows = [&](int x, int r0) {  // what was fetched
       less = raw_lse[x] == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse[x] * kLog2e;
@@ -227,6 +238,14 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     const int first_row = row_begin + (SPLIT ? 16 * wave : 0);
     const int row_count = rows_end > 0 ? rows_all : 0;
     if (first_row < row_count && !rows_held) {
+#pragma unroll
+      for (int x = 0; x < DEPTH; ++x) {
+        raw_lse[x] = kNegInf;
+#pragma unroll
+        for (int i = 0; i < NG; ++i)
+#pragma unroll
+          for (int e = 0; e < kWords; ++e) raw[x][i][e] = 0u;
+      }
       find_row(first_row), fetch_rows(0);
 #pragma unroll
       for (int x = 1; x < DEPTH; ++x)
