@@ -205,8 +205,8 @@ int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, con
   p.tiles = ((int64_t)c->table_width * c->page_size + 31) / 32;
   const int64_t most = w->max_new > 0 ? std::min<int64_t>(w->max_new, c->tokens) : c->tokens;
   // The waves of a workgroup share a key tile's rows where these are many, else its keys. Over 8192 keys, heads of 64 of bf16 (of 128 in 4 bits),
-  // keys shared and rows shared: 128 rows of 16 sequences 24 and 34 us (41 and 72), of 4 sequences 13 and 11 (19 and 21); 512 rows of 16
-  // sequences 69 and 58 (144 and 155), of 4 sequences 39 and 18 (61 and 40).
+  // keys shared and rows shared: 128 rows of 16 sequences 24 and 30 us (40 and 75), of 4 sequences 13 and 11 (19 and 21); 512 rows of 16
+  // sequences 69 and 54 (142 and 150), of 4 sequences 39 and 18 (61 and 39).
   return hip_result(launch_weigh(p, c->dtype, most * p.group > 128, static_cast<hipStream_t>(stream)), "weigh launch");
 }
 
