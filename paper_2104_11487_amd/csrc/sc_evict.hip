@@ -4,9 +4,11 @@
 // First launch, a workgroup a sequence and key head: the weights' keys (ordered integers) go to LDS, where 36864 fit (beyond, each pass reads
 // the weights again); the key that divides kept from evicted is found digit by digit (11, 11 and 10 bits, a histogram in LDS each); then each
 // wave counts what stays of its section of the tokens, and writes their positions behind those of the waves before. Of equal weights at the
-// border the earlier tokens stay. Bound by latencies: 16 waves, of which the loads are in flight eight at a time. Second launch: the kept rows'
+// border the earlier tokens stay. Bound by latencies, of loads and of barriers: 16 waves, 16 loads of each in flight (16 sequences of up to 32768,
+// 4 key heads: 54 us, one sequence of 1100: 9; histograms for every third wave took as long). Second launch: the kept rows'
 // bytes move, in pieces of 16 bytes where the parts allow it; source and destination pages are different ones, so rows move in any order. Bound by
-// memory.
+// memory: up to 8192 tokens of each of those, 152 MB read and written, in 54 us; kept rows of 64 and 16 bytes lie apart in lines of 128, of which
+// the counters see 128 MB read.
 #include "sc_packed_device.h"
 #include "sc_stream.h"
 

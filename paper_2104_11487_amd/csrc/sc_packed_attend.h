@@ -1,4 +1,4 @@
-// Attention over a paged cache in 4 bits (sc_packed.h), every row count.
+// Attention over a paged cache in 4 bits (sc_packed.h): few rows, many rows of fp32, and of bf16 where heads are above kPackedWideDim.
 //
 //   o = sum_l exp(s_l - m) v_l / sum_l exp(s_l - m),   s_l = scale q . k_l,   over the keys l that the row sees
 //
@@ -14,6 +14,13 @@
 // softmax's scale), fp32 rows are two fp16 parts (22 bits). Scores and sums are fp32. For bf16 the exponentials are rounded to fp16 (2^-11 of each)
 // for the product with V, for fp32 they are two parts; they are formed 2^7 too large, so that those of up to 2^-21 of the
 // reference's stay normal numbers.
+//
+// Few rows are bound by the order of a wave's work first: a tile of 32 keys is some 400 vector instructions (13 for eight codes) between its
+// copies and its last product, and two waves a SIMD hide half of each other's waits. Two workgroups of four waves a compute unit rather than
+// one of eight: a workgroup's waves join at an item's end, and the other's work goes on (121 -> 105 us); three waves a SIMD have two stages of
+// LDS each and lose more by waiting (139 us). One token of 64 sequences of up to 16384, 32 / 4 heads of 128: 97 us and 8 for the join, 3.4 TB/s of codes and pairs (the
+// float cache's bytes would take 2.2 times as long at the copy's rate); of one sequence over 262141, 8 / 2 heads of 128: 26 and 7; over 777, 16 / 4 heads of 64: 11, a chain of latencies.
+// fp32, up to 300 tokens of 9 sequences, window 700, heads of 80: 21 and 5.
 #pragma once
 
 #include <type_traits>

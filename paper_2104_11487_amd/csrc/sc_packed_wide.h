@@ -4,7 +4,10 @@
 // tiles in LDS, scores and outputs are formed transposed, keys run one block of 32 ahead of values. What differs: a tile's codes come through
 // registers, become fp16 values (13 vector operations for 8) and are written to LDS by all waves, each value once for all of the workgroup's
 // rows; so workgroups are of eight waves, one a compute unit, and the tile after next is in flight as codes, a quarter of the
-// bytes. Queries and exponentials are fp16 as in sc_packed_attend.h.
+// bytes. Queries and exponentials are fp16 as in sc_packed_attend.h. Heads above 128 leave a SIMD one wave, heads above kPackedWideDim no registers for it.
+//
+// Bound by the vector unit beside the matrix unit, as there, with the codes' share on top, a tenth: 8192 tokens of two sequences over up to 24576, 16 / 4 heads
+// of 128, 1740 to 1865 us by card (the float cache's kernel: 1570), 863 to 923 TFLOP/s; 4096 tokens of 4 sequences over 12288, 8 / 4 heads of 64, 446 to 478 us (409).
 #pragma once
 
 #include "sc_attend_wide.h"

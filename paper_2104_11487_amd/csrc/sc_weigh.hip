@@ -3,10 +3,15 @@
 // (a new token's own: the sum alone). Scores as in the attention kernels, transposed: S' = K Q', keys held in registers, rows streamed.
 //
 // A unit of work is a tile of keys of one sequence and key head; a workgroup takes an equal share of them in a row (lengths are on the device, so
-// the launch does not know how many there are). Where rows are few the four waves take 32 keys each, and keep the rows' operand while the share
+// the launch does not know how many there are). Where rows are few the four waves take keys of their own, and keep the rows' operand while the share
 // stays with a key head; where they are many the waves take the same keys and every fourth block of 16 rows, and are added in LDS, in wave
 // order: no atomics, equal calls give equal bits. Keys in 4 bits are fp16 numbers: few rows of bf16 come into fp16, exactly, by a power of two
 // (as in sc_packed_attend.h); for many rows, that would cost more than it saves, and the keys become two bf16 parts (8 + 3 bits) instead.
+//
+// Few rows are bound by the vector unit's work on codes and sums and by a unit's chain of latencies (page number, keys, old weight), three waves a
+// SIMD: one token of 32 sequences of up to 16384, 32 / 4 heads of 128 in 4 bits, 32 us, 2.9 TB/s. Many rows by the exponentials (a fused
+// multiply-add, an exponential and a sum for each score of each row) and the begin and end of units: 512 tokens of 4 sequences over 12000, 8 / 2 heads of 64
+// of bf16, 59 us, 415 TFLOP/s. Blocks of 32 rows and keys, whose sums take the registers of a wave, 67 us.
 #include "sc_packed_device.h"
 
 #include <algorithm>
