@@ -47,9 +47,16 @@ struct PackedStager {
     for (int t = 0; t < kItems; ++t) {
       const int i = t * THREADS + thread, r = i / groups;
       value[t] = r >= KEYS;
-      row[t] = r < 2 * KEYS ? r & (KEYS - 1) : -1;
+      row[t] = r < 2 * KEYS ? spread(r & (KEYS - 1)) : -1;
       group[t] = i - r * groups;
     }
+  }
+  // Rows whose pieces a wave writes together: of each 16 in the order in which the permutation of a row's pieces puts those of one place
+  // into other banks (in their own order four rows' met in one, 15 % of a prompt's cycles).
+  __device__ __forceinline__ static int spread(int r) {
+    if constexpr (TL::kChunks >= 16) return (r & ~15) | ((r & 3) << 2) | ((r >> 2) & 3);
+    else if constexpr (TL::kChunks == 8) return (r & ~15) | (r & 1) | ((r & 6) << 1) | ((r & 8) >> 2);
+    else return r;
   }
   __device__ __forceinline__ void load_row(int t, uint4* c, uint32_t* s) const {
     const CacheView& v = p.a.c;
