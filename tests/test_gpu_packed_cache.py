@@ -579,6 +579,11 @@ WEIGHS = [
     ([(1, 150), (30, 60)], 6, 2, 160, 16, "f32", True), ([(3, 100)], 4, 2, 32, 5, "f32", True), ([(70, 90)], 2, 1, 256, 16, "f32", True), ([(33, 70)], 4, 4, 64, 16, "f32", True),
     ([(1, 77), (30, 200)], 4, 2, 64, 16, "bf16", False), ([(1, 40)] * 70, 2, 1, 128, 16, "bf16", False), ([(9, 90)], 2, 2, 40, 3, "bf16", False), ([(90, 100)], 2, 1, 256, 16, "bf16", False),
     ([(1, 77), (30, 200)], 4, 2, 80, 16, "f32", False), ([(100, 120)], 2, 1, 256, 32, "f32", False), ([(4, 50)], 1, 1, 8, 16, "f32", False),
+    # rows shared between waves: several blocks a wave, groups that do not divide them
+    ([(200, 290), (3, 40), (0, 9), (65, 65)], 6, 2, 64, 16, "bf16", True), ([(150, 140), (40, 300)], 5, 1, 24, 7, "bf16", True), ([(90, 130), (70, 200)], 6, 2, 200, 32, "bf16", True),
+    ([(140, 333)], 3, 3, 128, 64, "bf16", True), ([(200, 290), (3, 40), (65, 65)], 6, 2, 64, 16, "bf16", False), ([(130, 200)], 7, 1, 32, 5, "bf16", False),
+    ([(70, 210), (1, 1)], 10, 1, 128, 48, "bf16", False), ([(150, 160), (9, 30)], 3, 1, 64, 16, "f32", True), ([(131, 190)], 2, 2, 32, 3, "f32", True),
+    ([(60, 100), (30, 31)], 5, 1, 96, 16, "f32", True), ([(150, 160), (9, 30)], 3, 1, 64, 16, "f32", False), ([(200, 201)], 1, 1, 16, 16, "f32", False), ([(50, 190)], 6, 1, 128, 32, "f32", False),
 ]
 
 
@@ -619,6 +624,21 @@ def test_weight(case, mask):
             _compare_weights(np.where(untouched, 0.0, weights.double().cpu().numpy()), keep, size, dim, decay, np.nan_to_num(before), most * heads // kv_heads)
             again = cache.weigh(q, lse, batch, _gpu(before), causal=mask[0], window=mask[1], decay=decay)
             assert torch.equal(again.view(torch.int32), weights.view(torch.int32))
+
+
+@pytest.mark.parametrize("packed", [True, False], ids=["packed", "paged"])
+@pytest.mark.parametrize("dtype,new", [("bf16", 3), ("bf16", 150), ("f32", 3), ("f32", 150)])
+def test_weight_of_queries_of_other_strides(dtype, new, packed):
+    """Every second head of wider rows, and heads before tokens: the bits of packed queries."""
+    rng, cache, k64, q, q64, table, starts, length = _weigh_case(([(new, 190), (1, 70)], 6, 2, 64, 16, dtype, packed), 154)
+    batch = _device(table, starts, length)
+    _, lse = cache.attend(q, batch, return_lse=True)
+    want = cache.weigh(q, lse, batch, torch.zeros(k64.shape[:3], device="cuda"))
+    wide = torch.full((q.shape[0], 13, 80), float("nan"), dtype=q.dtype, device="cuda")
+    wide[:, 1::2, 8:72] = q
+    for other in (wide[:, 1::2, 8:72], q.transpose(0, 1).contiguous().transpose(0, 1)):
+        got = cache.weigh(other, lse, batch, torch.zeros(k64.shape[:3], device="cuda"))
+        assert torch.equal(got.view(torch.int32), want.view(torch.int32))
 
 
 def test_weight_adds_up_to_the_rows():
