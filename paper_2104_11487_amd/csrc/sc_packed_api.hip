@@ -86,11 +86,11 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
   return SKIPCONV_OK;
 }
 
-// Every lane's row of a 16-key block lies in the block's page, at an offset of 30 bits, and a page's stride has 32.
+// Every lane's row of a 16-key block lies in the block's page, at an offset of 30 bits, and a page's stride and its slots' offsets have 32.
 bool whole_pages(const CacheView& c, const ScaleView& s) {
   const int64_t slot = std::max(std::max(c.k_slot, c.v_slot), std::max(s.k_slot, s.v_slot));
   const int64_t page = std::max(std::max(c.k_page, c.v_page), std::max(s.k_page, s.v_page));
-  return c.page_size % 16 == 0 && 16 * slot < (1ll << 30) && page < (1ll << 32);
+  return c.page_size % 16 == 0 && 16 * slot < (1ll << 30) && page < (1ll << 32) && c.page_size * slot < (1ll << 32);
 }
 
 int check_weigh(const skipconv_cache* c, const skipconv_weigh* w) {

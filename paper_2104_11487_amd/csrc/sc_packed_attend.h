@@ -15,12 +15,12 @@
 // for the product with V, for fp32 they are two parts; they are formed 2^7 too large, so that those of up to 2^-21 of the
 // reference's stay normal numbers.
 //
-// Few rows are bound by the order of a wave's work first: a tile of 32 keys is some 400 vector instructions (13 for eight codes) between its
-// copies and its last product, and two waves a SIMD hide half of each other's waits. Two workgroups of four waves a compute unit rather than
-// one of eight: a workgroup's waves join at an item's end, and the other's work goes on (121 -> 105 us); three waves a SIMD have two stages of
-// LDS each and lose more by waiting (139 us). One token of 64 sequences of up to 16384, 32 / 4 heads of 128: 97 us and 8 for the join, 3.4 TB/s of codes and pairs (the
-// float cache's bytes would take 2.2 times as long at the copy's rate); of one sequence over 262141, 8 / 2 heads of 128: 26 and 7; over 777, 16 / 4 heads of 64: 11, a chain of latencies.
-// fp32, up to 300 tokens of 9 sequences, window 700, heads of 80: 21 and 5.
+// Few rows are bound by the stream of codes and, beside it, by the order of a wave's work: a tile of 32 keys is some 350 vector instructions (13 for
+// eight codes) between its copies and its last product, of which two waves a SIMD hide half of each other's waits. One token of 64 sequences over
+// 8192, 32 / 4 heads of 128: 83 us; without products 72, without copies 67, 8 of each the join. Two workgroups of four waves a compute unit rather than one
+// of eight: a workgroup's waves join at an item's end, and the other's work goes on (sequences of up to 16384: 121 -> 104 us, 3.5 TB/s); three waves
+// a SIMD have two stages of LDS each and lose more by waiting (139 us), a fourth stage changes nothing (111 us). One sequence over 262141, 8 / 2 heads of 128: 25 us and 7 for the join; over
+// 777, 16 / 4 heads of 64: 12, a chain of latencies. fp32, up to 300 tokens of 9 sequences, window 700, heads of 80: 20 and 5.
 #pragma once
 
 #include <type_traits>
@@ -97,6 +97,7 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
     // page and slot strides of the keys' codes and pairs, the values' codes and pairs
     const uint32_t k_page = alone(p.c.k_page), k_slot = alone(p.c.k_slot), ks_page = alone(pp.s.k_page), ks_slot = alone(pp.s.k_slot);
     const uint32_t v_page = alone(p.c.v_page), v_slot = alone(p.c.v_slot), vs_page = alone(pp.s.v_page), vs_slot = alone(pp.s.v_slot);
+    const bool alike = k_page == v_page && k_slot == v_slot && ks_page == vs_page && ks_slot == vs_slot;
     const uint32_t v_sel = NG >= 4 ? 0x0c040c00u : 0x0c040c00u + ((NG * col) & 3) * 0x00010001u;  // picks a byte of two words into 16-bit halves
     const int rows = u.n * p.group, row0 = u.row0 + (MANY ? wave * WROWS : 0);
 
@@ -150,9 +151,12 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
         const char* pairs[4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint64_t page = (uint32_t)page_of_entry(p.c, entry[j]), at = (uint32_t)slot[j];
-          base[j] = kb + (page * k_page + at * k_slot), pairs[j] = ksb + (page * ks_page + at * ks_slot);
-          base[2 + j] = vb + (page * v_page + at * v_slot), pairs[2 + j] = vsb + (page * vs_page + at * vs_slot);
+          const uint64_t page = (uint32_t)page_of_entry(p.c, entry[j]);
+          const uint32_t at = (uint32_t)slot[j];
+          const uint64_t k_off = page * k_page + at * k_slot, ks_off = page * ks_page + at * ks_slot;  // within a page 32 bits
+          uint64_t v_off = k_off, vs_off = ks_off;
+          if (!alike) v_off = page * v_page + at * v_slot, vs_off = page * vs_page + at * vs_slot;
+          base[j] = kb + k_off, pairs[j] = ksb + ks_off, base[2 + j] = vb + v_off, pairs[2 + j] = vsb + vs_off;
         }
         if constexpr (NG >= 4) {  // a copy's rows are of one block
           constexpr int kRows = 64 / NG;
@@ -300,9 +304,10 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
       const bool edge = key0 < inside_lo || key0 > inside_hi;  // some row does not see some of the keys
       const char* const tile_at = ring + stage;
       floatx4 s[2];
+      uint32_t codes[2][NG], k_pairs[2][PIECES];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        uint32_t kc[NG], kp[PIECES];
+        uint32_t (&kc)[NG] = codes[j];
         if constexpr (NG == 1) {
           kc[0] = *reinterpret_cast<const uint32_t*>(tile_at + k_at[0] + j * 16 * Ring::kRow);
         } else if constexpr (NG == 2) {
@@ -316,11 +321,15 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
           }
         }
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) kp[i] = *reinterpret_cast<const uint32_t*>(tile_at + kp_at + j * 64 * NG + 4 * i);
+        for (int i = 0; i < PIECES; ++i) k_pairs[j][i] = *reinterpret_cast<const uint32_t*>(tile_at + kp_at + j * 64 * NG + 4 * i);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // both blocks' reads before the first one's products
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
         s[j] = floatx4{};
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const half8 kf = values8(kc[i], kp[NG == 8 ? i / 4 : 0], bits);
+          const half8 kf = values8(codes[j][i], k_pairs[j][NG == 8 ? i / 4 : 0], bits);
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) s[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[part][i], s[j], 0, 0, 0);
         }
@@ -347,6 +356,8 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
         }
         ref = fmaxf(ref, top);  // nothing to rescale yet
       }
+      uint32_t vc[8][PIECES], pairs[8];
+      load_values(tile_at, vc, pairs);  // ahead of the exponentials
       __builtin_amdgcn_sched_barrier(0);
       const float base = ref == kNegInf ? 0.0f : ref - kPackedLift;
       uint32_t w[PARTS][4];
@@ -367,8 +378,6 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
       // Where some row does not see some key, that key's exponential is zero, but zero times an infinity or a NaN is not: pairs of keys that
       // no row sees become zero, and so do those whose smallest or largest value is not finite, which are added by themselves.
       bool odd = false;
-      uint32_t vc[8][PIECES], pairs[8];
-      load_values(tile_at, vc, pairs);
       if (edge) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
