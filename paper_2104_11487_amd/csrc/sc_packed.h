@@ -51,13 +51,10 @@ constexpr int kPackedManyWaves = 4;  // of a workgroup whose waves take 16 rows 
 // Few rows: a unit is 16 rows, whose keys the workgroup's waves share.
 hipError_t launch_packed_few_bf16(const PackedAttendParams& p, int waves, int whole_pages, hipStream_t stream);
 hipError_t launch_packed_few_f32(const PackedAttendParams& p, int waves, int whole_pages, hipStream_t stream);
-hipError_t launch_packed_many_bf16(const PackedAttendParams& p, int whole_pages, hipStream_t stream);  // heads above kPackedWideDim
 hipError_t launch_packed_many_f32(const PackedAttendParams& p, int whole_pages, hipStream_t stream);
-// Many rows of bf16, heads of up to kPackedWideDim, sharing key tiles in LDS: rows of a unit, of which heads of up to kWideDoubleDim also take
-// twice as many; keys of a tile.
+// Many rows of bf16 sharing key tiles in LDS: rows of a unit, of which heads of up to kWideDoubleDim also take twice as many; keys of a tile.
 inline int log_packed_wide_rows(int dim) { return dim <= 128 ? 8 : 7; }
 constexpr int packed_wide_keys(int dim) { return dim <= 64 ? 128 : 64; }
-constexpr int kPackedWideDim = 192;
 hipError_t launch_packed_wide_bf16(const PackedAttendParams& p, hipStream_t stream);
 
 // Accumulated attention weight. The cache's keys are codes where `packed`, else of the dtype.

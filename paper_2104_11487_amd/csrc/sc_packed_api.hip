@@ -42,13 +42,11 @@ int plan_packed(const skipconv_cache* c, const skipconv_attend* a, PackedPlan* p
   // Few rows: 16 a workgroup, whose waves share the keys, while a second block of rows costs less than rows that share keys in LDS or with
   // waves of their own. 16 sequences over 4000, heads of 64: 8 rows of bf16 21 us, by the other kernel 25, 32 rows 30 and 26, but over 300 keys
   // 10 and 12, and 64 sequences over 4000 40 and 47 (64 rows: 61 and 49); of fp32, 64 rows 34 and 33, over 300 keys 10 and 18, 128 rows 40 and 41,
-  // of 64 sequences 112 and 105. Heads of 256, 64 sequences over 4000: 128 rows of bf16 290 and 281, of fp32 335 and 320, of 16 sequences 83
-  // and 101, 94 and 113.
+  // of 64 sequences 112 and 105. Larger heads, 64 sequences over 4000: of 192, bf16, 64 rows 157 and 141, over 4096 of 16 sequences 60 both, 128 rows
+  // 297 and 232; of 256, 64 rows 155 and 240, 128 rows 297 and 371, of one sequence 35 and 52; of fp32, 128 rows 335 and 320, of 16 sequences 94 and 113.
   const bool half = c->dtype == SKIPCONV_BF16, large = c->head_dim > 128;
-  p->few = most * group <= (large ? 128 : half ? 32 : 64);
-  // Heads of 192, 8192 rows of two sequences: 1037 us with tiles shared in LDS, 2090 without; of 256, where the outputs leave those too few
-  // registers, 3895 and 2099.
-  p->wide = !p->few && half && c->head_dim <= kPackedWideDim;
+  p->few = most * group <= (half ? (c->head_dim > 192 ? 128 : large ? 64 : 32) : large ? 128 : 64);
+  p->wide = !p->few && half;
   // 512 rows a unit read LDS less than 256, where they are enough to fill the GPU: 4096 rows, 8 heads of 64 over 8192 269 and 323 us, 2048 rows over
   // 4096 123 and 91.
   const bool twice = p->wide && c->head_dim <= kWideDoubleDim && most * group > 256 && items(9) >= 256;
@@ -156,7 +154,7 @@ int skipconv_packed_attend(const skipconv_cache* c, const skipconv_packing* s, c
   const int whole = whole_pages(p.a.c, p.s);
   const bool half = c->dtype == SKIPCONV_BF16;
   hipError_t e = plan.few    ? (half ? launch_packed_few_bf16(p, plan.waves, whole, st) : launch_packed_few_f32(p, plan.waves, whole, st))
-                 : plan.wide ? launch_packed_wide_bf16(p, st) : half ? launch_packed_many_bf16(p, whole, st) : launch_packed_many_f32(p, whole, st);
+                 : plan.wide ? launch_packed_wide_bf16(p, st) : launch_packed_many_f32(p, whole, st);
   // (512 rows of 16 sequences over 4000: a workgroup a row 22 us, lane groups 28; 2048 rows of 64 sequences over 8192 74 and 67)
   if (e == hipSuccess && plan.slots) e = launch_attend_join(p.a, elem_of(c), 1024, st);
   return hip_result(e, "attend launch");

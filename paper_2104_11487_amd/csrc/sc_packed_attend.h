@@ -1,4 +1,4 @@
-// Attention over a paged cache in 4 bits (sc_packed.h): few rows, many rows of fp32, and of bf16 where heads are above kPackedWideDim.
+// Attention over a paged cache in 4 bits (sc_packed.h): few rows, and many rows of fp32.
 //
 //   o = sum_l exp(s_l - m) v_l / sum_l exp(s_l - m),   s_l = scale q . k_l,   over the keys l that the row sees
 //

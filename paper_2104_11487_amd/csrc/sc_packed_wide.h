@@ -4,10 +4,11 @@
 // tiles in LDS, scores and outputs are formed transposed, keys run one block of 32 ahead of values. What differs: a tile's codes come through
 // registers, become fp16 values (13 vector operations for 8) and are written to LDS by all waves, each value once for all of the workgroup's
 // rows; so workgroups are of eight waves, one a compute unit, and the tile after next is in flight as codes, a quarter of the
-// bytes. Queries and exponentials are fp16 as in sc_packed_attend.h. Heads above 128 leave a SIMD one wave, heads above kPackedWideDim no registers for it.
+// bytes. Queries and exponentials are fp16 as in sc_packed_attend.h. Heads above 128 leave a SIMD one wave. What is small is made to be inlined: the
+// program is long enough for the compiler to call it otherwise, with operands in scratch memory.
 //
 // Bound by the vector unit beside the matrix unit, as there, with the codes' share on top, a tenth: 8192 tokens of two sequences over up to 24576, 16 / 4 heads
-// of 128, 1740 to 1865 us by card (the float cache's kernel: 1570), 863 to 923 TFLOP/s; 4096 tokens of 4 sequences over 12288, 8 / 4 heads of 64, 446 to 478 us (409).
+// of 128, 1720 to 1840 us by card (the float cache's kernel: 1570), 875 to 936 TFLOP/s; 4096 tokens of 4 sequences over 12288, 8 / 4 heads of 64, 446 to 478 us (409).
 #pragma once
 
 #include "sc_attend_wide.h"
@@ -120,7 +121,7 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
   constexpr int NB = KEYS / 32, ND = DP / 32;  // blocks of 32 keys of a tile; of 32 dimensions
   using TL = Tile<uint16_t, DP, KEYS, NW, true>;
   constexpr int QF = DP / 16;  // 16-byte pieces of a row that a lane holds
-  __shared__ alignas(16) char lds[4 * TL::kBytes];  // keys, values; two buffers
+  __shared__ alignas(512) char lds[4 * TL::kBytes];  // keys, values; two buffers
   const AttendParams& p = pp.a;
 
   const Units batch(p);
@@ -150,13 +151,17 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
     // Values: see read_column4; e picks the upper four of eight keys.
     const uint32_t lds0 = (uint32_t)(uintptr_t)SC_LDS(lds, char);
     const int vr = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    uint32_t kat[QF], vat[2][ND];
+    // Where registers are short, a fragment's address is formed from one of three: a row is aligned to its length, so that a piece is bits of it
+    // (heads of 256, 8192 tokens of two sequences: 2765 -> 1618 us; heads of 64, two blocks of rows: 645 -> 634; of 128 it would cost 2 %).
+    constexpr bool kForm = DP > 128 || NR == 2;
+    static_assert((TL::kRowBytes & (TL::kRowBytes - 1)) == 0 && TL::kRowBytes <= 512, "the tile's alignment");
+    uint32_t kat[kForm ? 1 : QF], vat[2][kForm ? 1 : ND];
 #pragma unroll
-    for (int i = 0; i < QF; ++i) kat[i] = lds0 + col * TL::kRowBytes + (((2 * i + half) ^ (TL::swizzle(col) & (TL::kChunks - 1))) << 4);
+    for (int i = 0; i < (kForm ? 1 : QF); ++i) kat[i] = lds0 + col * TL::kRowBytes + (((2 * i + half) ^ (TL::swizzle(col) & (TL::kChunks - 1))) << 4);
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
+      for (int d = 0; d < (kForm ? 1 : ND); ++d)
         vat[e][d] = lds0 + 2 * TL::kBytes + (8 * e + vr) * TL::kRowBytes + (((4 * d + vc) ^ (TL::swizzle(8 * e + vr) & (TL::kChunks - 1))) << 4) + (lane & 1) * 8;
 
     const int rows = u.n * p.group;
@@ -207,16 +212,18 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
     }
 
     // `at`: byte offset of a block's rows in the keys' (values') two buffers
-    auto key_piece = [&](int i, int at) {  // 16 bytes of a key's row: the score products' operand
-      return *(__attribute__((address_space(3))) const u32x4_lds*)(kat[i] + at);
+    auto key_piece = [&](int i, int at) __attribute__((always_inline)) {  // 16 bytes of a key's row: the score products' operand
+      const uint32_t from = kForm ? kat[0] ^ (uint32_t)(i << 5) : kat[kForm ? 0 : i];
+      return *(__attribute__((address_space(3))) const u32x4_lds*)(from + at);
     };
-    auto value_piece = [&](int k, int d, int at) {  // 8 keys' values of a dimension: the value products' operand
+    auto value_piece = [&](int k, int d, int at) __attribute__((always_inline)) {  // 8 keys' values of a dimension: the value products' operand
       // rows 16 keys on keep the permutation, which repeats every 16 rows
-      const u32x2 a = read_column4(vat[0][d] + at + 16 * k * TL::kRowBytes), b = read_column4(vat[1][d] + at + 16 * k * TL::kRowBytes);
+      const uint32_t piece = kForm ? (uint32_t)(d << 6) : 0u;
+      const u32x2 a = read_column4((vat[0][kForm ? 0 : d] ^ piece) + at + 16 * k * TL::kRowBytes), b = read_column4((vat[1][kForm ? 0 : d] ^ piece) + at + 16 * k * TL::kRowBytes);
       return u32x4_lds{a[0], a[1], b[0], b[1]};
     };
     using Scores = floatx16[NR];
-    auto score_block = [&](int at, Scores& s) {  // the scores of the 32 keys at `at`
+    auto score_block = [&](int at, Scores& s) __attribute__((always_inline)) {  // the scores of the 32 keys at `at`
 #pragma unroll
       for (int n = 0; n < NR; ++n) s[n] = floatx16{};
 #pragma unroll
@@ -231,7 +238,7 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
     struct Tops {
       float at[NR];
     };
-    auto largest = [](const Scores& s) {
+    auto largest = [](const Scores& s) __attribute__((always_inline)) {
       Tops top;
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
@@ -241,14 +248,14 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
       }
       return top;
     };
-    auto key_of = [&](int r) { return 8 * (r >> 2) + 4 * half + (r & 3); };  // of a block, that score r of a lane belongs to
-    auto hide = [&](Scores& s, int key0) {
+    auto key_of = [&](int r) __attribute__((always_inline)) { return 8 * (r >> 2) + 4 * half + (r & 3); };  // of a block, that score r of a lane belongs to
+    auto hide = [&](Scores& s, int key0) __attribute__((always_inline)) {
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[n][r] = key0 + key_of(r) >= seen[n].lo && key0 + key_of(r) <= seen[n].hi ? s[n][r] : kNegInf;
     };
-    auto refer = [&](Tops top) {  // takes the largest score of the next block into the reference
+    auto refer = [&](Tops top) __attribute__((always_inline)) {  // takes the largest score of the next block into the reference
       bool past = false;
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
@@ -270,18 +277,19 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
         }
       }
     };
-    auto exponent = [&](float x, int n) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, factor[n], -base[n])); };
+    auto exponent = [&](float x, int n) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, factor[n], -base[n])); };
 
     // A block's exponentials and values, and the scores of the next one (keys at `kt`, values at `vt`).
-    auto run_block = [&](int kt, int vt, Scores& s, Scores& next) {
+    auto run_block = [&](int kt, int vt, Scores& s, Scores& next) __attribute__((always_inline)) {
       {
+        if constexpr (kForm) kat[0] = here(kat[0]), vat[0][0] = here(vat[0][0]), vat[1][0] = here(vat[1][0]);  // no addresses from one block to the next
         // Laid out by hand: each slot is one fragment's products, with the LDS reads of the one PRE slots later and a share of the
         // vector unit's work (this block's exponentials, then the next one's largest score) to run beside it.
         using PL = SlotPlan<QF, ND>;
         constexpr int PRE = 3, kAll = NR * 16;
         u32x4_lds frag[PL::kSlots];
         uint32_t packed[NR][8];
-        auto read = [&](auto slot) {
+        auto read = [&](auto slot) __attribute__((always_inline)) {
           constexpr int m = slot;
           if constexpr (m < PL::kSlots) {
             constexpr int x = PL::kOrder.at[m];
@@ -289,7 +297,7 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
             else frag[m] = value_piece((x - QF) / ND, (x - QF) % ND, vt);
           }
         };
-        auto form = [&](auto from, auto to) {  // exponentials [from, to) of the lane, in pairs: a half's keys, row block by row block
+        auto form = [&](auto from, auto to) __attribute__((always_inline)) {  // exponentials [from, to) of the lane, in pairs: a half's keys, row block by row block
           constexpr int f = from, t = to;
 #pragma unroll
           for (int e = f; e < t; e += 2) {
@@ -303,11 +311,11 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
         Tops top;
 #pragma unroll
         for (int n = 0; n < NR; ++n) top.at[n] = kNegInf, next[n] = floatx16{};
-        unrolled<PRE>([&](auto m) { read(m); });
+        unrolled<PRE>([&](auto m) __attribute__((always_inline)) { read(m); });
         form(std::integral_constant<int, 0>{}, std::integral_constant<int, PL::exps_by(-1, kAll)>{});
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);  // ahead of the other workgroup's wave, which is then in its copies, waits and reference
-        unrolled<PL::kSlots>([&](auto slot) {
+        unrolled<PL::kSlots>([&](auto slot) __attribute__((always_inline)) {
           constexpr int m = slot, x = PL::kOrder.at[m];
           read(std::integral_constant<int, m + PRE>{});
 #pragma unroll
@@ -340,7 +348,7 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
     // A tile of which some row does not see some key. A masked key's exponential is zero, but zero times an infinity or a NaN is not: the
     // values of keys that no row of the unit sees are zero in LDS already, and those that are not finite are added to the rows
     // that see their key and cleared too.
-    auto settle = [&](int key0, int buf) {
+    auto settle = [&](int key0, int buf) __attribute__((always_inline)) {
       uint4* const rows_of = reinterpret_cast<uint4*>(values + buf * TL::kBytes);
       int odd = 0;
       for (int i = threadIdx.x; i < KEYS * TL::kChunks; i += 64 * NW) odd |= not_finite_h(rows_of[i]);
@@ -366,23 +374,23 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
       for (int i = threadIdx.x; i < KEYS * TL::kChunks; i += 64 * NW) rows_of[i] = finite_of_h(rows_of[i]);
       __syncthreads();
     };
-    auto arrive = [&](int key0, int buf) {  // this tile is in LDS; the other buffers are free
+    auto arrive = [&](int key0, int buf) __attribute__((always_inline)) {  // this tile is in LDS; the other buffers are free
       __syncthreads();
       if (key0 < all_lo || key0 + KEYS - 1 > all_hi) settle(key0, buf);
     };
     // The next tile's codes become values in LDS, and those of the one after it leave memory. Half of the waves do so at a tile's begin, the others
     // in its middle, so that a SIMD's matrix unit has one wave's products meanwhile.
     const bool early = wave < NW / 2;
-    auto stage = [&](int key0, int buf) {
+    auto stage = [&](int key0, int buf) __attribute__((always_inline)) {
       if (key0 + KEYS >= u.hi) return;
       stager.place(key0 + KEYS, buf ^ 1);
       if (key0 + 2 * KEYS >= u.hi) return;
       stager.load();
       stager.find(key0 + 3 * KEYS);
     };
-    auto all_see = [&](int key) { return key >= all_lo && key + 31 <= all_hi; };
+    auto all_see = [&](int key) __attribute__((always_inline)) { return key >= all_lo && key + 31 <= all_hi; };
     // The block at `at` of the tile, keys from key0 on, and the scores and reference of the next one.
-    auto block = [&](int key0, int at, Scores& s, Scores& next) {
+    auto block = [&](int key0, int at, Scores& s, Scores& next) __attribute__((always_inline)) {
       Tops top = run_block(at, at, s, next);
       if (key0 + 32 >= u.hi) return;
       if (!all_see(key0 + 32)) {

@@ -9,7 +9,8 @@ hipError_t launch_packed_wide_bf16(const PackedAttendParams& p, hipStream_t stre
   if (p.a.dim <= 64) return twice ? launch_packed_wide<64, 2>(p, stream) : launch_packed_wide<64, 1>(p, stream);
   if (p.a.dim <= 96) return launch_packed_wide<96, 1>(p, stream);
   if (p.a.dim <= 128) return launch_packed_wide<128, 1>(p, stream);
-  return launch_packed_wide<192, 1>(p, stream);
+  if (p.a.dim <= 192) return launch_packed_wide<192, 1>(p, stream);
+  return launch_packed_wide<256, 1>(p, stream);
 }
 
 }  // namespace sc
