@@ -405,6 +405,23 @@ def test_what_a_row_does_not_see_does_not_reach_it(dtype, lens, heads, page, val
             _compare(out, lse, want, dtype, 64, _largest(v64))
 
 
+@pytest.mark.parametrize("value", ["nan", "inf"])
+@pytest.mark.parametrize("new", [3, 90])
+@pytest.mark.parametrize("dtype,dim", [("bf16", 32), ("bf16", 96), ("bf16", 128), ("bf16", 192), ("bf16", 256), ("f32", 128), ("f32", 256)])
+def test_what_a_row_does_not_see_in_heads_of_every_size(dtype, dim, new, value):
+    """The last group of a head: the last of the registers, lanes and waves that hold one."""
+    def spoil(codes, scales, table):
+        for at in {149, 149 - new // 2, max(150 - new - 20, 0)}:
+            scales[1][table[0, at // 16], 1, at % 16, -1] = (np.nan, np.nan) if value == "nan" else (0.0, np.inf)
+    rng = _rng(147)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, 150), (2, 33)], 4, 2, dim, 16, dtype, spoil=spoil)
+    for mask in ((True, -1), (True, 5), (False, 10)):
+        with np.errstate(invalid="ignore"):
+            want = O.attend(q64, k64, v64, table, starts, length, *mask)
+        for _, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1]):
+            _compare(out, lse, want, dtype, dim, _largest(v64))
+
+
 @pytest.mark.parametrize("dtype,new,kv", [("bf16", 1, 40), ("bf16", 1, 6000), ("bf16", 9, 6000), ("bf16", 50, 300), ("bf16", 200, 900),
                                           ("f32", 1, 6000), ("f32", 60, 300)])
 def test_scores_that_are_nan_stay_nan(dtype, new, kv):
