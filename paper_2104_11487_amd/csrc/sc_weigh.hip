@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     }
     if (key0 >= s.len) i1 = -1;
     const bool whole_keys = key0 + 16 * BLOCKS <= s.len;
-    const int rows_end = (i1 + 1) * p.group, row_begin = SPLIT ? i0 * p.group : 0;
+    const int rows_end = (max(i1, -1) + 1) * p.group, row_begin = SPLIT ? i0 * p.group : 0;
     // (few rows: all of them, so that the operand holds for every unit)
     const int rows_all = SPLIT ? rows_end : s.n * p.group;
 
