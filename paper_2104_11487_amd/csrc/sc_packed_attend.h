@@ -254,8 +254,8 @@ __global__ void __launch_bounds__(64 * NW, NG == 8 ? 1 : 2) attend_packed_kernel
       for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][e]));
     }
     most = max_across32(max_across16(most));
-    const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);  // the largest element comes into [2^14, 2^15)
-    const float factor = ldexpf(p.scale_log2, -lift);  // of a score, to powers of two
+    const int lift = lift_of(most);
+    const float factor = factor_of(p.scale_log2, lift);  // of a score, to powers of two
 #pragma unroll
     for (int i = 0; i < NG; ++i)
 #pragma unroll

@@ -45,6 +45,15 @@ __device__ __forceinline__ half8 values8(uint32_t w, uint32_t pair, const CodeBi
   return __builtin_bit_cast(half8, v);
 }
 
+// A row of queries comes into fp16's range by a power of two: lift_of that which takes its largest element into [2^14, 2^15) (a row of zeros or subnormal
+// numbers: 2^141, below it), factor_of what takes its scores, formed of the lifted row, to powers of two. The factor stays a normal number: as zero it
+// would make a masked score, minus infinity, NaN, and as infinity a score of zero. Below 2^-126 the row's scores are under 2^-87 either way (lifted ones
+// are 2^39 at most) and count as nothing; past 2^128 two that differ (by 2^-48 at least, lifted) do so by 2^80 or more.
+__device__ __forceinline__ int lift_of(float most) { return 141 - (int)((__float_as_uint(most) >> 23) & 255u); }
+__device__ __forceinline__ float factor_of(float scale_log2, int lift) {
+  return __builtin_amdgcn_fmed3f(ldexpf(scale_log2, -lift), __uint_as_float(0x00800000u), __uint_as_float(0x7f7fffffu));
+}
+
 // Of two packed fp16 values those outside the mask become zero, and so do those that are infinite or NaN, which set *odd.
 __device__ __forceinline__ uint32_t finite2h(uint32_t v, uint32_t mask, int* odd) {
   v &= mask;

@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(64 * packed_wide_waves(DP), packed_wide_waves(
         for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(w[e] << 16)), fabsf(__uint_as_float(w[e] & 0xffff0000u))));
       }
       most = max_across32(most);
-      const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);  // the largest element comes into [2^14, 2^15)
-      factor[n] = ldexpf(p.scale_log2, -lift);
+      const int lift = lift_of(most);
+      factor[n] = factor_of(p.scale_log2, lift);
 #pragma unroll
       for (int i = 0; i < QF; ++i) {
         const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};

@@ -212,15 +212,15 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     const auto take_rows = [&](int x, int r0) {  // what was fetched
       less = raw_lse[x] == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse[x] * kLog2e;
       factor = p.scale_log2;
-      if constexpr (W::kScaled) {  // the largest element comes into [2^14, 2^15)
+      if constexpr (W::kScaled) {
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < NG; ++i)
 #pragma unroll
           for (int e = 0; e < 4; ++e) most = fmaxf(most, fmaxf(fabsf(__uint_as_float(raw[x][i][e] << 16)), fabsf(__uint_as_float(raw[x][i][e] & 0xffff0000u))));
         most = max_across32(max_across16(most));
-        const int lift = 141 - (int)((__float_as_uint(most) >> 23) & 255u);
-        factor = ldexpf(p.scale_log2, -lift);
+        const int lift = lift_of(most);
+        factor = factor_of(p.scale_log2, lift);
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
           float y[8];

@@ -14,7 +14,8 @@ from oracle import stream_attention_oracle as O  # noqa: E402
 from paper_2104_11487_amd import skipconv as S  # noqa: E402
 from paper_2104_11487_amd import stream_attention as A  # noqa: E402
 from parity_util import say  # noqa: E402
-from test_gpu_packed_cache import DT, U, _batch, _certain, _device, _garbage, _gpu, _held, _laid, _packed, _rng, _same, _stored  # noqa: E402
+from test_gpu_packed_cache import (DT, U, _attend_both, _batch, _certain, _compare, _compare_weights, _device, _filled, _garbage, _gpu, _held, _laid,  # noqa: E402
+                                   _largest, _packed, _rng, _same, _stored)
 pytestmark = pytest.mark.gpu
 
 
@@ -73,3 +74,47 @@ def test_append_turns_the_way_that_its_rotation_says(dim, pairs, adjacent, dtype
                 assert np.array_equal(codes[which][p, fine, slot, 16 * g:16 * g + 16], want_c[row, fine, 16 * g:16 * g + 16])
                 assert _same(scales[which][p, fine, slot, g], want_s[row, fine, g])
     assert compared > 0.7 * 2 * tokens * kv_heads * groups  # an element in doubt makes its group so
+
+
+# what the rows' elements are, and the scale: the largest comes into fp16's range by a power of two, which the scale gives back
+SIZES = {"zero": (0.0, 1e-3), "zero, tiny scale": (0.0, 1e-30), "subnormal": (1e-40, 1e-4), "tiny": (2.0 ** -120, 2.0 ** -20), "least scale": (1.0, 1e-45), "zero, scale 1": (0.0, 1.0)}
+
+
+@pytest.mark.parametrize("size", list(SIZES))
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 256)])
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_rows_of_vanishing_queries_take_the_mean(new, dtype, dim, size):
+    """Scores of next to nothing: every seen key counts alike, and the masked ones not at all. One of the rows is an ordinary one."""
+    gain, scale = SIZES[size]
+    rng = _rng(192 + new)
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, [(new, 2 * new + 61), (1, 9)], 4, 2, dim, 16, dtype)
+    ordinary = q[0, 1].clone()
+    q *= gain
+    if gain == 0.0:
+        q[0, 1] = ordinary  # beside rows of zeros
+    q64 = q.double().cpu().numpy()
+    for mask in ((True, -1), (True, 20), (False, 7), (False, -1)):
+        want = O.attend(q64, k64, v64, table, starts, length, *mask, scale=scale)
+        for hint, out, lse in _attend_both(cache, q, table, starts, length, causal=mask[0], window=mask[1], scale=scale):
+            say(f"[packed attention, {size}] {new} {dtype} {dim} mask={mask} max_new={hint}")
+            _compare(out, lse, want, dtype, dim, _largest(v64))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_scores_of_huge_queries_and_zero_keys_are_zero(new, dtype):
+    """The scale and the largest element's power of two pass fp32 together: no score is 0 times infinity."""
+    def spoil(codes, scales, table):
+        codes[0][...] = 0
+        scales[0][...] = 0.0
+    rng = _rng(193 + new)
+    cache, k64, v64, q, _, table, starts, length = _filled(rng, [(new, 2 * new + 61)], 4, 2, 64, 16, dtype, spoil=spoil)
+    q = torch.full_like(q, 3e38)
+    q64 = q.double().cpu().numpy()
+    want = O.attend(q64, k64, v64, table, starts, length, scale=1e5)
+    for hint, out, lse in _attend_both(cache, q, table, starts, length, scale=1e5):
+        _compare(out, lse, want, dtype, 64, _largest(v64))
+    batch = _device(table, starts, length)
+    w = cache.weigh(q, lse, batch, torch.zeros(k64.shape[:3], device="cuda"), scale=1e5)
+    want, size = P.weigh(np.zeros(k64.shape[:3]), q64, lse.double().cpu().numpy(), k64, table, starts, length, scale=1e5)
+    _compare_weights(w.double().cpu().numpy(), want, size, 64, 1.0, 0.0, 2 * new)
