@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
   const auto element = [&](int i) { return W::kPacked ? 8 * (NG * quad + i) : 32 * i + 8 * quad; };
   // a block of rows, in the right operand's layout
   uint32_t qf[NG][kWords];
-  float less = 0.0f, factor = 0.0f;  // of the lane's row: lse in powers of two (infinite: it gives nothing); of a score, to powers of two
+  float less = 0.0f, factor = 0.0f;  // of the lane's row: lse in powers of two; of a score, to powers of two
+  bool gives = false;                // whether it is a row, and not left out by an lse of minus infinity
   int seen_lo = 0, seen_hi = -1;
 
   for (; unit < end; ++unit) {
@@ -210,7 +211,7 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       }
     };
     const auto take_rows = [&](int x, int r0) {  // what was fetched
-      less = raw_lse[x] == kNegInf || r0 + col >= rows_all ? -kNegInf : raw_lse[x] * kLog2e;
+      less = raw_lse[x] * kLog2e, gives = raw_lse[x] != kNegInf && r0 + col < rows_all;
       factor = p.scale_log2;
       if constexpr (W::kScaled) {
         float most = 0.0f;
@@ -364,10 +365,9 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
     floatx4 got[BLOCKS];
 #pragma unroll
     for (int j = 0; j < BLOCKS; ++j) got[j] = floatx4{};
-    // The held rows' scores with the held keys, and what they give. kAll: 16 rows, which see every key; kRows: so do those that there are.
+    // The held rows' scores with the held keys, and what they give. kAll: 16 rows that give, and see every key; kRows: those that give see every key.
     constexpr int kAll = 0, kRows = 1, kSome = 2;
     const auto add = [&](const uint32_t (&rows)[NG][kWords], int which) {
-      const bool gives = less != -kNegInf;
 #pragma unroll
       for (int j = 0; j < BLOCKS; ++j) {
         floatx4 score = floatx4{};
@@ -412,9 +412,8 @@ __global__ void __launch_bounds__(64 * kWaves, (Weigh<KIND, NG, SPLIT>::kWavesPe
       }
     };
     const int all_from = all0 * p.group, all_to = whole_keys ? (max(all1, -1) + 1) * p.group : 0;  // rows that see all of the wave's keys
-    const auto which_of = [&](int r0) {  // of the 16 rows from r0 on (uniform)
-      const int to = min(r0 + 16, rows_all);
-      return r0 < all_from || to > all_to ? kSome : to < r0 + 16 ? kRows : kAll;
+    const auto which_of = [&](int r0) {  // of the 16 rows from r0 on, which were taken (uniform)
+      return r0 < all_from || min(r0 + 16, rows_all) > all_to ? kSome : __all(gives) ? kAll : kRows;
     };
 
     if constexpr (SPLIT) {

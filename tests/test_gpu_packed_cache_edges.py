@@ -118,3 +118,37 @@ def test_scores_of_huge_queries_and_zero_keys_are_zero(new, dtype):
     w = cache.weigh(q, lse, batch, torch.zeros(k64.shape[:3], device="cuda"), scale=1e5)
     want, size = P.weigh(np.zeros(k64.shape[:3]), q64, lse.double().cpu().numpy(), k64, table, starts, length, scale=1e5)
     _compare_weights(w.double().cpu().numpy(), want, size, 64, 1.0, 0.0, 2 * new)
+
+
+@pytest.mark.parametrize("packed", [True, False], ids=["packed", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,new", [(64, 8), (128, 8), (64, 48), (128, 160), (256, 160)])
+def test_rows_that_are_left_out_by_their_lse_give_nothing(dtype, packed, dim, new):
+    """lse = -inf takes a row out, whatever it sees: a key that is NaN, in a block that all rows see or in one that some do not, gets nothing of it. An lse of
+    infinity is what the formula makes of it: no weight for finite scores."""
+    say(f"[weigh, left out] {dtype} packed={packed} {dim} {new}")
+    lens, heads, kv_heads, page = [(new, 400)], 4, 2, 16
+    bad = (20, 150, 400 - new + 1)  # seen by all rows, whole blocks around them; by some rows
+    rng = _rng(194 + dim)
+
+    def spoil(codes, scales, table):
+        for at in bad:
+            scales[0][table[0, at // page], 0, at % page] = np.nan
+    cache, k64, v64, q, q64, table, starts, length = _filled(rng, lens, heads, kv_heads, dim, page, dtype, spoil=spoil)
+    if not packed:
+        kp, k64 = _stored(k64, dtype)
+        cache = A.PagedCache(kp, kp)
+    with np.errstate(invalid="ignore"):
+        _, lse, _ = O.attend(q64, k64, np.zeros_like(k64), table, starts, length)
+    lse = lse.astype(np.float32)
+    lse[:, :2] = -np.inf       # the rows of the key head with NaN
+    lse[::3, 2] = -np.inf      # some of the other's
+    given = lse.copy()
+    given[1, 3] = np.inf       # the oracle's formula with its bound has no number for it
+    lse[1, 3] = -np.inf
+    before = rng.random(k64.shape[:3]).astype(np.float32)
+    for hint in sorted({0, new, 1}):
+        weights = cache.weigh(q, _gpu(given), _device(table, starts, length, max_new=hint), _gpu(before), decay=0.5)
+        want, size = P.weigh(before, q64, lse.astype(np.float64), k64, table, starts, length, decay=0.5)
+        assert np.isfinite(want).all()
+        _compare_weights(weights.double().cpu().numpy(), want, size, dim, 0.5, before, 2 * new)
