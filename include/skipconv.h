@@ -576,9 +576,9 @@ int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, con
  * tokens 0, 1, ... of the sequence in the pages of `into` (batch x
  * into_width), keys, values and weights; key heads keep tokens of their own. kept (batch x
  * kv_heads x keep) receives their positions, ascending, then -1, and lengths (batch)
- * how many they are. s: NULL for a float cache. Tokens that have no page in the
- * cache count less than any weight, and what has none on either side is not moved. The
- * pages of `into` must hold no token of the batch and be different ones: rows
+ * how many they are; neither may overlap kv_len, page_table, into or the other.
+ * s: NULL for a float cache. Tokens that have no page in the cache count less than
+ * any weight, and what has none on either side is not moved. The pages of `into` must hold no token of the batch and be different ones: rows
  * move in any order. Of c's batch, row_start is not looked at (it may be NULL). */
 typedef struct skipconv_evict {
   float* weights;        /* pages x kv_heads x page_size */

@@ -101,6 +101,12 @@ int check_weigh(const skipconv_cache* c, const skipconv_weigh* w) {
   return SKIPCONV_OK;
 }
 
+// Whether arrays of n and m 32-bit numbers share any.
+bool overlap(const void* a, int64_t n, const void* b, int64_t m) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + 4 * (uintptr_t)m && y < x + 4 * (uintptr_t)n;
+}
+
 int check_any_cache(const skipconv_cache* c, const skipconv_packing* s) {
   if (int e = check_cache(c, true, s ? 1 : elem_of(c))) return e;
   return s ? check_packing(c, s, true) : SKIPCONV_OK;
@@ -223,6 +229,16 @@ int skipconv_cache_evict(const skipconv_cache* c, const skipconv_packing* s, con
   if (!e->weights || !e->into || !e->lengths || !e->kept) return invalid("evict: NULL pointer");
   if (((uintptr_t)e->weights | (uintptr_t)e->into | (uintptr_t)e->lengths | (uintptr_t)e->kept) % 4 != 0) return invalid("evict: a tensor is not aligned to its elements");
   if ((int64_t)c->batch * c->kv_heads > kMostGroups / (std::min<int64_t>(e->keep, room) / 8 + 1)) return fail(SKIPCONV_E_UNSUPPORTED, "evict: too many rows");
+  // Both launches read the lengths and tables in many workgroups: what is written must lie elsewhere.
+  const int64_t places = (int64_t)c->batch * c->kv_heads * e->keep;
+  const struct {
+    const void* at;
+    int64_t n;
+  } read[] = {{c->kv_len, c->batch}, {c->page_table, (int64_t)c->batch * c->table_width}, {e->into, (int64_t)c->batch * e->into_width}};
+  for (const auto& r : read)
+    if (overlap(e->lengths, c->batch, r.at, r.n) || overlap(e->kept, places, r.at, r.n))
+      return invalid("evict: lengths and kept must not overlap kv_len, page_table or into");
+  if (overlap(e->lengths, c->batch, e->kept, places)) return invalid("evict: lengths and kept must not overlap");
   EvictParams p = {};
   fill_cache(&p.c, &no_rows);
   const int64_t unit = s ? 1 : elem_of(c);

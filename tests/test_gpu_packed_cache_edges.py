@@ -152,3 +152,32 @@ def test_rows_that_are_left_out_by_their_lse_give_nothing(dtype, packed, dim, ne
         want, size = P.weigh(before, q64, lse.astype(np.float64), k64, table, starts, length, decay=0.5)
         assert np.isfinite(want).all()
         _compare_weights(weights.double().cpu().numpy(), want, size, dim, 0.5, before, 2 * new)
+
+
+@pytest.mark.parametrize("packed", [True, False], ids=["packed", "paged"])
+def test_evict_takes_arrays_side_by_side(packed):
+    """Lengths and positions next to what the call reads, in one tensor: the C call's results are the class's."""
+    rng = _rng(197)
+    lens, heads, page, keep, recent = [(0, 90), (0, 33), (0, 64)], 2, 16, 40, 7
+    cache, _, _, _, _, table, starts, length = _filled(rng, lens, heads, heads, 64, page, "bf16")
+    if not packed:
+        cache = A.PagedCache(*(torch.randn((cache.pages, heads, page, 64), device="cuda").bfloat16() for _ in range(2)))
+    into = np.setdiff1d(np.arange(cache.pages), table)[:3, None].repeat(3, 1).astype(np.int32)  # the spare pages: not enough for all, so tokens go nowhere
+    into[:, 1:] = -1
+    weights = _gpu(rng.random((cache.pages, heads, page)).astype(np.float32))
+    start, held = weights.clone(), [x.clone() for x in cache._tensors]
+    want_lengths, want = cache.evict(weights, _device(table, starts, length), _gpu(into), keep=keep, recent=recent)
+    want_weights, want_held = weights.clone(), [x.clone() for x in cache._tensors]
+    sizes = [len(lens) * heads * keep, table.size, len(lens), len(lens), into.size]  # kept, table, kv_len, lengths, into
+    whole = torch.full((sum(sizes),), -5, dtype=torch.int32, device="cuda")
+    kept, tables, kv_len, lengths, to = whole.split(sizes)
+    tables.copy_(_gpu(table).flatten()), kv_len.copy_(_gpu(length)), to.copy_(_gpu(into).flatten())
+    weights.copy_(start)
+    for x, y in zip(cache._tensors, held):
+        x.copy_(y)
+    c = cache.desc(A.CacheBatch(tables.view(table.shape), _gpu(starts), kv_len), 0)
+    e = S.skipconv_evict(weights.data_ptr(), to.data_ptr(), lengths.data_ptr(), kept.data_ptr(), into.shape[1], keep, recent)
+    A.skipconv_cache_evict(c, cache._scales if packed else None, e, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(lengths, want_lengths) and torch.equal(kept.view(want.shape), want) and torch.equal(weights, want_weights)
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(cache._tensors, want_held))
+    assert np.array_equal(tables.cpu().numpy().reshape(table.shape), table) and np.array_equal(kv_len.cpu().numpy(), length)
