@@ -579,7 +579,9 @@ int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, con
  * how many they are; neither may overlap kv_len, page_table, into or the other.
  * s: NULL for a float cache. Tokens that have no page in the cache count less than
  * any weight, and what has none on either side is not moved. The pages of `into` must hold no token of the batch and be different ones: rows
- * move in any order. Of c's batch, row_start is not looked at (it may be NULL). */
+ * move in any order. Of c's batch, row_start is not looked at (it may be NULL).
+ * The next call's kv_len is lengths plus its new tokens (else these would take the
+ * places of the last ones kept), and `into` its page_table, with room for them too. */
 typedef struct skipconv_evict {
   float* weights;        /* pages x kv_heads x page_size */
   const int32_t* into;   /* device, batch x into_width */

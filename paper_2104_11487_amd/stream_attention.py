@@ -13,13 +13,22 @@ autograd; the other calls record no graph and refuse tensors that require a grad
     q = cache.append(k, v, batch, rotary=rotary, pos=pos, q=q)
     out = cache.attend(q, batch, causal=False)
 
-A long stream's cache is a PackedCache, in 4 bits, and is kept short by eviction:
+A long stream's cache is a PackedCache, in 4 bits, and is kept short by eviction. A batch's kv_len counts its new tokens, so they are added to
+the lengths that an eviction leaves, and the pages that it moves tokens to need room for them too:
 
+    new = 64 * 64  # tokens of a frame; 4096 earlier ones are kept
     cache = PackedCache.empty(pages=256, page_size=64, kv_heads=2, head_dim=64)
-    out, lse = cache.attend(q, batch, causal=False, return_lse=True)
-    cache.weigh(q, lse, batch, weights, causal=False)                      # weights: float32, pages x kv_heads x page_size
-    lengths, kept = cache.evict(weights, batch, other_pages, keep=4096, recent=256)
-    batch = CacheBatch(other_pages, row_start, lengths, max_new=64 * 64)
+    here, there = torch.arange(256, dtype=torch.int32, device="cuda").view(2, 1, 128)  # one sequence's pages, in turn: 128 hold 4096 + new tokens
+    row_start = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    lengths = torch.zeros(1, dtype=torch.int32, device="cuda")
+    weights = torch.empty(256, 2, 64, device="cuda")  # float32, pages x kv_heads x page_size
+    for q, k, v, pos in frames:
+        batch = CacheBatch(here, row_start, lengths + new, max_new=new)
+        q = cache.append(k, v, batch, rotary=rotary, pos=pos, q=q)
+        out, lse = cache.attend(q, batch, causal=False, return_lse=True)
+        cache.weigh(q, lse, batch, weights, causal=False)
+        lengths, kept = cache.evict(weights, batch, there, keep=4096, recent=256)
+        here, there = there, here
 """
 from __future__ import annotations
 
@@ -407,7 +416,8 @@ class _Cache:
         the largest weights (of equal ones the earlier). In their order they become the tokens of the sequence in the pages of `into`
         (int32, sequences x width): keys, values and weights. These pages must be different ones, and hold no token of the batch.
         Returns (lengths, kept): int32, the tokens of each sequence now, and their earlier positions, sequences x kv_heads x keep, -1 past
-        the last. What comes next is CacheBatch(into, row_start, lengths).
+        the last. The next tokens come behind them: CacheBatch(into, row_start, lengths + new), where new counts each sequence's new tokens (a batch's
+        kv_len holds them), for which `into` needs room too; with kv_len = lengths they would take the places of the last ones kept.
         """
         index = self._index
         self._weights(weights)

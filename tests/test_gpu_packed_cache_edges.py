@@ -3,6 +3,7 @@
 Bounds, and the caches that the tests are made of, are those of test_gpu_packed_cache.py.
 """
 import ctypes
+import textwrap
 
 import numpy as np
 import pytest
@@ -181,3 +182,43 @@ def test_evict_takes_arrays_side_by_side(packed):
     assert torch.equal(lengths, want_lengths) and torch.equal(kept.view(want.shape), want) and torch.equal(weights, want_weights)
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(cache._tensors, want_held))
     assert np.array_equal(tables.cpu().numpy().reshape(table.shape), table) and np.array_equal(kv_len.cpu().numpy(), length)
+
+
+def test_the_modules_example_keeps_what_it_kept():
+    """The loop of the module's documentation, as it stands there: what an eviction keeps, the next frame's tokens find."""
+    text = A.__doc__.split("kept short by eviction")[1].split("\n\n", 1)[1]
+    example = textwrap.dedent("\n".join(line for line in text.split("\n") if line.startswith("    ") or not line.strip()))
+    assert "evict(" in example and "for " in example
+    g = torch.Generator(device="cuda")
+    g.manual_seed(195)
+    new, kept_ones, appended = 64 * 64, [], []
+
+    def held(cache, pages, length):
+        return [x.transpose(0, 1).reshape(cache.kv_heads, -1, cache.head_dim)[:, :length].clone() for x in cache.unpack(pages)]
+
+    def frames():
+        for t in range(4):
+            if t:
+                kept_ones.append((names["kept"].clone(), held(names["cache"], names["here"][0], int(names["lengths"][0]))))
+            k, v, q = (torch.randn(new, h, 64, device="cuda", generator=g).bfloat16() for h in (2, 2, 8))
+            i = torch.arange(new, device="cuda")
+            yield q, k, v, torch.stack([torch.full_like(i, t), i // 64, i % 64], 1).int()
+        kept_ones.append((names["kept"].clone(), held(names["cache"], names["here"][0], int(names["lengths"][0]))))
+
+    class Watched(A.PackedCache):  # looks at what a frame's append leaves
+        def append(self, k, v, batch, **kw):
+            got = super().append(k, v, batch, **kw)
+            appended.append(held(self, batch.page_table[0], int(batch.kv_len[0])))
+            return got
+    names = dict(vars(A), torch=torch, frames=frames(), rotary=A.Rotary(A.axis_frequencies((11, 11, 10)), 64), PackedCache=Watched)
+    exec(compile(example, "example", "exec"), names)
+    assert len(kept_ones) == len(appended) == 4
+    for t, ((kept, values), all_of) in enumerate(zip(kept_ones, appended)):
+        before, total = (0 if t == 0 else 4096), all_of[0].shape[1]
+        assert total == before + new and (kept >= 0).all() and kept.shape == (1, 2, 4096)
+        for which in (0, 1):
+            if t:  # the tokens that were kept are there yet when the new ones have come
+                assert torch.equal(all_of[which][:, :before], kept_ones[t - 1][1][which])
+            for h in range(2):  # and the next ones to stay are taken from them all
+                assert torch.equal(values[which][h], all_of[which][h][kept[0, h].long()])
+        assert (kept[0, :, -256:] == torch.arange(total - 256, total, device="cuda")).all()
