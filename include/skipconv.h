@@ -532,8 +532,9 @@ typedef struct skipconv_packing {
 int skipconv_packed_append(const skipconv_cache* c, const skipconv_packing* s, const skipconv_append* a, void* stream);
 
 /* skipconv_cache_attend over such a cache: the same masks, batches, outputs
- * and lse. Values are taken exactly, queries exactly (fp32: to 22 bits of the
- * row's largest element); scores, sums and outputs are formed in 32 bits, and for bf16 the
+ * and lse. Values are taken exactly; queries of bf16 exactly where an element is at
+ * least 2^-31 of its row's largest, smaller ones to 2^-39 of that, queries of fp32 to
+ * 22 bits of it; scores, sums and outputs are formed in 32 bits, and for bf16 the
  * exponentials are rounded to fp16 for the product with v. Scales that make values
  * infinite (append writes none): a row that sees one may get NaN in its place. */
 int skipconv_packed_attend_workspace(const skipconv_cache* c, const skipconv_attend* a, size_t* bytes);

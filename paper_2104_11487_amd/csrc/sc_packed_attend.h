@@ -10,8 +10,9 @@
 //   Outputs: O' = V' P'. Lane (c, g) holds of the keys 4 g + r (r < 4) of each of the tile's two 16-key blocks the c-th 16th of the row's
 //   bytes, two elements a byte: the two nibbles of a byte position over the 8 keys are the operands of two products, which stand for the
 //   elements 2 NG c + j. A lane's scores are those of the same 8 keys, so the exponentials are the other operand as they are.
-// Values are fp16 by the format, and queries exact: bf16 rows are scaled by a power of two into fp16 (the factor goes into the
-// softmax's scale), fp32 rows are two fp16 parts (22 bits). Scores and sums are fp32. For bf16 the exponentials are rounded to fp16 (2^-11 of each)
+// Values are fp16 by the format. Queries: bf16 rows are scaled by a power of two into fp16 (the factor goes into the
+// softmax's scale), exactly but for elements below 2^-31 of their row's largest, whose last bits pass fp16's least step (off by 2^-39 of the largest at
+// most); fp32 rows are two fp16 parts (22 bits). Scores and sums are fp32. For bf16 the exponentials are rounded to fp16 (2^-11 of each)
 // for the product with V, for fp32 they are two parts; they are formed 2^7 too large, so that those of up to 2^-21 of the
 // reference's stay normal numbers.
 //

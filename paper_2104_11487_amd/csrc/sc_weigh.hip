@@ -5,8 +5,8 @@
 // A unit of work is a tile of keys of one sequence and key head; a workgroup takes an equal share of them in a row (lengths are on the device, so
 // the launch does not know how many there are). Where rows are few the four waves take keys of their own, and keep the rows' operand while the share
 // stays with a key head; where they are many the waves take the same keys and every fourth block of 16 rows, and are added in LDS, in wave
-// order: no atomics, equal calls give equal bits. Keys in 4 bits are fp16 numbers: few rows of bf16 come into fp16, exactly, by a power of two
-// (as in sc_packed_attend.h); for many rows, that would cost more than it saves, and the keys become two bf16 parts (8 + 3 bits) instead.
+// order: no atomics, equal calls give equal bits. Keys in 4 bits are fp16 numbers: few rows of bf16 come into fp16 by a power of two
+// (exactly but for the smallest elements, as in sc_packed_attend.h); for many rows, that would cost more than it saves, and the keys become two bf16 parts (8 + 3 bits) instead.
 //
 // Few rows are bound by the vector unit's work on codes and sums and by a unit's chain of latencies (page number, keys, old weight), three waves a
 // SIMD: one token of 32 sequences of up to 16384, 32 / 4 heads of 128 in 4 bits, 32 us, 2.9 TB/s. Many rows by the exponentials (a fused

@@ -222,3 +222,28 @@ def test_the_modules_example_keeps_what_it_kept():
             for h in range(2):  # and the next ones to stay are taken from them all
                 assert torch.equal(values[which][h], all_of[which][h][kept[0, h].long()])
         assert (kept[0, :, -256:] == torch.arange(total - 256, total, device="cuda")).all()
+
+
+@pytest.mark.parametrize("new", [1, 40, 300])
+def test_small_elements_beside_large_ones(new):
+    """bf16 elements of at least 2^-31 of their row's largest are taken exactly, smaller ones to 2^-39 of it. The large one meets a key's zero, so that the
+    score is the small one's alone, and of size one by the scale."""
+    kv, dim, page = 64, 64, 16
+    half = np.arange(kv).reshape(4, 1, page) >= kv // 2  # of these keys element 33 is one; all else is zero
+    codes, scales = np.zeros((4, 1, page, 32), np.uint8), np.zeros((4, 1, page, 2, 2), np.float16)
+    codes[..., 16] = np.where(half, 1 << 4, 0)
+    scales[..., 1, 0] = 1.0
+    cache = _packed([codes] * 2, [scales] * 2, dim, "bf16")
+    batch = _device(np.arange(4, dtype=np.int32)[None], np.array([0, new], np.int32), np.array([kv], np.int32))
+    large = 255 / 128  # all bits of the mantissa
+    slack = 4 * (2 * dim + 6) * U * large + 16 * U * (large + 1) + 2 * kv * U + 32 * U + 8 * U * np.log(kv * np.exp(large))
+    total = lambda s: np.log(kv // 2 * (1 + np.exp(s)))  # noqa: E731
+    for small in (-8, -25, -31, -33, -36, -39, -45):
+        say(f"[packed attention, 2^{small} beside 1] {new}")
+        q = torch.zeros((new, 2, dim), dtype=torch.bfloat16, device="cuda")
+        q[..., 2], q[:, 0, 33] = large, large * 2.0 ** small
+        _, lse = cache.attend(q, batch, causal=False, scale=2.0 ** -small, return_lse=True)
+        lse = lse.double().cpu().numpy()
+        off = 0.0 if small >= -31 else min(2.0 ** (-39 - small), 1.0) * large  # an element that vanishes is off by itself
+        assert (lse[:, 0] >= total(large - off) - slack).all() and (lse[:, 0] <= total(large + off) + slack).all(), small
+        assert np.abs(lse[:, 1] - np.log(kv)).max() <= slack
