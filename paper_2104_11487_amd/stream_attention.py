@@ -5,7 +5,7 @@ also torch-facing classes).
 A 1 x 1 ``SkipConv`` layer's activation output, N x H x W x (heads * head_dim), viewed as
 N*H*W x heads x head_dim, is a tensor of tokens that these calls take as it lies. Work is enqueued on the current torch
 stream of the tensors' device; nothing is copied to the host. An object's calls are not thread-safe. ``Rotary.__call__`` runs under
-autograd; the other calls record no graph and refuse tensors that require a gradient while gradients are recorded.
+autograd; the other calls record no graph and refuse tensors that require a gradient while gradients are recorded, or that carry a tangent.
 
     rotary = Rotary(axis_frequencies((11, 11, 10)), head_dim=64)
     cache = PagedCache.empty(pages=256, page_size=64, kv_heads=2, head_dim=64)
@@ -36,6 +36,7 @@ import ctypes
 from typing import Optional, Sequence
 
 import torch
+import torch.autograd.forward_ad as _forward
 
 from . import skipconv as _S
 
@@ -162,6 +163,13 @@ def _refuse_graph():
                      "calling the Rotary itself")
 
 
+def _refuse_tangents(*tensors) -> None:
+    """Forward-mode tangents, which torch.no_grad() leaves on: no call computes one. To be asked where a level of them is open."""
+    for t in tensors:
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            raise ValueError("this call computes no forward-mode gradient, and a tensor of it carries a tangent")
+
+
 def _fixed(name: str) -> property:
     """What a description took at construction: to be read, not replaced (the description would keep the address of a tensor that is gone)."""
     return property(lambda self: getattr(self, name))
@@ -212,6 +220,8 @@ class Rotary:
         tokens, heads, xt, xh = _heads_of(x, "x", None, None, dim, dtype, index)
         if _recording() and (x.requires_grad or self._freq.requires_grad or (out is not None and out.requires_grad)):
             _refuse_graph()
+        if _forward._current_level >= 0:
+            _refuse_tangents(x, self._freq, out)
         inverse = 1 if inverse else 0
         self.desc(pos, tokens, inverse)
         if out is None:
@@ -305,7 +315,9 @@ class _Cache:
         return c
 
     def _graph(self, *tensors) -> bool:
-        """Whether gradients are recorded and one of these tensors, or of the pages, requires one."""
+        """Whether gradients are recorded and one of these tensors, or of the pages, requires one. Tangents are refused at once."""
+        if _forward._current_level >= 0:
+            _refuse_tangents(*tensors, *self._tensors)
         if not _recording():
             return False
         for t in tensors:

@@ -16,7 +16,7 @@ from paper_2104_11487_amd import skipconv as S  # noqa: E402
 from paper_2104_11487_amd import stream_attention as A  # noqa: E402
 from parity_util import say  # noqa: E402
 from test_gpu_packed_cache import (DT, U, _attend_both, _batch, _certain, _compare, _compare_weights, _device, _filled, _garbage, _gpu, _held, _laid,  # noqa: E402
-                                   _largest, _packed, _rng, _same, _stored)
+                                   _largest, _packed, _rng, _same, _small, _stored)
 pytestmark = pytest.mark.gpu
 
 
@@ -247,3 +247,37 @@ def test_small_elements_beside_large_ones(new):
         off = 0.0 if small >= -31 else min(2.0 ** (-39 - small), 1.0) * large  # an element that vanishes is off by itself
         assert (lse[:, 0] >= total(large - off) - slack).all() and (lse[:, 0] <= total(large + off) + slack).all(), small
         assert np.abs(lse[:, 1] - np.log(kv)).max() <= slack
+
+
+def test_no_tangent_is_lost():
+    """Forward-mode tangents: the calls compute none, so tensors that carry one are refused, in every cache and in a rotation into a tensor."""
+    import torch.autograd.forward_ad as forward
+    cache, batch, q, weights = _small()
+    lse, into = torch.zeros(2, 4, device="cuda"), torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+    pages = [torch.zeros((cache.pages, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    rotary, pos = A.Rotary(A.axis_frequencies((11, 11, 10)), 64), torch.zeros((2, 3), dtype=torch.int32, device="cuda")
+    before = [x.clone() for x in cache._tensors]
+    with forward.dual_level():
+        dual = lambda x: forward.make_dual(x.clone(), torch.ones_like(x))  # noqa: E731
+        x = dual(q)
+        learned = A.PackedCache(*cache._tensors[:2], *(dual(t) for t in cache._tensors[2:]), cache.head_dim)
+        for c in (cache, A.PagedCache(*pages)):
+            for call in (lambda: c.append(x[:, :2], q[:, 2:], batch), lambda: c.append(q[:, :2], x[:, 2:], batch), lambda: c.append(q[:, :2], q[:, 2:], batch, rotary=rotary, pos=pos, q=x),
+                         lambda: c.attend(x, batch), lambda: c.attend(q, batch, out=dual(q)), lambda: c.weigh(x, lse, batch, weights), lambda: c.weigh(q, dual(lse), batch, weights),
+                         lambda: c.weigh(q, lse, batch, dual(weights)), lambda: c.evict(dual(weights), batch, into, keep=8)):
+                with pytest.raises(ValueError, match="gradient"):
+                    call()
+        for call in (lambda: learned.attend(q, batch), lambda: learned.unpack(into), lambda: learned.weigh(q, lse, batch, weights), lambda: rotary.rotate(x, pos),
+                     lambda: rotary.rotate(q, pos, out=dual(q)), lambda: A.PagedCache(dual(pages[0]), pages[1]).attend(q, batch)):
+            with pytest.raises(ValueError, match="gradient"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="gradient"):  # which leaves tangents on
+                call()
+        with pytest.raises((ValueError, RuntimeError)):
+            rotary(x, pos)
+        with torch.inference_mode():  # and that turns them off
+            cache.attend(x, batch)
+        plain = cache.attend(q, batch)  # tensors without one are as anywhere else
+        cache.weigh(q, lse, batch, weights.clone())
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, cache._tensors))
+    assert torch.equal(plain, cache.attend(q, batch))
