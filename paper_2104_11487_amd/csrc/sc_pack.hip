@@ -310,7 +310,8 @@ __global__ void __launch_bounds__(kThreads) unpack_kernel(UnpackParams p, int wo
   const CodeBits bits = code_bits();
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < items; i += (int64_t)gridDim.x * kThreads) {
     const int64_t row = i / words, entry = row / rows;
-    const int word = (int)(i - row * words), rest = (int)(row - entry * rows), h = rest / p.c.page_size, slot = rest - h * p.c.page_size;
+    const int64_t rest = row - entry * rows;  // heads and slots of a page together may pass 2^31
+    const int word = (int)(i - row * words), h = (int)divide(rest, p.c.page_size), slot = (int)(rest - (int64_t)h * p.c.page_size);
     const int page = p.list[entry];
     const bool there = page >= 0 && page < p.c.pages;
 #pragma unroll

@@ -281,3 +281,24 @@ def test_no_tangent_is_lost():
         cache.weigh(q, lse, batch, weights.clone())
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, cache._tensors))
     assert torch.equal(plain, cache.attend(q, batch))
+
+
+def test_unpack_of_a_page_of_more_than_2_to_31_rows():
+    """One page of 2049 heads of 2^20 slots: rows are counted past 32 bits. Codes of a slot are the same in every head, and the pairs of a head in every slot,
+    so that the cache itself is small; what it stands for is 69 GB."""
+    heads, page, dim = 2049, 1 << 20, 8
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 90 GB of free GPU memory")
+    rng = _rng(196)
+    codes = [_gpu(rng.integers(0, 256, (1, 1, page, 16)).astype(np.uint8)).expand(1, heads, page, 16) for _ in range(2)]
+    scales = [_gpu(rng.random((1, heads, 1, 1, 2)).astype(np.float16)).expand(1, heads, page, 1, 2) for _ in range(2)]
+    cache = A.PackedCache(*codes, *scales, dim)
+    got = cache.unpack(torch.zeros(1, dtype=torch.int32, device="cuda"))
+    for which in (0, 1):
+        for h in (0, 1, 1023, 2046, 2047, 2048):
+            c, s = (x[which][0, h if x is scales else 0].cpu().numpy() for x in (codes, scales))
+            assert np.array_equal(got[which][0, h].double().cpu().numpy(), P.values(c, s, dim)), (which, h)
+    del got
+    torch.cuda.empty_cache()
