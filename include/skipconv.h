@@ -490,7 +490,7 @@ typedef struct skipconv_attend {
   int32_t q_heads;       /* a multiple of kv_heads */
   int32_t causal;        /* 0 or 1 */
   int32_t window;
-  float scale;           /* > 0, finite */
+  float scale;           /* > 0, at most 2.3e38 */
   int32_t max_new;
 } skipconv_attend;
 
@@ -565,7 +565,7 @@ typedef struct skipconv_weigh {
   int32_t q_heads;       /* a multiple of kv_heads */
   int32_t causal;        /* 0 or 1 */
   int32_t window;
-  float scale;           /* > 0, finite */
+  float scale;           /* > 0, at most 2.3e38 */
   float decay;           /* finite */
   int32_t max_new;
 } skipconv_weigh;

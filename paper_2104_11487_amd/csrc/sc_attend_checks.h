@@ -97,11 +97,15 @@ inline void fill_cache(CacheView* v, const skipconv_cache* c) {
   v->magic = (uint32_t)(((1ull << (31 + v->shift)) + c->page_size - 1) / c->page_size);
 }
 
+// The factor of a score as the exponent of a power of two.
+inline float scale_log2_of(float scale) { return (float)((double)scale * 1.4426950408889634); }
+inline bool scale_ok(float scale) { return scale > 0.0f && std::isfinite(scale_log2_of(scale)); }  // infinite, it would make a score of zero NaN
+
 inline int check_attend(const skipconv_cache* c, const skipconv_attend* a) {
   if (a->q_heads < 1 || a->q_heads % c->kv_heads != 0) return invalid("attend: q_heads must be a multiple of kv_heads");
   if (c->tokens > kMostRows / a->q_heads) return fail(SKIPCONV_E_UNSUPPORTED, "attend: too many rows");
   if (a->causal != 0 && a->causal != 1) return invalid("attend: causal must be 0 or 1");
-  if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return invalid("attend: scale must be positive and finite");
+  if (!scale_ok(a->scale)) return invalid("attend: scale must be positive and at most 2.3e38");
   if (a->max_new < 0) return invalid("attend: max_new must be >= 0");
   return SKIPCONV_OK;
 }
@@ -162,7 +166,7 @@ inline int take_attend(const skipconv_cache* c, const skipconv_attend* a, Attend
   p->q_heads = a->q_heads, p->kv_heads = c->kv_heads, p->group = a->q_heads / c->kv_heads, p->dim = c->head_dim;
   p->causal = a->causal;
   p->window = a->window < 0 ? -1 : a->window;
-  p->scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+  p->scale_log2 = scale_log2_of(a->scale);
   return SKIPCONV_OK;
 }
 

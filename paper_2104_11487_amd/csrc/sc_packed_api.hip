@@ -95,7 +95,7 @@ int check_weigh(const skipconv_cache* c, const skipconv_weigh* w) {
   if (w->q_heads < 1 || w->q_heads % c->kv_heads != 0) return invalid("weigh: q_heads must be a multiple of kv_heads");
   if (c->tokens > (kMostRows - 1024) / w->q_heads) return fail(SKIPCONV_E_UNSUPPORTED, "weigh: too many rows");  // rows are counted ahead
   if (w->causal != 0 && w->causal != 1) return invalid("weigh: causal must be 0 or 1");
-  if (!(w->scale > 0.0f) || !std::isfinite(w->scale)) return invalid("weigh: scale must be positive and finite");
+  if (!scale_ok(w->scale)) return invalid("weigh: scale must be positive and at most 2.3e38");
   if (!std::isfinite(w->decay)) return invalid("weigh: decay must be finite");
   if (w->max_new < 0) return invalid("weigh: max_new must be >= 0");
   return SKIPCONV_OK;
@@ -205,7 +205,7 @@ int skipconv_cache_weigh(const skipconv_cache* c, const skipconv_packing* s, con
   p.q_heads = w->q_heads, p.kv_heads = c->kv_heads, p.group = w->q_heads / c->kv_heads, p.dim = c->head_dim, p.groups = pack_groups(c->head_dim);
   p.causal = w->causal, p.window = w->window < 0 ? -1 : w->window, p.packed = s != nullptr;
   p.whole = c->page_size % 16 == 0 && 16 * std::max(p.c.k_slot, p.s.k_slot) < (1ll << 30) && std::max(p.c.k_page, p.s.k_page) < (1ll << 32);
-  p.scale_log2 = (float)((double)w->scale * 1.4426950408889634), p.decay = w->decay;
+  p.scale_log2 = scale_log2_of(w->scale), p.decay = w->decay;
   p.tiles = ((int64_t)c->table_width * c->page_size + 31) / 32;
   const int64_t most = w->max_new > 0 ? std::min<int64_t>(w->max_new, c->tokens) : c->tokens;
   // The waves of a workgroup share a key tile's rows where these are many, else its keys. Over 8192 keys, heads of 64 of bf16 (of 128 in 4 bits),
