@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) pack_kernel(PackParams pp) {
       turns -= rint(turns);
       double c, s;
       sincospi(2.0 * turns, &s, &c);
-      s *= (double)p.sign;
+      s = p.sign < 0.0f ? -s : s;
       turn[i] = Turn{c, s, floatx2{(float)c, (float)s}};
     }
   }

@@ -51,7 +51,7 @@ __device__ __forceinline__ half8 values8(uint32_t w, uint32_t pair, const CodeBi
 // are 2^39 at most) and count as nothing; past 2^128 two that differ (by 2^-48 at least, lifted) do so by 2^80 or more.
 __device__ __forceinline__ int lift_of(float most) { return 141 - (int)((__float_as_uint(most) >> 23) & 255u); }
 __device__ __forceinline__ float factor_of(float scale_log2, int lift) {
-  return __builtin_amdgcn_fmed3f(ldexpf(scale_log2, -lift), __uint_as_float(0x00800000u), __uint_as_float(0x7f7fffffu));
+  return fminf(fmaxf(ldexpf(scale_log2, -lift), 0x1p-126f), 0x1.fffffep127f);
 }
 
 // Of two packed fp16 values those outside the mask become zero, and so do those that are infinite or NaN, which set *odd.
