@@ -506,8 +506,14 @@ template <int DP, int NR>
 hipError_t launch_packed_wide(const PackedAttendParams& p, hipStream_t stream) {
   const dim3 grid((unsigned)p.a.units), block(64 * packed_wide_waves(DP));
   if (p.a.keys != packed_wide_keys(DP) || (1 << p.a.log_rows) != 32 * NR * packed_wide_waves(DP)) return hipErrorInvalidValue;
-  if (p.a.target > 0) attend_packed_wide_kernel<DP, NR, true><<<grid, block, 0, stream>>>(p);
-  else attend_packed_wide_kernel<DP, NR, false><<<grid, block, 0, stream>>>(p);
+  if constexpr (NR == 1) {
+    if (p.a.target > 0) {
+      attend_packed_wide_kernel<DP, NR, true><<<grid, block, 0, stream>>>(p);
+      return hipGetLastError();
+    }
+  }
+  if (p.a.target > 0) return hipErrorInvalidValue;  // two blocks of rows are taken where they fill the GPU: nothing is shared
+  attend_packed_wide_kernel<DP, NR, false><<<grid, block, 0, stream>>>(p);
   return hipGetLastError();
 }
 
