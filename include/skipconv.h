@@ -553,7 +553,8 @@ int skipconv_packed_unpack(const skipconv_cache* c, const skipconv_packing* s, c
  *   head) that see l of exp(scale q . k_l - lse[i][h]),
  * for the new tokens themselves the sum alone (so their slots need no clearing). Masks
  * as in skipconv_cache_attend, whose lse this takes (rows with lse = -inf
- * give nothing). s: NULL for a float cache. Sums are formed in 32 bits in a fixed
+ * give nothing; keys that scales make infinite, which append writes none of, may
+ * get NaN). s: NULL for a float cache. Sums are formed in 32 bits in a fixed
  * order: equal calls give equal bits. Tokens whose page number is outside the cache are
  * left out. Two tokens of sequences with new ones that share a slot (pages of a common prefix) race. max_new: as in
  * skipconv_attend. */

@@ -6,9 +6,10 @@
 // nearest, ties to even. The turn is formed in 64 bits because a code changes where (y - low) / scale passes a half: so a code depends on the
 // inputs alone, not on how the call was cut. Queries turn as skipconv_rotate's.
 //
-// Four lanes hold a group, a word of eight codes each; a workgroup takes up to eight tokens, whose sines and cosines all heads share. Bound by the
-// vector unit (two 64-bit products and sums an element, a division where a quotient is near a half) and memory: 4 x 4096 tokens of 8 + 4 + 4 heads of 64
-// 28 us, 2.8 TB/s; 32 tokens 8 us, a chain of latencies. Reading back is bound by memory: 16 x 8192 tokens of 4 heads of 128, 352 MB, in 82 us, 4.3 TB/s.
+// Four lanes hold a group, a word of eight codes each; a workgroup takes up to eight tokens, whose sines and cosines all heads share. Many
+// tokens: 4 x 4096 of 8 + 4 + 4 heads of 64 28 us, 2 TB/s, bound neither by memory nor by the vector unit (two 64-bit products and sums an element, a
+// division where a quotient is near a half), which is busy for 47 % of the time: waves wait for half of theirs, for the loads of the first round and the
+// sines and cosines, and at each round's barrier, which queries that turn in place need. 32 tokens 8 us, a chain of latencies. Reading back is bound by memory: 16 x 8192 tokens of 4 heads of 128, 352 MB, in 82 us, 4.3 TB/s.
 #include "sc_packed_device.h"
 #include "sc_stream.h"
 
