@@ -407,7 +407,7 @@ class _Cache:
         """Adds the attention weight that each cached token received from the new tokens' queries to `weights` (float32, pages x kv_heads x
         page_size), and returns it: decay times what it held, plus the sum over the query heads and the new tokens that see it of exp(score - lse);
         a new token's own is set, so its slot needs no clearing. q, lse: what attend() took, and returned with return_lse; the mask and the
-        scale as there. Tokens of sequences without new ones stay as they are; sequences with new ones must not share slots.
+        scale as there. A row whose lse is -inf gives nothing. Tokens of sequences without new ones stay as they are; sequences with new ones must not share slots.
         """
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
