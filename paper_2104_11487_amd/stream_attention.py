@@ -293,6 +293,7 @@ class _Cache:
     def _describe(self, k: torch.Tensor, v: torch.Tensor, tensors, packing, append, attend, workspace):
         """k, v: what the C description's pages are; tensors: all that a call may write; packing: a reference to the C packing, or None."""
         self._tensors = tensors
+        self._first, self._second, self._more = tensors[0], tensors[1], tensors[2:]
         c = skipconv_cache()
         c.k_pages, c.v_pages = k.data_ptr(), v.data_ptr()
         c.k_page, c.k_head, c.k_slot = k.stride()[:3]
@@ -335,8 +336,13 @@ class _Cache:
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, _, kt, kh = _heads_of(k, "k", None, self._kv_heads, dim, dtype, index)
         _, _, vt, vh = _heads_of(v, "v", tokens, self._kv_heads, dim, dtype, index)
-        if self._graph(k, v, q, q_out, None if rotary is None else rotary._freq):
+        # (in line, as attend()'s: these are the calls whose time on the host a stream's step is made of)
+        if _recording() and (k.requires_grad or v.requires_grad or self._first.requires_grad or self._second.requires_grad
+                             or (q is not None and q.requires_grad) or (q_out is not None and q_out.requires_grad)
+                             or (rotary is not None and rotary._freq.requires_grad) or (self._more and self._graph())):
             _refuse_graph()
+        if _forward._current_level >= 0:
+            _refuse_tangents(k, v, q, q_out, None if rotary is None else rotary._freq, *self._tensors)
         a = skipconv_append(k.data_ptr(), v.data_ptr(), None, None, kt, kh, vt, vh)
         if rotary is not None:
             if pos is None or rotary._head_dim != dim:
@@ -374,8 +380,11 @@ class _Cache:
         """
         dim, dtype, index = self._head_dim, self._dtype, self._index
         tokens, heads, qt, qh = _heads_of(q, "q", None, None, dim, dtype, index)
-        if self._graph(q, out):
+        if _recording() and (q.requires_grad or self._first.requires_grad or self._second.requires_grad or (out is not None and out.requires_grad)
+                             or (self._more and self._graph())):
             _refuse_graph()
+        if _forward._current_level >= 0:
+            _refuse_tangents(q, out, *self._tensors)
         if out is None:
             out = _like(q)
             ot, oh = heads * dim, dim
